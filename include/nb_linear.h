@@ -278,6 +278,61 @@ int nb_lora_da_stacked(void *da_stack, const void *u_stack, const void *inp, int
 int nb_cast_f32_to_bf16(void *dst, const void *src, int64_t n, void *stream);
 
 /*
+ * Layer norm with the residual add in front of it (paper: Figure 1, the two norms of a block and the last one, each in front of
+ * a linear layer, behind the add of the layer before; Results/Speed names the add fused into the norm that follows it).
+ * Rows of C elements, C a multiple of 8 and at most NB_LAYERNORM_MAX_C; BT is arbitrary.
+ *
+ * nb_layernorm_forward:
+ *     s    = inp + branch, rounded to the stream's type (branch NULL: s = inp)
+ *     mean = sum_j s_j / C;  rstd = 1 / sqrt(sum_j (s_j - mean)^2 / C + eps)
+ *     out  = (s - mean) * rstd * weight + bias
+ *   out    [out] [BT, C] bf16: the input of the next linear layer
+ *   sum    [out] [BT, C] stream_dtype: s; given if and only if branch is
+ *   mean, rstd [out] [BT] fp32, for the backward pass; both or neither (inference)
+ *   inp    [in]  [BT, C] stream_dtype: the residual stream
+ *   branch [in]  [BT, C] bf16 or NULL: what the stream takes up, the output of a linear layer
+ *   weight [in]  [C] bf16;  bias [C] bf16 or NULL (16-byte aligned)
+ *   stream_dtype NB_DTYPE_BF16 or NB_DTYPE_F32
+ * Statistics, deviations and products are held in fp32; s and out are rounded once each. sum may be inp, and out may be branch.
+ * Any other overlap of an output with an input is not allowed.
+ * A row with an infinity or a NaN gives NaN in that row alone. BT == 0 does nothing.
+ *
+ * nb_layernorm_backward, with s, mean and rstd of the forward pass, xh = (s - mean) * rstd and g = dout * weight:
+ *     dinp    = dres + rstd * (g - mean_j(g) - xh * mean_j(g * xh))
+ *     dweight (+)= sum over rows of dout * xh;  dbias (+)= sum over rows of dout
+ *   dinp    [out] [BT, C] stream_dtype: the stream's gradient, which is that of branch too
+ *   dbranch [out] [BT, C] bf16 or NULL: the same, rounded to bf16 (once, from fp32): the dout of the linear layer that made branch
+ *   dweight, dbias [i/o] [C] fp32 or NULL; accumulate as in nb_linear_backward. Summed in a fixed order.
+ *   dout    [in]  [BT, C] bf16;  dres [BT, C] stream_dtype or NULL: the stream's gradient from above
+ *   inp     [in]  [BT, C] stream_dtype: s (the forward's sum, or its inp where there was no branch)
+ *   workspace     device memory of nb_layernorm_workspace(BT, C) bytes, 16-byte aligned, the caller's: calls that may run at the same
+ *                 time (on two streams, in two graphs) take one each. NULL is enough where dweight and dbias are NULL.
+ * dinp may be dres, and dbranch may be dout. BT == 0: dinp untouched, dweight and dbias zeroed when accumulate == 0.
+ * nb_layernorm_workspace returns -1 for sizes that the call would refuse.
+ */
+#define NB_LAYERNORM_MAX_C 8192
+int nb_layernorm_forward(void *out, void *sum, void *mean, void *rstd, const void *inp, const void *branch,
+                         const void *weight, const void *bias, int64_t BT, int64_t C, float eps,
+                         int stream_dtype, void *stream);
+int64_t nb_layernorm_workspace(int64_t BT, int64_t C);
+int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias, const void *dout,
+                          const void *dres, const void *inp, const void *mean, const void *rstd,
+                          const void *weight, int64_t BT, int64_t C, int accumulate, int stream_dtype,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Application of an update to the master weights, with the compute copies of the next step (takes the place of
+ * nb_cast_f32_to_bf16 in a step), for n tensors of `count` elements each:
+ *     master <- decay * master - step * update;  weight <- bf16(master)
+ *   master [i/o] n fp32 tensors;  weight [out] n bf16 tensors, or NULL for none;  update [in] n bf16 tensors
+ * The three are host arrays of n device pointers, each 16-byte aligned; the arrays are read before the call returns. With learning rate lr
+ * and weight decay wd, decay = 1 - lr * wd and step = lr times the update's scale. n at most NB_MUON_MAX_N. No tensor may be given twice.
+ */
+#define NB_MUON_MAX_N 1024
+int nb_muon_apply(void *const *master, void *const *weight, const void *const *update, int64_t n,
+                  int64_t count, float decay, float step, void *stream);
+
+/*
  * Bias gradient of a GELU layer without any allocation (the paper has no counterpart; this
  * exists for callers that must not allocate device memory):
  *

@@ -29,7 +29,8 @@ EXPORTS = (
     "nb_debug_split_plan", "nb_cast_f32_to_bf16", "nb_lm_head_ce_forward", "nb_ce_backward",
     "nb_lora_linear_forward", "nb_lora_linear_backward", "nb_debug_layer_bwd_plan", "nb_debug_gemm_timeout",
     "nb_lora_down_stacked", "nb_lora_linear_forward_stacked", "nb_lora_linear_backward_stacked",
-    "nb_lora_da_stacked", "nb_debug_route",
+    "nb_lora_da_stacked", "nb_debug_route", "nb_layernorm_forward", "nb_layernorm_workspace", "nb_layernorm_backward",
+    "nb_muon_apply",
 )
 
 CALL_FORWARD, CALL_BACKWARD, CALL_LORA_FORWARD, CALL_LORA_BACKWARD = range(4)
@@ -78,6 +79,11 @@ def lib() -> ctypes.CDLL:
         L.nb_lora_da_stacked.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, _int, _vp]
         L.nb_lm_head_ce_forward.argtypes = [_vp] * 6 + [_i64] * 4 + [_vp]
         L.nb_ce_backward.argtypes = [_vp] * 4 + [ctypes.c_float] + [_i64] * 3 + [_vp]
+        L.nb_layernorm_forward.argtypes = [_vp] * 8 + [_i64] * 2 + [ctypes.c_float, _int, _vp]
+        L.nb_layernorm_workspace.argtypes = [_i64] * 2
+        L.nb_layernorm_workspace.restype = _i64
+        L.nb_layernorm_backward.argtypes = [_vp] * 10 + [_i64] * 2 + [_int] * 2 + [_vp, _i64, _vp]
+        L.nb_muon_apply.argtypes = [ctypes.POINTER(_vp)] * 3 + [_i64] * 2 + [ctypes.c_float] * 2 + [_vp]
         L.nb_debug_split_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int)]
         L.nb_debug_gemm_timeout.argtypes = [_vp, _vp, _vp, _i64]
         L.nb_debug_layer_bwd_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int), _i64]
@@ -120,6 +126,12 @@ def _stream_address(s):
             raise TypeError(f"a stream or its address is wanted, not {type(s).__name__}")
         s = s._as_parameter_
     return s.value if isinstance(s, ctypes.c_void_p) else s
+
+
+def _size(nbytes: int, what: str) -> int:
+    if nbytes < 0:
+        raise NbError(NB_ERR_UNSUPPORTED, f"{what}: no such size")
+    return nbytes
 
 
 def _check(rc: int) -> None:
@@ -249,6 +261,30 @@ def nb_cast_f32_to_bf16(dst, src, n, stream=None) -> None:
     (_native or _load_native()).nb_cast_f32_to_bf16(dst, src, n, stream)
 
 
+def nb_layernorm_forward(out, sum, mean, rstd, inp, branch, weight, bias, BT, C, eps, stream_dtype, stream=None) -> None:
+    """s = inp + branch (stored in sum, in the stream's type; branch None: s = inp); out = layer norm of s; mean and rstd for the backward
+    pass, or None."""
+    (_native or _load_native()).nb_layernorm_forward(out, sum, mean, rstd, inp, branch, weight, bias, BT, C, eps, stream_dtype,
+                                                     stream)
+
+
+def nb_layernorm_workspace(BT: int, C: int) -> int:
+    """Bytes of workspace that nb_layernorm_backward needs for dweight and dbias."""
+    return _size(lib().nb_layernorm_workspace(BT, C), f"layer norm of [{BT}, {C}]")
+
+
+def nb_layernorm_backward(dinp, dbranch, dweight, dbias, dout, dres, inp, mean, rstd, weight, BT, C, accumulate, stream_dtype,
+                          workspace, workspace_bytes, stream=None) -> None:
+    """dinp = dres + the norm's input gradient (dbranch: the same in bf16); dweight, dbias (+)= column sums."""
+    (_native or _load_native()).nb_layernorm_backward(dinp, dbranch, dweight, dbias, dout, dres, inp, mean, rstd, weight, BT, C,
+                                                      accumulate, stream_dtype, workspace, workspace_bytes, stream)
+
+
+def nb_muon_apply(master, weight, update, n, count, decay, step, stream=None) -> None:
+    """master <- decay * master - step * update, weight <- bf16(master), for n tensors of count elements given as sequences."""
+    (_native or _load_native()).nb_muon_apply(master, weight, update, n, count, decay, step, stream)
+
+
 def nb_debug_split_plan(M: int, N: int, K: int, slots: int, tile_m: int):
     """(row tiles, column tiles, split-K factor, k-blocks per split, k-blocks) of a wgrad."""
     out = (_int * 5)()
@@ -314,3 +350,39 @@ def linear_backward(dout, inp, weight, pre_act=None, inp_pre_act=None, act=ACT_N
     """Allocate missing outputs and call nb_linear_backward_ex. Returns (dinp, dweight, dbias)."""
     return (_native or _load_native()).linear_backward(dout, inp, weight, pre_act, inp_pre_act, act, dweight, dbias,
                                                        accumulate, need_dinp, need_dweight, need_dbias)
+
+
+def _stream_dtype(t) -> int:
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"the residual stream is bf16 or fp32, not {t.dtype}")
+    return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
+
+
+def layernorm_forward(inp, weight, bias=None, branch=None, eps=1e-5, train=True):
+    """Allocate the outputs and call nb_layernorm_forward. inp [BT, C] is the residual stream (bf16 or fp32), branch what it takes
+    up (bf16). Returns (out, sum, mean, rstd): sum is inp where there is no branch; mean and rstd are None unless train."""
+    BT, C = inp.shape
+    out = torch.empty((BT, C), dtype=torch.bfloat16, device=inp.device)
+    total = None if branch is None else torch.empty_like(inp)
+    mean, rstd = (torch.empty(BT, dtype=torch.float32, device=inp.device) for _ in range(2)) if train else (None, None)
+    nb_layernorm_forward(out, total, mean, rstd, inp, branch, weight, bias, BT, C, eps, _stream_dtype(inp))
+    return out, inp if branch is None else total, mean, rstd
+
+
+def layernorm_backward(dout, inp, mean, rstd, weight, dres=None, dweight=None, dbias=None, accumulate=False, need_dweight=True,
+                       need_dbias=True):
+    """Allocate missing outputs and call nb_layernorm_backward. inp is the sum that the forward pass normed. Returns (dinp, dbranch,
+    dweight, dbias): dinp in the stream's type, dbranch the same in bf16 (dinp itself where the stream is bf16)."""
+    BT, C = inp.shape
+    dtype = _stream_dtype(inp)
+    dinp = torch.empty_like(inp)
+    dbranch = dinp if dtype == DTYPE_BF16 else torch.empty((BT, C), dtype=torch.bfloat16, device=inp.device)
+    if need_dweight and dweight is None:
+        dweight = torch.zeros(C, dtype=torch.float32, device=inp.device) if accumulate else torch.empty(C, dtype=torch.float32, device=inp.device)
+    if need_dbias and dbias is None:
+        dbias = torch.zeros(C, dtype=torch.float32, device=inp.device) if accumulate else torch.empty(C, dtype=torch.float32, device=inp.device)
+    ws = torch.empty(nb_layernorm_workspace(BT, C) if need_dweight or need_dbias else 0, dtype=torch.uint8, device=inp.device)
+    nb_layernorm_backward(dinp, None if dbranch is dinp else dbranch, dweight if need_dweight else None,
+                          dbias if need_dbias else None, dout, dres, inp, mean, rstd, weight, BT, C, int(accumulate), dtype,
+                          ws, ws.numel())
+    return dinp, dbranch, dweight, dbias

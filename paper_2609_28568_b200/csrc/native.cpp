@@ -10,6 +10,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -17,6 +18,7 @@
 #include <tuple>
 #include <type_traits>
 #include <utility>
+#include <vector>
 
 #include "nb_linear.h"
 
@@ -95,8 +97,20 @@ bool convert(PyObject *o, T &v)
     return true;
 }
 
+// Whether a tensor lies on the device that the call will launch on. The operators that came with this check refuse another
+// device's tensors; the older calls leave that to the caller.
+bool on_current_device(PyObject *o)
+{
+    if (!THPVariable_Check(o)) return true;  // an address: the caller's own business
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.get_device() == c10::cuda::current_device()) return true;
+    PyErr_Format(PyExc_ValueError, "a tensor lies on device %d, the current device is %d", static_cast<int>(t.get_device()),
+                 static_cast<int>(c10::cuda::current_device()));
+    return false;
+}
+
 // fn(args..., stream): the last argument may be left out or None, for the current stream.
-template <class... A, size_t... I>
+template <bool DEVICE_CHECKED, class... A, size_t... I>
 PyObject *call(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, std::index_sequence<I...>)
 {
     constexpr Py_ssize_t N = sizeof...(A);
@@ -115,6 +129,9 @@ PyObject *call(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, std::index_
         return convert(args[i], dst);
     };
     if (!(one(std::get<I>(v), I) && ...)) return nullptr;
+    if constexpr (DEVICE_CHECKED)
+        for (Py_ssize_t i = 0; i < N - 1; ++i)
+            if (!on_current_device(args[i])) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = std::apply(fn, v);
@@ -123,12 +140,12 @@ PyObject *call(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, std::index_
     Py_RETURN_NONE;
 }
 
-template <auto fn>
+template <auto fn, bool DEVICE_CHECKED = false>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     return [&]<class... A>(int (*f)(A...)) {
-        return call(f, args, n, std::index_sequence_for<A...>{});
+        return call<DEVICE_CHECKED>(f, args, n, std::index_sequence_for<A...>{});
     }(fn);
     END_HANDLE_TH_ERRORS
 }
@@ -222,6 +239,56 @@ PyObject *linear_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// n device pointers from a sequence of tensors and addresses. Empty for None.
+struct Pointers {
+    std::vector<void *> p;
+    bool given = false;
+    void **data() { return given ? p.data() : nullptr; }
+};
+bool to_pointers(PyObject *o, Pointers &v, int64_t n, const char *name)
+{
+    if (o == Py_None) return true;
+    PyObject *seq = PySequence_Fast(o, "a sequence of tensors is wanted");
+    if (!seq) return false;
+    bool ok = PySequence_Fast_GET_SIZE(seq) == n;
+    if (!ok) PyErr_Format(PyExc_ValueError, "%s has %zd tensors, not %lld", name, PySequence_Fast_GET_SIZE(seq), static_cast<long long>(n));
+    if (ok) v.p.resize(static_cast<size_t>(n));
+    for (int64_t i = 0; ok && i < n; ++i) {
+        PyObject *t = PySequence_Fast_GET_ITEM(seq, i);
+        ok = to_pointer(t, v.p[static_cast<size_t>(i)]) && on_current_device(t);
+    }
+    Py_DECREF(seq);
+    v.given = ok;
+    return ok;
+}
+bool to_stream_or_current(PyObject *const *args, Py_ssize_t n, Py_ssize_t at, void *&stream)
+{
+    if (n <= at || args[at] == Py_None) return stream = current_stream(), true;
+    return to_stream(args[at], stream);
+}
+
+// nb_muon_apply(master, weight or None, update, n, count, decay, step, stream)
+PyObject *muon_apply(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    Pointers master, weight, update;
+    int64_t n = 0, count = 0;
+    float decay = 0, step = 0;
+    void *stream = nullptr;
+    if (nargs != 7 && nargs != 8) return PyErr_Format(PyExc_TypeError, "7 or 8 arguments are wanted, not %zd", nargs);
+    if (!convert(args[3], n) || !convert(args[4], count) || !convert(args[5], decay) || !convert(args[6], step) ||
+        !to_pointers(args[0], master, n, "master") || !to_pointers(args[1], weight, n, "weight") ||
+        !to_pointers(args[2], update, n, "update") || !to_stream_or_current(args, nargs, 7, stream))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nb_muon_apply(master.data(), weight.data(), update.data(), n, count, decay, step, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != NB_OK) return raise(rc);
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 // set_python(NbError, pointer_of, stream_of)
 PyObject *set_python(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -233,6 +300,8 @@ PyObject *set_python(PyObject *, PyObject *const *args, Py_ssize_t n)
 }
 
 #define NB_ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&entry<name>)), METH_FASTCALL, nullptr}
+#define NB_ENTRY_CHECKED(name) \
+    {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&entry<name, true>)), METH_FASTCALL, nullptr}
 #define NB_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     NB_ENTRY(nb_linear_forward_ex),
@@ -247,6 +316,9 @@ PyMethodDef g_methods[] = {
     NB_ENTRY(nb_lm_head_ce_forward),
     NB_ENTRY(nb_ce_backward),
     NB_ENTRY(nb_cast_f32_to_bf16),
+    NB_ENTRY_CHECKED(nb_layernorm_forward),
+    NB_ENTRY_CHECKED(nb_layernorm_backward),
+    {"nb_muon_apply", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&muon_apply)), METH_FASTCALL, nullptr},
     NB_FAST(linear_forward),
     NB_FAST(linear_backward),
     NB_FAST(set_python),

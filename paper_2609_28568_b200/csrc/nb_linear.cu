@@ -12,12 +12,15 @@
 #include <cstring>
 #include <mutex>
 #include <string>
+#include <type_traits>
 #include <unordered_map>
 
 #include "elementwise.cuh"
 #include "gemm_sm100.cuh"
 #include "layer_bwd_sm100.cuh"
 #include "lora_udb_sm100.cuh"
+#include "muon.cuh"
+#include "norm.cuh"
 #include "rows_sm100.cuh"
 #include "tile_sm100.cuh"
 
@@ -388,6 +391,24 @@ int launch_chained(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = dependent_launch_allowed(stream) ? 1 : 0;
+    NB_CUDA(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
+    return NB_OK;
+}
+
+// The same with dynamic shared memory.
+template <class... P, class... A>
+int launch_chained_smem(void (*kernel)(P...), dim3 grid, int threads, size_t smem_bytes, cudaStream_t stream, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem_bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1718,6 +1739,88 @@ int run_lora_backward(DeviceState &s, const LoraBwd &l, cudaStream_t stream)
     return want_a ? run_wgrad_f32(s, l.u, l.inp, l.dlora_a, nullptr, BT, r, C, l.accumulate, stream) : NB_OK;
 }
 
+// ----------------------------------------------------------------------------- layer norm
+// Threads of a row's team and vectors per thread by the row's length: a warp up to 1024 elements, where its
+// shuffles are all the meeting it needs, a block above.
+struct NormForm {
+    int threads, nv;
+};
+NormForm norm_form(int64_t C)
+{
+    const int nvec = static_cast<int>(C / 8);
+    if (nvec <= 128) return {32, (nvec + 31) / 32};
+    if (nvec <= 512) return {256, (nvec + 255) / 256};
+    return {512, 2};
+}
+
+// Blocks of a backward pass, by sizes alone so that the workspace is known before the device is: up to two of
+// eight warps on each of 148 SMs.
+int norm_backward_blocks(int64_t BT, int64_t C)
+{
+    const NormForm f = norm_form(C);
+    const int64_t teams = f.threads == 32 ? 8 : 1;
+    const int64_t blocks = (BT + teams - 1) / teams, most = f.threads == 512 ? 148 : 296;
+    return static_cast<int>(blocks < most ? blocks : most);
+}
+
+template <bool F32, int T, int NV>
+int launch_norm_forward(DeviceState &s, const NormForward &p, cudaStream_t stream)
+{
+    constexpr int teams = kNormThreads<T> / T;
+    const long long blocks = (p.BT + teams - 1) / teams, most = 8ll * s.num_sms;
+    return launch_chained(layernorm_forward_kernel<F32, T, NV>, dim3(static_cast<unsigned>(blocks < most ? blocks : most)),
+                          kNormThreads<T>, stream, p);
+}
+
+template <bool F32, int T, int NV>
+int launch_norm_backward(DeviceState &s, const NormBackward &p, int blocks, cudaStream_t stream)
+{
+    const size_t smem = T == 32 && p.part ? static_cast<size_t>(p.nvec) * 8 * 64 : 0;  // eight warps' sums
+    static bool attr_set[kMaxDevices] = {};
+    int dev = 0;
+    NB_CUDA(cudaGetDevice(&dev));
+    if (T == 32 && !attr_set[dev]) {
+        NB_CUDA(cudaFuncSetAttribute(layernorm_backward_kernel<F32, T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     NV * 32 * 8 * 64));
+        attr_set[dev] = true;
+    }
+    (void)s;
+    return launch_chained_smem(layernorm_backward_kernel<F32, T, NV>, dim3(static_cast<unsigned>(blocks)), kNormThreads<T>, smem,
+                               stream, p);
+}
+
+template <int V>
+using IntC = std::integral_constant<int, V>;
+// fn(threads, vectors) of the form, as constants
+template <class F>
+int with_norm_form(const NormForm &f, F &&fn)
+{
+    if (f.threads == 32) {
+        switch (f.nv) {
+            case 1: return fn(IntC<32>{}, IntC<1>{});
+            case 2: return fn(IntC<32>{}, IntC<2>{});
+            case 3: return fn(IntC<32>{}, IntC<3>{});
+            default: return fn(IntC<32>{}, IntC<4>{});
+        }
+    }
+    if (f.threads == 256) return f.nv == 1 ? fn(IntC<256>{}, IntC<1>{}) : fn(IntC<256>{}, IntC<2>{});
+    return fn(IntC<512>{}, IntC<2>{});
+}
+
+int check_norm(int64_t BT, int64_t C, int stream_dtype)
+{
+    if (BT < 0 || C <= 0) return fail(NB_ERR_INVALID_ARG, "negative or zero dimension");
+    if (stream_dtype != NB_DTYPE_F32 && stream_dtype != NB_DTYPE_BF16)
+        return fail(NB_ERR_INVALID_ARG, "unknown stream_dtype %d", stream_dtype);
+    if (C % 8 != 0 || C > NB_LAYERNORM_MAX_C)
+        return fail(NB_ERR_UNSUPPORTED, "C (%lld) must be a multiple of 8 and at most %d", static_cast<long long>(C),
+                    NB_LAYERNORM_MAX_C);
+    if (BT >= (1ll << 31) || BT * C >= (1ll << 40)) return fail(NB_ERR_UNSUPPORTED, "dimension too large");
+    return NB_OK;
+}
+
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
 }  // namespace
 
 // ================================================================================ C ABI
@@ -2197,6 +2300,144 @@ int nb_cast_f32_to_bf16(void *dst, const void *src, int64_t n, void *stream_)
                         static_cast<__nv_bfloat16 *>(dst), static_cast<const float *>(src), n);
     if (rc != NB_OK) return rc;
     ++g_launches;
+    return NB_OK;
+}
+
+// ----------------------------------------------------------------------------- layer norm
+int nb_layernorm_forward(void *out, void *sum, void *mean, void *rstd, const void *inp, const void *branch, const void *weight,
+                         const void *bias, int64_t BT, int64_t C, float eps, int stream_dtype, void *stream_)
+{
+    int rc = check_norm(BT, C, stream_dtype);
+    if (rc != NB_OK) return rc;
+    if (!(eps >= 0.0f) || eps > 3.0e38f) return fail(NB_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (BT == 0) return NB_OK;  // tensors without elements have no address
+    if (!out || !inp || !weight) return fail(NB_ERR_INVALID_ARG, "out, inp and weight must not be NULL");
+    if (!branch != !sum) return fail(NB_ERR_INVALID_ARG, "branch and sum are given together or not at all");
+    if (!mean != !rstd) return fail(NB_ERR_INVALID_ARG, "mean and rstd are given together or not at all");
+    if (!aligned16(out) || !aligned16(sum) || !aligned16(inp) || !aligned16(branch) || !aligned16(weight) || !aligned16(bias) ||
+        !aligned4(mean) || !aligned4(rstd))
+        return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, mean and rstd 4-byte aligned");
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    if ((rc = get_state(&s)) != NB_OK) return rc;
+    NormForward p{};
+    p.out = out;
+    p.sum = sum;
+    p.mean = static_cast<float *>(mean);
+    p.rstd = static_cast<float *>(rstd);
+    p.inp = inp;
+    p.branch = branch;
+    p.weight = weight;
+    p.bias = bias;
+    p.BT = BT;
+    p.nvec = static_cast<int>(C / 8);
+    p.inv_c = static_cast<float>(1.0 / static_cast<double>(C));
+    p.eps = eps;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    rc = with_norm_form(norm_form(C), [&](auto T, auto NV) {
+        return stream_dtype == NB_DTYPE_F32 ? launch_norm_forward<true, T.value, NV.value>(*s, p, stream)
+                                            : launch_norm_forward<false, T.value, NV.value>(*s, p, stream);
+    });
+    if (rc != NB_OK) return rc;
+    ++g_launches;
+    return NB_OK;
+}
+
+int64_t nb_layernorm_workspace(int64_t BT, int64_t C)
+{
+    if (BT < 0 || C <= 0 || C % 8 != 0 || C > NB_LAYERNORM_MAX_C) return -1;
+    return static_cast<int64_t>(norm_backward_blocks(BT, C)) * 2 * C * static_cast<int64_t>(sizeof(float));
+}
+
+int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias, const void *dout, const void *dres, const void *inp,
+                          const void *mean, const void *rstd, const void *weight, int64_t BT, int64_t C, int accumulate,
+                          int stream_dtype, void *workspace, int64_t workspace_bytes, void *stream_)
+{
+    int rc = check_norm(BT, C, stream_dtype);
+    if (rc != NB_OK) return rc;
+    if (BT > 0 && (!dinp || !dout || !inp || !mean || !rstd || !weight))  // tensors without elements have no address
+        return fail(NB_ERR_INVALID_ARG, "dinp, dout, inp, mean, rstd and weight must not be NULL");
+    if (!aligned16(dinp) || !aligned16(dbranch) || !aligned16(dout) || !aligned16(dres) || !aligned16(inp) || !aligned16(weight) ||
+        !aligned16(dweight) || !aligned16(dbias) || !aligned16(workspace) || !aligned4(mean) || !aligned4(rstd))
+        return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, mean and rstd 4-byte aligned");
+    const bool grads = dweight || dbias;
+    if (grads && BT > 0 && (!workspace || workspace_bytes < nb_layernorm_workspace(BT, C)))
+        return fail(NB_ERR_INVALID_ARG, "dweight and dbias need a workspace of %lld bytes (nb_layernorm_workspace)",
+                    static_cast<long long>(nb_layernorm_workspace(BT, C)));
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (BT == 0) {
+        if (accumulate || !grads) return NB_OK;
+        if ((rc = get_state(&s)) != NB_OK) return rc;
+        return launch_clear(*s, dweight ? dweight : dbias, C, dweight ? dbias : nullptr, C, stream);
+    }
+    if ((rc = get_state(&s)) != NB_OK) return rc;
+    NormBackward p{};
+    p.dinp = dinp;
+    p.dbranch = dbranch;
+    p.part = grads ? static_cast<float *>(workspace) : nullptr;
+    p.dout = dout;
+    p.dres = dres;
+    p.inp = inp;
+    p.mean = static_cast<const float *>(mean);
+    p.rstd = static_cast<const float *>(rstd);
+    p.weight = weight;
+    p.BT = BT;
+    p.nvec = static_cast<int>(C / 8);
+    p.inv_c = static_cast<float>(1.0 / static_cast<double>(C));
+    const int blocks = norm_backward_blocks(BT, C);
+    rc = with_norm_form(norm_form(C), [&](auto T, auto NV) {
+        return stream_dtype == NB_DTYPE_F32 ? launch_norm_backward<true, T.value, NV.value>(*s, p, blocks, stream)
+                                            : launch_norm_backward<false, T.value, NV.value>(*s, p, blocks, stream);
+    });
+    if (rc != NB_OK) return rc;
+    ++g_launches;
+    if (!grads) return NB_OK;
+    rc = launch_chained(layernorm_reduce_kernel, dim3(static_cast<unsigned>((2 * C + 31) / 32)), 256, stream,
+                        static_cast<float *>(dweight), static_cast<float *>(dbias), static_cast<const float *>(p.part), blocks,
+                        static_cast<int>(C), accumulate);
+    if (rc != NB_OK) return rc;
+    ++g_launches;
+    return NB_OK;
+}
+
+// ----------------------------------------------------------------------------- orthogonalised momentum
+int nb_muon_apply(void *const *master, void *const *weight, const void *const *update, int64_t n, int64_t count, float decay,
+                  float step, void *stream_)
+{
+    if (n < 0 || count < 0) return fail(NB_ERR_INVALID_ARG, "negative size");
+    if (n > NB_MUON_MAX_N || count >= (1ll << 40)) return fail(NB_ERR_UNSUPPORTED, "too many matrices or elements");
+    if (n > 0 && (!master || !update)) return fail(NB_ERR_INVALID_ARG, "master and update must not be NULL");
+    for (int64_t i = 0; i < n; ++i) {
+        if (!master[i] || !update[i] || (weight && !weight[i])) return fail(NB_ERR_INVALID_ARG, "matrix %d has a NULL pointer", static_cast<int>(i));
+        if (!aligned16(master[i]) || !aligned16(update[i]) || (weight && !aligned16(weight[i])))
+            return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+    }
+    if (n == 0 || count == 0) return NB_OK;
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    int rc = get_state(&s);
+    if (rc != NB_OK) return rc;
+    for (int64_t at = 0; at < n; at += kMuonBatch) {
+        const int now = static_cast<int>(n - at < kMuonBatch ? n - at : kMuonBatch);
+        MuonApply p{};
+        for (int i = 0; i < now; ++i) {
+            p.master[i] = static_cast<float *>(master[at + i]);
+            p.weight[i] = weight ? weight[at + i] : nullptr;
+            p.update[i] = update[at + i];
+        }
+        p.count = count;
+        p.decay = decay;
+        p.step = step;
+        // two vectors of eight per thread, up to sixteen blocks per SM over all matrices
+        long long blocks = (count / 8 + 511) / 512, most = (16ll * s->num_sms + now - 1) / now;
+        blocks = blocks < 1 ? 1 : blocks < most ? blocks : most;
+        rc = launch_chained(muon_apply_kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(now)), 256,
+                            static_cast<cudaStream_t>(stream_), p);
+        if (rc != NB_OK) return rc;
+        ++g_launches;
+    }
     return NB_OK;
 }
 

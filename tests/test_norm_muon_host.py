@@ -1,0 +1,106 @@
+"""Layer norm and the orthogonalised update, without a GPU: refusals, workspace sizes, and the references that the GPU tests use."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2609_28568_b200 import binding as nb
+from paper_2609_28568_b200 import build
+from norm_reference import norm_backward, norm_forward
+
+P = 0x10000  # a fake aligned device address: a refused call never touches it
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build()
+    return nb.lib()
+
+
+def test_norm_forward_refusals(L):
+    def call(out=P, total=P, mean=P, rstd=P, inp=P, branch=P, w=P, b=P, BT=4, C=64, eps=1e-5, dtype=nb.DTYPE_BF16):
+        return L.nb_layernorm_forward(out, total, mean, rstd, inp, branch, w, b, BT, C, eps, dtype, None)
+    bad = nb.NB_ERR_INVALID_ARG
+    for kw in (dict(out=None), dict(inp=None), dict(w=None), dict(total=None), dict(branch=None), dict(mean=None), dict(rstd=None),
+               dict(BT=-1), dict(C=0), dict(eps=-1e-5), dict(eps=float("nan")), dict(eps=float("inf")), dict(dtype=2), dict(out=P + 8), dict(total=P + 2),
+               dict(inp=P + 4), dict(branch=P + 2), dict(w=P + 2), dict(b=P + 2), dict(mean=P + 2), dict(rstd=P + 1)):
+        assert call(**kw) == bad, kw
+        assert nb.nb_last_error()
+    for kw in (dict(C=12), dict(C=8200), dict(BT=1 << 31), dict(BT=(1 << 31) - 1, C=8192)):
+        assert call(**kw) == nb.NB_ERR_UNSUPPORTED, kw
+    assert call(BT=0) == nb.NB_OK
+
+
+def test_norm_backward_refusals(L):
+    need = nb.nb_layernorm_workspace(4, 64)
+
+    def call(dinp=P, dbranch=P, dw=P, db=P, dout=P, dres=P, inp=P, mean=P, rstd=P, w=P, BT=4, C=64, acc=0, dtype=nb.DTYPE_F32, ws=P,
+             size=need):
+        return L.nb_layernorm_backward(dinp, dbranch, dw, db, dout, dres, inp, mean, rstd, w, BT, C, acc, dtype, ws, size, None)
+    for kw in (dict(dinp=None), dict(dout=None), dict(inp=None), dict(mean=None), dict(rstd=None), dict(w=None), dict(ws=None),
+               dict(size=need - 1), dict(size=0), dict(dw=None, size=0), dict(BT=-4), dict(C=-8), dict(dtype=7), dict(dinp=P + 4), dict(dbranch=P + 2), dict(dw=P + 4),
+               dict(db=P + 8), dict(dout=P + 2), dict(dres=P + 4), dict(inp=P + 8), dict(w=P + 2), dict(ws=P + 8), dict(mean=P + 3),
+               dict(rstd=P + 2)):
+        assert call(**kw) == nb.NB_ERR_INVALID_ARG, kw
+    for kw in (dict(C=20), dict(C=8200)):
+        assert call(**kw) == nb.NB_ERR_UNSUPPORTED, kw
+    assert call(BT=0, acc=1) == nb.NB_OK
+
+
+def test_norm_workspace(L):
+    assert L.nb_layernorm_workspace(-1, 64) == -1 and L.nb_layernorm_workspace(4, 12) == -1 and L.nb_layernorm_workspace(4, 8200) == -1
+    with pytest.raises(nb.NbError):
+        nb.nb_layernorm_workspace(4, 12)
+    assert nb.nb_layernorm_workspace(0, 64) == 0
+    for C in (8, 64, 768, 1024, 1032, 2048, 4096, 8192):
+        sizes = [nb.nb_layernorm_workspace(rows, C) for rows in (1, 8, 9, 100, 4096, 1 << 30)]
+        assert all(s > 0 and s % (8 * C) == 0 for s in sizes) and sizes == sorted(sizes)
+        assert sizes[0] == 8 * C  # one block's sums
+
+
+def _array(*addresses):
+    return (ctypes.c_void_p * len(addresses))(*addresses)
+
+
+def test_apply_refusals(L):
+    def call(m=_array(P, P + 64), w=_array(P, P + 32), u=_array(P, P + 32), n=2, count=10):
+        return L.nb_muon_apply(m, w, u, n, count, 0.9, 0.1, None)
+    for kw in (dict(m=None), dict(u=None), dict(n=-1), dict(count=-1), dict(m=_array(P, None)), dict(u=_array(None, P)),
+               dict(w=_array(P, None)), dict(m=_array(P, P + 4)), dict(u=_array(P + 2, P)), dict(w=_array(P, P + 8))):
+        assert call(**kw) == nb.NB_ERR_INVALID_ARG, kw
+    assert call(n=1025) == nb.NB_ERR_UNSUPPORTED
+    assert call(count=1 << 40) == nb.NB_ERR_UNSUPPORTED
+    assert call(n=0) == nb.NB_OK and call(count=0) == nb.NB_OK
+    assert L.nb_muon_apply(None, None, None, 0, 10, 0.9, 0.1, None) == nb.NB_OK
+
+
+def test_binding_refusals(L):
+    with pytest.raises(ValueError, match="master"):
+        nb.nb_muon_apply([P], None, [P, P], 2, 0, 0.9, 0.1, 0)
+    with pytest.raises(TypeError):
+        nb.nb_muon_apply(P, None, [P], 1, 0, 0.9, 0.1, 0)
+    with pytest.raises(nb.NbError):
+        nb.nb_muon_apply([P], None, [None], 1, 8, 0.9, 0.1, 0)
+    with pytest.raises(AssertionError):  # a CPU tensor
+        nb.nb_muon_apply([torch.zeros(8)], None, [P], 1, 0, 0.9, 0.1, 0)
+    with pytest.raises(TypeError):
+        nb._stream_dtype(torch.zeros(1, dtype=torch.float16))
+    nb.nb_muon_apply([P], None, (P,), 1, 0, 0.9, 0.1, 0)  # nothing to do
+    nb.nb_muon_apply([], [], [], 0, 8, 0.9, 0.1, 0)
+
+
+def test_reference_gradients_against_differences():
+    g = torch.Generator().manual_seed(3)
+    s, w, b, r = (torch.randn(shape, generator=g, dtype=torch.float64) for shape in ((3, 16), (16,), (16,), (3, 16)))
+    f = lambda s_, w_, b_: (norm_forward(s_, w_, b_, 1e-5)["out"] * r).sum()  # noqa: E731
+    fw = norm_forward(s, w, b, 1e-5)
+    got = norm_backward(r, s, fw["mean"], fw["rstd"], w, None)
+    h = 1e-6
+    for name, at, grad in (("s", s, got["dinp"]), ("w", w, got["dweight"]), ("b", b, got["dbias"])):
+        for i in range(at.numel()):
+            d = torch.zeros_like(at)
+            d.view(-1)[i] = h
+            args = [(x + d if x is at else x, x - d if x is at else x) for x in (s, w, b)]
+            diff = (f(*(a[0] for a in args)) - f(*(a[1] for a in args))) / (2 * h)
+            # central differences: third derivatives times h^2, and 64-bit cancellation over h
+            assert abs(diff - grad.view(-1)[i]) < 1e-8 * max(1.0, grad.abs().max().item()), (name, i)
