@@ -321,6 +321,34 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
                           void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
+ * Update of two-dimensional weights by orthogonalised momentum (no counterpart in the paper, whose optimizer is AdamW: for the same
+ * gradients, those that nb_linear_backward leaves), for n matrices [R, C] of one shape:
+ *     m <- mu * m + g                                                   (momentum NULL: m = g, and nothing is stored)
+ *     v  = g + mu * m if nesterov, else m;   x = v / (|v| + eps)        (Frobenius norm)
+ *     steps times:  y = x x^T,  x <- a x + (b y + c y y) x              (R > C: from the other side, the same result)
+ *     update = bf16(x)
+ * The iteration brings x's singular values towards one, which a = 3.4445, b = -4.7750, c = 2.0315 with five steps does for all
+ * from about 1e-3 up. steps == 0 gives the normalised v.
+ *   update   [out] n bf16 matrices;  momentum [i/o] n fp32 matrices or NULL;  grad [in] n matrices of grad_dtype (NB_DTYPE_*)
+ *   workspace     device memory of nb_muon_workspace(n, R, C) bytes, 128-byte aligned, the caller's: calls that may run at the same time (on
+ *                 two streams, in two graphs) take one each. Matrices are worked off 32 at a time; the size grows no further from there.
+ * update, momentum and grad are host arrays of n device pointers, each 16-byte aligned and dense; the arrays are read before the call returns.
+ * No tensor may be given twice. R and C are multiples of 8 and at most NB_MUON_MAX_DIM, n at most NB_MUON_MAX_N, steps at most 32.
+ * m, v and the norm are held in fp32 and more; x, y and the polynomial between the products in fp16 at fixed powers of two, products
+ * are accumulated in fp32. Rounding errors grow as small singular values do (485 times in five steps): against 64 bits the update is 1.2e-3 off
+ * before its own rounding to bf16 for gradients of full rank (as of training: a few strong directions over noise), 2e-2 where singular values fall off
+ * as 1/j^2. Coefficients that would carry singular values from [0, 1] out of the intermediates' range return NB_ERR_UNSUPPORTED.
+ * An infinity or a NaN in a matrix makes its update NaN and touches no other matrix. A zero matrix gives a zero update.
+ * nb_muon_workspace returns -1 for sizes that the call would refuse.
+ */
+#define NB_MUON_MAX_N 1024
+#define NB_MUON_MAX_DIM 32768
+int64_t nb_muon_workspace(int64_t n, int64_t R, int64_t C);
+int nb_muon_update(void *const *update, void *const *momentum, const void *const *grad, int64_t n,
+                   int64_t R, int64_t C, float mu, int nesterov, int steps, float a, float b, float c,
+                   float eps, int grad_dtype, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * Application of an update to the master weights, with the compute copies of the next step (takes the place of
  * nb_cast_f32_to_bf16 in a step), for n tensors of `count` elements each:
  *     master <- decay * master - step * update;  weight <- bf16(master)
@@ -328,7 +356,6 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
  * The three are host arrays of n device pointers, each 16-byte aligned; the arrays are read before the call returns. With learning rate lr
  * and weight decay wd, decay = 1 - lr * wd and step = lr times the update's scale. n at most NB_MUON_MAX_N. No tensor may be given twice.
  */
-#define NB_MUON_MAX_N 1024
 int nb_muon_apply(void *const *master, void *const *weight, const void *const *update, int64_t n,
                   int64_t count, float decay, float step, void *stream);
 

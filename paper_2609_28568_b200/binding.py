@@ -30,7 +30,7 @@ EXPORTS = (
     "nb_lora_linear_forward", "nb_lora_linear_backward", "nb_debug_layer_bwd_plan", "nb_debug_gemm_timeout",
     "nb_lora_down_stacked", "nb_lora_linear_forward_stacked", "nb_lora_linear_backward_stacked",
     "nb_lora_da_stacked", "nb_debug_route", "nb_layernorm_forward", "nb_layernorm_workspace", "nb_layernorm_backward",
-    "nb_muon_apply",
+    "nb_muon_workspace", "nb_muon_update", "nb_muon_apply",
 )
 
 CALL_FORWARD, CALL_BACKWARD, CALL_LORA_FORWARD, CALL_LORA_BACKWARD = range(4)
@@ -83,6 +83,10 @@ def lib() -> ctypes.CDLL:
         L.nb_layernorm_workspace.argtypes = [_i64] * 2
         L.nb_layernorm_workspace.restype = _i64
         L.nb_layernorm_backward.argtypes = [_vp] * 10 + [_i64] * 2 + [_int] * 2 + [_vp, _i64, _vp]
+        L.nb_muon_workspace.argtypes = [_i64] * 3
+        L.nb_muon_workspace.restype = _i64
+        L.nb_muon_update.argtypes = ([ctypes.POINTER(_vp)] * 3 + [_i64] * 3 + [ctypes.c_float, _int, _int] + [ctypes.c_float] * 4 +
+                                     [_int, _vp, _i64, _vp])
         L.nb_muon_apply.argtypes = [ctypes.POINTER(_vp)] * 3 + [_i64] * 2 + [ctypes.c_float] * 2 + [_vp]
         L.nb_debug_split_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int)]
         L.nb_debug_gemm_timeout.argtypes = [_vp, _vp, _vp, _i64]
@@ -280,6 +284,18 @@ def nb_layernorm_backward(dinp, dbranch, dweight, dbias, dout, dres, inp, mean, 
                                                       accumulate, stream_dtype, workspace, workspace_bytes, stream)
 
 
+def nb_muon_workspace(n: int, R: int, C: int) -> int:
+    """Bytes of workspace that nb_muon_update needs for n matrices [R, C]."""
+    return _size(lib().nb_muon_workspace(n, R, C), f"{n} matrices [{R}, {C}]")
+
+
+def nb_muon_update(update, momentum, grad, n, R, C, mu, nesterov, steps, a, b, c, eps, grad_dtype, workspace, workspace_bytes,
+                   stream=None) -> None:
+    """m <- mu m + g, v = g + mu m or m, update = bf16 of v orthogonalised in `steps` steps, for n matrices [R, C] given as sequences."""
+    (_native or _load_native()).nb_muon_update(update, momentum, grad, n, R, C, mu, nesterov, steps, a, b, c, eps, grad_dtype,
+                                               workspace, workspace_bytes, stream)
+
+
 def nb_muon_apply(master, weight, update, n, count, decay, step, stream=None) -> None:
     """master <- decay * master - step * update, weight <- bf16(master), for n tensors of count elements given as sequences."""
     (_native or _load_native()).nb_muon_apply(master, weight, update, n, count, decay, step, stream)
@@ -354,7 +370,7 @@ def linear_backward(dout, inp, weight, pre_act=None, inp_pre_act=None, act=ACT_N
 
 def _stream_dtype(t) -> int:
     if t.dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError(f"the residual stream is bf16 or fp32, not {t.dtype}")
+        raise TypeError(f"a tensor of bf16 or fp32 is wanted, not {t.dtype}")
     return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
 
 
@@ -386,3 +402,23 @@ def layernorm_backward(dout, inp, mean, rstd, weight, dres=None, dweight=None, d
                           dbias if need_dbias else None, dout, dres, inp, mean, rstd, weight, BT, C, int(accumulate), dtype,
                           ws, ws.numel())
     return dinp, dbranch, dweight, dbias
+
+
+MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def muon_update(grad, momentum=None, mu=0.95, nesterov=True, steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7):
+    """Allocate the updates and the workspace and call nb_muon_update. grad is a list of matrices of one shape and type (fp32 or bf16),
+    momentum their fp32 momenta (changed in place) or None. Returns the list of updates (bf16)."""
+    if not grad:
+        return []
+    R, C = grad[0].shape
+    if any(g.shape != (R, C) or g.dtype != grad[0].dtype for g in grad):
+        raise ValueError("the matrices of a call have one shape and one type")
+    if momentum is not None and any(m.shape != (R, C) or m.dtype != torch.float32 for m in momentum):
+        raise ValueError("momenta are fp32, of the gradients' shape")
+    update = [torch.empty((R, C), dtype=torch.bfloat16, device=g.device) for g in grad]
+    ws = torch.empty(nb_muon_workspace(len(grad), R, C), dtype=torch.uint8, device=grad[0].device)
+    nb_muon_update(update, momentum, grad, len(grad), R, C, mu, int(nesterov), steps, *coefficients, eps, _stream_dtype(grad[0]), ws,
+                   ws.numel())
+    return update

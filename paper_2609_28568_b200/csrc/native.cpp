@@ -267,6 +267,33 @@ bool to_stream_or_current(PyObject *const *args, Py_ssize_t n, Py_ssize_t at, vo
     return to_stream(args[at], stream);
 }
 
+// nb_muon_update(update, momentum or None, grad, n, R, C, mu, nesterov, steps, a, b, c, eps, grad_dtype, workspace, workspace_bytes,
+//                stream)
+PyObject *muon_update(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    Pointers update, momentum, grad;
+    int64_t n = 0, R = 0, C = 0, bytes = 0;
+    float mu = 0, a = 0, b = 0, c = 0, eps = 0;
+    int nesterov = 0, steps = 0, dtype = 0;
+    void *ws = nullptr, *stream = nullptr;
+    if (nargs != 16 && nargs != 17) return PyErr_Format(PyExc_TypeError, "16 or 17 arguments are wanted, not %zd", nargs);
+    if (!convert(args[3], n) || !convert(args[4], R) || !convert(args[5], C) || !convert(args[6], mu) || !convert(args[7], nesterov) ||
+        !convert(args[8], steps) || !convert(args[9], a) || !convert(args[10], b) || !convert(args[11], c) || !convert(args[12], eps) ||
+        !convert(args[13], dtype) || !to_pointer(args[14], ws) || !on_current_device(args[14]) || !convert(args[15], bytes) ||
+        !to_pointers(args[0], update, n, "update") || !to_pointers(args[1], momentum, n, "momentum") ||
+        !to_pointers(args[2], grad, n, "grad") || !to_stream_or_current(args, nargs, 16, stream))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nb_muon_update(update.data(), momentum.data(), grad.data(), n, R, C, mu, nesterov, steps, a, b, c, eps, dtype, ws, bytes,
+                        stream);
+    Py_END_ALLOW_THREADS
+    if (rc != NB_OK) return raise(rc);
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 // nb_muon_apply(master, weight or None, update, n, count, decay, step, stream)
 PyObject *muon_apply(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
@@ -318,6 +345,7 @@ PyMethodDef g_methods[] = {
     NB_ENTRY(nb_cast_f32_to_bf16),
     NB_ENTRY_CHECKED(nb_layernorm_forward),
     NB_ENTRY_CHECKED(nb_layernorm_backward),
+    {"nb_muon_update", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&muon_update)), METH_FASTCALL, nullptr},
     {"nb_muon_apply", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&muon_apply)), METH_FASTCALL, nullptr},
     NB_FAST(linear_forward),
     NB_FAST(linear_backward),

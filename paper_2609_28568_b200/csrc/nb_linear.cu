@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -20,6 +21,7 @@
 #include "layer_bwd_sm100.cuh"
 #include "lora_udb_sm100.cuh"
 #include "muon.cuh"
+#include "newton_schulz_sm100.cuh"
 #include "norm.cuh"
 #include "rows_sm100.cuh"
 #include "tile_sm100.cuh"
@@ -62,10 +64,11 @@ struct TmapKey {
     const void *ptr;
     uint64_t rows, cols, ld;
     uint32_t box_cols, box_rows, dtype;
+    uint64_t depth;  // matrices of a batch (3-D map); 0: a 2-D map
     bool operator==(const TmapKey &o) const
     {
         return ptr == o.ptr && rows == o.rows && cols == o.cols && ld == o.ld && box_cols == o.box_cols &&
-               box_rows == o.box_rows && dtype == o.dtype;
+               box_rows == o.box_rows && dtype == o.dtype && depth == o.depth;
     }
 };
 struct TmapKeyHash {
@@ -76,7 +79,7 @@ struct TmapKeyHash {
         h ^= (k.cols + 0x165667B1ull) * 0x94D049BB133111EBull;
         h ^= (k.ld + 0x2545F491ull) * 0xD6E8FEB86659FD93ull;
         h ^= (static_cast<uint64_t>(k.box_cols) << 40) ^ (static_cast<uint64_t>(k.box_rows) << 20) ^
-             k.dtype;
+             k.dtype ^ (k.depth << 8);
         return static_cast<size_t>(h ^ (h >> 29));
     }
 };
@@ -162,7 +165,7 @@ int get_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t rows, u
     if (ld < cols || (ld * esz) % 16 != 0)
         return fail(NB_ERR_UNSUPPORTED, "row stride of %llu elements is not a multiple of 16 bytes",
                     static_cast<unsigned long long>(ld));
-    TmapKey key{ptr, rows, cols, ld, box_cols, box_rows, dtype};
+    TmapKey key{ptr, rows, cols, ld, box_cols, box_rows, dtype, 0};
     auto it = s.tmaps.find(key);
     if (it != s.tmaps.end()) {
         *out = it->second;
@@ -183,6 +186,36 @@ int get_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t rows, u
     if (r != CUDA_SUCCESS)
         return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) for [%llu, %llu] at %p",
                     static_cast<int>(r), static_cast<unsigned long long>(rows),
+                    static_cast<unsigned long long>(cols), ptr);
+    if (s.tmaps.size() > 8192) s.tmaps.clear();
+    s.tmaps.emplace(key, m);
+    *out = m;
+    return NB_OK;
+}
+
+// n dense fp16 matrices [rows, cols] one after the other, as boxes of box_rows x box_cols of one of them. Boxes of 64 columns
+// have the 128-byte swizzle, others none. What lies outside a matrix reads as zero and is not written.
+int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n, uint64_t rows, uint64_t cols, uint32_t box_cols,
+                   uint32_t box_rows)
+{
+    TmapKey key{ptr, rows, cols, cols, box_cols, box_rows, 2, n};
+    auto it = s.tmaps.find(key);
+    if (it != s.tmaps.end()) {
+        *out = it->second;
+        return NB_OK;
+    }
+    cuuint64_t dims[3] = {cols, rows, n};
+    cuuint64_t strides[2] = {cols * 2, rows * cols * 2};
+    cuuint32_t box[3] = {box_cols, box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    alignas(64) CUtensorMap m;
+    memset(&m, 0, sizeof(m));
+    CUresult r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) for %llu x [%llu, %llu] at %p", static_cast<int>(r),
+                    static_cast<unsigned long long>(n), static_cast<unsigned long long>(rows),
                     static_cast<unsigned long long>(cols), ptr);
     if (s.tmaps.size() > 8192) s.tmaps.clear();
     s.tmaps.emplace(key, m);
@@ -1807,6 +1840,211 @@ int with_norm_form(const NormForm &f, F &&fn)
     return fn(IntC<512>{}, IntC<2>{});
 }
 
+// ----------------------------------------------------------------------------- orthogonalised momentum
+// The workspace of a group of at most kMuonBatch matrices: two of the iterate, S, P (all fp16), and the norms' partial sums.
+struct MuonSpace {
+    int64_t x[2], s, p, part, bytes;
+};
+int muon_parts(int64_t nvec)  // blocks that read a matrix: about four vectors of eight per thread, 256 at most
+{
+    const int64_t b = (nvec + 1023) / 1024;
+    return static_cast<int>(b < 256 ? b : 256);
+}
+MuonSpace muon_space(int64_t n, int64_t R, int64_t C)
+{
+    if (n > kMuonBatch) n = kMuonBatch;
+    const int64_t m = R < C ? R : C;
+    auto up = [](int64_t b) { return (b + 1023) & ~int64_t{1023}; };
+    MuonSpace w;
+    w.x[0] = 0;
+    w.x[1] = up(n * R * C * 2);
+    w.s = w.x[1] + up(n * R * C * 2);
+    w.p = w.s + up(n * m * m * 2);
+    w.part = w.p + up(n * m * m * 2);
+    w.bytes = w.part + up(n * muon_parts(R * C / 8) * 8);
+    return w;
+}
+
+struct NsArgs {
+    const CUtensorMap *A, *B, *D, *T;  // T: D's transposed boxes, or D
+    int M, N, K, n;
+    float alpha, beta, diag;
+    const __half *aux;
+    void *const *out;
+};
+
+template <class Cfg>
+int launch_ns(DeviceState &s, const NsArgs &a, cudaStream_t stream)
+{
+    static int max_clusters[kMaxDevices] = {};
+    int dev = 0;
+    NB_CUDA(cudaGetDevice(&dev));
+    if (max_clusters[dev] == 0) {
+        NB_CUDA(cudaFuncSetAttribute(newton_schulz_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(Cfg::SMEM_BYTES)));
+        int fit = s.num_sms / Cfg::CG;
+        if (Cfg::CG == 2) {
+            cudaLaunchConfig_t qc = {};
+            qc.gridDim = dim3(static_cast<unsigned>(s.num_sms));
+            qc.blockDim = dim3(kNumThreads);
+            qc.dynamicSmemBytes = Cfg::SMEM_BYTES;
+            cudaLaunchAttribute qa[1];
+            qa[0].id = cudaLaunchAttributeClusterDimension;
+            qa[0].val.clusterDim.x = 2;
+            qa[0].val.clusterDim.y = 1;
+            qa[0].val.clusterDim.z = 1;
+            qc.attrs = qa;
+            qc.numAttrs = 1;
+            int n = 0;
+            NB_CUDA(cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel<Cfg>, &qc));
+            if (n < 1) return fail(NB_ERR_CUDA, "no CTA pair of this kernel fits on the device");
+            if (n < fit) fit = n;
+        }
+        max_clusters[dev] = fit;
+    }
+    NsParams p{};
+    p.M = a.M;
+    p.N = a.N;
+    p.tiles_m = (a.M + Cfg::TILE_M - 1) / Cfg::TILE_M;
+    p.tiles_n = (a.N + Cfg::BLOCK_N - 1) / Cfg::BLOCK_N;
+    p.tiles = Cfg::SYM ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+    p.units = p.tiles * a.n;
+    p.kblocks = kblocks_of(a.K);
+    p.alpha = a.alpha;
+    p.beta = a.beta;
+    p.diag = a.diag;
+    p.aux = a.aux;
+    p.status = s.status;
+    p.timeout_ns = kDefaultTimeoutNs;
+    for (int i = 0; a.out && i < a.n; ++i) p.out[i] = a.out[i];
+    const int clusters = p.units < max_clusters[dev] ? p.units : max_clusters[dev];
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(clusters * Cfg::CG));
+    cfg.blockDim = dim3(kNumThreads);
+    cfg.dynamicSmemBytes = Cfg::SMEM_BYTES;
+    cfg.stream = stream;
+    cudaLaunchAttribute attrs[2];
+    attrs[0].id = cudaLaunchAttributeClusterDimension;
+    attrs[0].val.clusterDim.x = Cfg::CG;
+    attrs[0].val.clusterDim.y = 1;
+    attrs[0].val.clusterDim.z = 1;
+    attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = dependent_launch_allowed(stream) ? 2 : 1;
+    NB_CUDA(cudaLaunchKernelEx(&cfg, newton_schulz_kernel<Cfg>, *a.A, *a.B, *a.D, *a.T, p));
+    ++g_launches;
+    return NB_OK;
+}
+
+template <bool A_MN, bool B_MN, int EPI>
+int launch_ns_auto(DeviceState &s, const NsArgs &a, cudaStream_t stream)
+{
+    // pairs of CTAs on 256 x 256 tiles where these fill most of the SMs, else a CTA on 128 x 128
+    const int tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
+    const int units = a.n * (EPI == kNsGram || EPI == kNsPoly ? tm * (tm + 1) / 2 : tm * tn);
+    if (2 * units > s.num_sms / 2) return launch_ns<NsCfg<2, 256, A_MN, B_MN, EPI>>(s, a, stream);
+    return launch_ns<NsCfg<1, 128, A_MN, B_MN, EPI>>(s, a, stream);
+}
+
+struct MuonCall {
+    void *const *update, *const *momentum;
+    const void *const *grad;
+    int64_t R, C;
+    float mu;
+    int nesterov, steps;
+    float a, b, c, eps;
+    bool grad_f32;
+    unsigned char *workspace;
+};
+
+// A group of n <= kMuonBatch matrices, from the at-th on.
+int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t stream)
+{
+    const MuonSpace w = muon_space(n, q.R, q.C);
+    const int R = static_cast<int>(q.R), C = static_cast<int>(q.C);
+    const bool tall = R > C;
+    const int m = tall ? C : R, k = tall ? R : C;
+    MuonPrepare pr{};
+    for (int i = 0; i < n; ++i) {
+        pr.grad[i] = q.grad[at + i];
+        pr.momentum[i] = q.momentum ? static_cast<float *>(q.momentum[at + i]) : nullptr;
+        pr.out[i] = q.update[at + i];
+    }
+    pr.part = reinterpret_cast<double *>(q.workspace + w.part);
+    pr.x = reinterpret_cast<__half *>(q.workspace + w.x[0]);
+    pr.nvec = q.R * q.C / 8;
+    pr.parts = muon_parts(pr.nvec);
+    pr.nesterov = q.nesterov;
+    pr.mu = q.mu;
+    pr.scale = kNsScaleX;
+    pr.eps = q.eps;
+    const dim3 grid(static_cast<unsigned>(pr.parts), static_cast<unsigned>(n));
+    int rc = q.grad_f32 ? launch_chained(muon_momentum_kernel<true>, grid, 256, stream, pr)
+                        : launch_chained(muon_momentum_kernel<false>, grid, 256, stream, pr);
+    if (rc != NB_OK) return rc;
+    if (q.steps == 0)
+        rc = q.grad_f32 ? launch_chained(muon_normalise_kernel<true, true>, grid, 256, stream, pr)
+                        : launch_chained(muon_normalise_kernel<false, true>, grid, 256, stream, pr);
+    else
+        rc = q.grad_f32 ? launch_chained(muon_normalise_kernel<true, false>, grid, 256, stream, pr)
+                        : launch_chained(muon_normalise_kernel<false, false>, grid, 256, stream, pr);
+    if (rc != NB_OK) return rc;
+    g_launches += 2;
+    if (q.steps == 0) return NB_OK;
+
+    CUtensorMap xl[2], xs[2], sl, ss, st, pl, ps, pt;  // loads, stores, transposed stores
+    for (int i = 0; i < 2; ++i) {
+        if ((rc = get_batch_tmap(s, &xl[i], q.workspace + w.x[i], n, R, C, 64, 64)) != NB_OK) return rc;
+        if ((rc = get_batch_tmap(s, &xs[i], q.workspace + w.x[i], n, R, C, 64, 32)) != NB_OK) return rc;
+    }
+    if ((rc = get_batch_tmap(s, &sl, q.workspace + w.s, n, m, m, 64, 64)) != NB_OK) return rc;
+    if ((rc = get_batch_tmap(s, &ss, q.workspace + w.s, n, m, m, 64, 32)) != NB_OK) return rc;
+    if ((rc = get_batch_tmap(s, &st, q.workspace + w.s, n, m, m, 32, 64)) != NB_OK) return rc;
+    if ((rc = get_batch_tmap(s, &pl, q.workspace + w.p, n, m, m, 64, 64)) != NB_OK) return rc;
+    if ((rc = get_batch_tmap(s, &ps, q.workspace + w.p, n, m, m, 64, 32)) != NB_OK) return rc;
+    if ((rc = get_batch_tmap(s, &pt, q.workspace + w.p, n, m, m, 32, 64)) != NB_OK) return rc;
+    for (int i = 0; i < q.steps; ++i) {
+        const CUtensorMap *x = &xl[i & 1];
+        const bool last = i == q.steps - 1;
+        NsArgs g{x, x, &ss, &st, m, m, k, n, kNsScaleS / (kNsScaleX * kNsScaleX), 0.0f, 0.0f, nullptr, nullptr};
+        rc = tall ? launch_ns_auto<true, true, kNsGram>(s, g, stream) : launch_ns_auto<false, false, kNsGram>(s, g, stream);
+        if (rc != NB_OK) return rc;
+        NsArgs y{&sl, &sl, &ps, &pt, m, m, m, n, q.c / kNsScaleS, q.b, q.a * kNsScaleS,
+                 reinterpret_cast<const __half *>(q.workspace + w.s), nullptr};
+        if ((rc = launch_ns_auto<false, false, kNsPoly>(s, y, stream)) != NB_OK) return rc;
+        // P X from P's rows and X's columns, or X P from X's rows and P's rows (which are its columns)
+        NsArgs u{tall ? x : &pl, tall ? &pl : x, &xs[(i + 1) & 1], &xs[(i + 1) & 1], R, C, m, n,
+                 last ? 1.0f / (kNsScaleS * kNsScaleX) : 1.0f / kNsScaleS, 0.0f, 0.0f, nullptr, last ? q.update + at : nullptr};
+        if (last)
+            rc = tall ? launch_ns_auto<false, false, kNsLast>(s, u, stream) : launch_ns_auto<false, true, kNsLast>(s, u, stream);
+        else
+            rc = tall ? launch_ns_auto<false, false, kNsStep>(s, u, stream) : launch_ns_auto<false, true, kNsStep>(s, u, stream);
+        if (rc != NB_OK) return rc;
+    }
+    return NB_OK;
+}
+
+// Whether the polynomial keeps everything within what fp16 holds at its scale: singular values start in [0, 1] and step to
+// |x (a + b x^2 + c x^4)|; X holds up to 16, S and P up to 64, and half of that is allowed.
+bool muon_in_range(int steps, double a, double b, double c)
+{
+    double top = 1.001;  // the first rounding may exceed one a little
+    for (int i = 0; i < steps; ++i) {
+        if (top * top > 32.0 || !(top <= 8.0)) return false;
+        double next = 0.0, most = 0.0;
+        for (int j = 0; j <= 1000; ++j) {
+            const double x = top * j / 1000.0, s = x * x, p = a + b * s + c * s * s;
+            if (!(std::fabs(p) <= 32.0)) return false;
+            next = std::fmax(next, std::fabs(x * p));
+            most = std::fmax(most, std::fabs(b) * s);
+        }
+        if (most > 32.0) return false;
+        top = next * 1.01;
+    }
+    return true;  // the last result is bf16
+}
+
 int check_norm(int64_t BT, int64_t C, int stream_dtype)
 {
     if (BT < 0 || C <= 0) return fail(NB_ERR_INVALID_ARG, "negative or zero dimension");
@@ -2403,6 +2641,50 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
 }
 
 // ----------------------------------------------------------------------------- orthogonalised momentum
+int64_t nb_muon_workspace(int64_t n, int64_t R, int64_t C)
+{
+    if (n < 0 || n > NB_MUON_MAX_N || R <= 0 || C <= 0 || R % 8 != 0 || C % 8 != 0 || R > NB_MUON_MAX_DIM || C > NB_MUON_MAX_DIM)
+        return -1;
+    return n == 0 ? 0 : muon_space(n, R, C).bytes;
+}
+
+int nb_muon_update(void *const *update, void *const *momentum, const void *const *grad, int64_t n, int64_t R, int64_t C, float mu,
+                   int nesterov, int steps, float a, float b, float c, float eps, int grad_dtype, void *workspace,
+                   int64_t workspace_bytes, void *stream_)
+{
+    if (n < 0 || R <= 0 || C <= 0) return fail(NB_ERR_INVALID_ARG, "negative or zero dimension");
+    if (grad_dtype != NB_DTYPE_F32 && grad_dtype != NB_DTYPE_BF16) return fail(NB_ERR_INVALID_ARG, "unknown grad_dtype %d", grad_dtype);
+    if (R % 8 != 0 || C % 8 != 0) return fail(NB_ERR_UNSUPPORTED, "R (%lld) and C (%lld) must be multiples of 8",
+                                              static_cast<long long>(R), static_cast<long long>(C));
+    if (n > NB_MUON_MAX_N || R > NB_MUON_MAX_DIM || C > NB_MUON_MAX_DIM) return fail(NB_ERR_UNSUPPORTED, "too many matrices or too large ones");
+    if (steps < 0 || steps > 32) return fail(NB_ERR_INVALID_ARG, "steps must be within [0, 32]");
+    if (!(eps >= 0.0f) || eps > 3.0e38f || !std::isfinite(mu)) return fail(NB_ERR_INVALID_ARG, "eps must be finite and not negative, mu finite");
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return fail(NB_ERR_INVALID_ARG, "a, b and c must be finite");
+    if (!muon_in_range(steps, a, b, c))
+        return fail(NB_ERR_UNSUPPORTED, "with a = %g, b = %g, c = %g singular values of at most one leave the range of the intermediates",
+                    static_cast<double>(a), static_cast<double>(b), static_cast<double>(c));
+    if (n == 0) return NB_OK;
+    if (!update || !grad) return fail(NB_ERR_INVALID_ARG, "update and grad must not be NULL");
+    for (int64_t i = 0; i < n; ++i) {
+        if (!update[i] || !grad[i] || (momentum && !momentum[i])) return fail(NB_ERR_INVALID_ARG, "matrix %d has a NULL pointer", static_cast<int>(i));
+        if (!aligned16(update[i]) || !aligned16(grad[i]) || (momentum && !aligned16(momentum[i])))
+            return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+    }
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 127u) || workspace_bytes < muon_space(n, R, C).bytes)
+        return fail(NB_ERR_INVALID_ARG, "a 128-byte aligned workspace of %lld bytes is needed (nb_muon_workspace)",
+                    static_cast<long long>(muon_space(n, R, C).bytes));
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    int rc = get_state(&s);
+    if (rc != NB_OK) return rc;
+    const MuonCall q{update, momentum, grad, R, C, mu, nesterov, steps, a, b, c, eps, grad_dtype == NB_DTYPE_F32,
+                     static_cast<unsigned char *>(workspace)};
+    for (int64_t at = 0; at < n; at += kMuonBatch)
+        if ((rc = run_muon(*s, q, at, static_cast<int>(n - at < kMuonBatch ? n - at : kMuonBatch), static_cast<cudaStream_t>(stream_))) != NB_OK)
+            return rc;
+    return NB_OK;
+}
+
 int nb_muon_apply(void *const *master, void *const *weight, const void *const *update, int64_t n, int64_t count, float decay,
                   float step, void *stream_)
 {

@@ -62,6 +62,49 @@ def _array(*addresses):
     return (ctypes.c_void_p * len(addresses))(*addresses)
 
 
+def test_update_refusals(L):
+    need = nb.nb_muon_workspace(2, 64, 128)
+
+    def call(u=_array(P, P + 64), m=_array(P, P + 64), g=_array(P, P + 64), n=2, R=64, C=128, mu=0.95, nesterov=1, steps=5,
+             co=nb.MUON_COEFFICIENTS, eps=1e-7, dtype=nb.DTYPE_F32, ws=P, size=need):
+        return L.nb_muon_update(u, m, g, n, R, C, mu, nesterov, steps, *co, eps, dtype, ws, size, None)
+    for kw in (dict(u=None), dict(g=None), dict(n=-1), dict(R=0), dict(C=-8), dict(mu=float("nan")), dict(eps=-1.0), dict(eps=float("nan")),
+               dict(steps=-1), dict(steps=33), dict(co=(1.0, float("inf"), 0.0)), dict(dtype=3), dict(ws=None), dict(ws=P + 64),
+               dict(size=need - 1), dict(u=_array(P, None)), dict(m=_array(None, P)), dict(g=_array(P, None)), dict(u=_array(P, P + 8)),
+               dict(m=_array(P + 4, P)), dict(g=_array(P, P + 2))):
+        assert call(**kw) == nb.NB_ERR_INVALID_ARG, kw
+        assert nb.nb_last_error()
+    for kw in (dict(R=12), dict(C=100), dict(n=1025), dict(R=32776), dict(co=(40.0, 0.0, 0.0)), dict(co=(3.0, 0.0, 0.0)), dict(co=(1.0, 50.0, -50.0))):
+        assert call(**kw) == nb.NB_ERR_UNSUPPORTED, kw
+    assert call(n=0) == nb.NB_OK
+    # polynomials in use: they keep [0, 1] near itself
+    for co in (nb.MUON_COEFFICIENTS, (2.0, -1.5, 0.5), (1.5, -0.5, 0.0), (1.875, -1.25, 0.375)):
+        assert call(n=0, co=co) == nb.NB_OK, co
+
+
+def test_update_workspace(L):
+    for bad in ((-1, 64, 64), (1, 0, 64), (1, 64, 12), (1025, 64, 64), (1, 32776, 64)):
+        assert L.nb_muon_workspace(*bad) == -1
+        with pytest.raises(nb.NbError):
+            nb.nb_muon_workspace(*bad)
+    assert nb.nb_muon_workspace(0, 64, 64) == 0
+    # two iterates, two symmetric matrices
+    assert nb.nb_muon_workspace(1, 768, 3072) >= 4 * 768 * 3072 + 4 * 768 * 768
+    assert nb.nb_muon_workspace(33, 64, 64) == nb.nb_muon_workspace(32, 64, 64)
+    assert nb.nb_muon_workspace(3, 64, 128) == nb.nb_muon_workspace(3, 128, 64)
+
+
+def test_update_binding_refusals(L):
+    t = torch.zeros(8, 8)
+    with pytest.raises(ValueError, match="one shape"):
+        nb.muon_update([t, torch.zeros(8, 16)])
+    with pytest.raises(ValueError, match="one shape"):
+        nb.muon_update([t, t.bfloat16()])
+    with pytest.raises(ValueError, match="momenta"):
+        nb.muon_update([t], [t.bfloat16()])
+    assert nb.muon_update([]) == []
+
+
 def test_apply_refusals(L):
     def call(m=_array(P, P + 64), w=_array(P, P + 32), u=_array(P, P + 32), n=2, count=10):
         return L.nb_muon_apply(m, w, u, n, count, 0.9, 0.1, None)
