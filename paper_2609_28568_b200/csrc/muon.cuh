@@ -82,6 +82,7 @@ struct MuonPrepare {
     float *momentum[kMuonBatch];   // or all null
     void *out[kMuonBatch];         // muon_normalise_kernel with no step to follow: bf16 results
     double *part;                  // [n][parts]
+    unsigned *done;                // [n], zeroed for the products' counts
     __half *x;                     // [n][count], times `scale`
     long long nvec;                // elements / 8
     int parts;
@@ -147,7 +148,10 @@ muon_momentum_kernel(const __grid_constant__ MuonPrepare p)
         for (int k = 0; k < 8; ++k) sq = fma(static_cast<double>(v[k]), static_cast<double>(v[k]), sq);
     }
     sq = block_sum_256(sq);
-    if (threadIdx.x == 0) p.part[static_cast<long long>(blockIdx.y) * p.parts + blockIdx.x] = sq;
+    if (threadIdx.x == 0) {
+        p.part[static_cast<long long>(blockIdx.y) * p.parts + blockIdx.x] = sq;
+        if (blockIdx.x == 0) p.done[blockIdx.y] = 0;
+    }
 }
 
 // x = fp16(scale v / (|v| + eps)); v from the momentum as the launch before left it. The division is by a 64-bit factor, so that it neither

@@ -193,12 +193,11 @@ int get_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t rows, u
     return NB_OK;
 }
 
-// n dense fp16 matrices [rows, cols] one after the other, as boxes of box_rows x box_cols of one of them. Boxes of 64 columns
-// have the 128-byte swizzle, others none. What lies outside a matrix reads as zero and is not written.
-int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n, uint64_t rows, uint64_t cols, uint32_t box_cols,
-                   uint32_t box_rows)
+// n dense fp16 matrices [rows, cols] one after the other, read as boxes of 64 x 64 of one of them with the 128-byte
+// swizzle. What lies outside a matrix reads as zero.
+int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n, uint64_t rows, uint64_t cols)
 {
-    TmapKey key{ptr, rows, cols, cols, box_cols, box_rows, 2, n};
+    TmapKey key{ptr, rows, cols, cols, 64, 64, 2, n};
     auto it = s.tmaps.find(key);
     if (it != s.tmaps.end()) {
         *out = it->second;
@@ -206,12 +205,12 @@ int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n
     }
     cuuint64_t dims[3] = {cols, rows, n};
     cuuint64_t strides[2] = {cols * 2, rows * cols * 2};
-    cuuint32_t box[3] = {box_cols, box_rows, 1};
+    cuuint32_t box[3] = {64, 64, 1};
     cuuint32_t estr[3] = {1, 1, 1};
     alignas(64) CUtensorMap m;
     memset(&m, 0, sizeof(m));
     CUresult r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS)
         return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) for %llu x [%llu, %llu] at %p", static_cast<int>(r),
@@ -1841,9 +1840,10 @@ int with_norm_form(const NormForm &f, F &&fn)
 }
 
 // ----------------------------------------------------------------------------- orthogonalised momentum
-// The workspace of a group of at most kMuonBatch matrices: two of the iterate, S, P (all fp16), and the norms' partial sums.
+// The workspace of a group of at most kMuonBatch matrices: two of the iterate, S, P (all fp16), the norms' partial sums
+// and the counts of tiles done.
 struct MuonSpace {
-    int64_t x[2], s, p, part, bytes;
+    int64_t x[2], s, p, part, done, bytes;
 };
 int muon_parts(int64_t nvec)  // blocks that read a matrix: about four vectors of eight per thread, 256 at most
 {
@@ -1861,66 +1861,20 @@ MuonSpace muon_space(int64_t n, int64_t R, int64_t C)
     w.s = w.x[1] + up(n * R * C * 2);
     w.p = w.s + up(n * m * m * 2);
     w.part = w.p + up(n * m * m * 2);
-    w.bytes = w.part + up(n * muon_parts(R * C / 8) * 8);
+    w.done = w.part + up(n * muon_parts(R * C / 8) * 8);
+    w.bytes = w.done + up(n * 4);
     return w;
 }
 
-struct NsArgs {
-    const CUtensorMap *A, *B, *D, *T;  // T: D's transposed boxes, or D
-    int M, N, K, n;
-    float alpha, beta, diag;
-    const __half *aux;
-    void *const *out;
-};
-
+// The products of all steps for n matrices: one cooperative launch, since its blocks wait for one another's tiles.
 template <class Cfg>
-int launch_ns(DeviceState &s, const NsArgs &a, cudaStream_t stream)
+int launch_ns(DeviceState &s, NsParams p, cudaStream_t stream)
 {
     static int max_clusters[kMaxDevices] = {};
     int dev = 0;
     NB_CUDA(cudaGetDevice(&dev));
-    if (max_clusters[dev] == 0) {
-        NB_CUDA(cudaFuncSetAttribute(newton_schulz_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     static_cast<int>(Cfg::SMEM_BYTES)));
-        int fit = s.num_sms / Cfg::CG;
-        if (Cfg::CG == 2) {
-            cudaLaunchConfig_t qc = {};
-            qc.gridDim = dim3(static_cast<unsigned>(s.num_sms));
-            qc.blockDim = dim3(kNumThreads);
-            qc.dynamicSmemBytes = Cfg::SMEM_BYTES;
-            cudaLaunchAttribute qa[1];
-            qa[0].id = cudaLaunchAttributeClusterDimension;
-            qa[0].val.clusterDim.x = 2;
-            qa[0].val.clusterDim.y = 1;
-            qa[0].val.clusterDim.z = 1;
-            qc.attrs = qa;
-            qc.numAttrs = 1;
-            int n = 0;
-            NB_CUDA(cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel<Cfg>, &qc));
-            if (n < 1) return fail(NB_ERR_CUDA, "no CTA pair of this kernel fits on the device");
-            if (n < fit) fit = n;
-        }
-        max_clusters[dev] = fit;
-    }
-    NsParams p{};
-    p.M = a.M;
-    p.N = a.N;
-    p.tiles_m = (a.M + Cfg::TILE_M - 1) / Cfg::TILE_M;
-    p.tiles_n = (a.N + Cfg::BLOCK_N - 1) / Cfg::BLOCK_N;
-    p.tiles = Cfg::SYM ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
-    p.units = p.tiles * a.n;
-    p.kblocks = kblocks_of(a.K);
-    p.alpha = a.alpha;
-    p.beta = a.beta;
-    p.diag = a.diag;
-    p.aux = a.aux;
-    p.status = s.status;
-    p.timeout_ns = kDefaultTimeoutNs;
-    for (int i = 0; a.out && i < a.n; ++i) p.out[i] = a.out[i];
-    const int clusters = p.units < max_clusters[dev] ? p.units : max_clusters[dev];
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(clusters * Cfg::CG));
-    cfg.blockDim = dim3(kNumThreads);
+    cfg.blockDim = dim3(kNsThreads);
     cfg.dynamicSmemBytes = Cfg::SMEM_BYTES;
     cfg.stream = stream;
     cudaLaunchAttribute attrs[2];
@@ -1928,23 +1882,39 @@ int launch_ns(DeviceState &s, const NsArgs &a, cudaStream_t stream)
     attrs[0].val.clusterDim.x = Cfg::CG;
     attrs[0].val.clusterDim.y = 1;
     attrs[0].val.clusterDim.z = 1;
-    attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attrs[1].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeCooperative;
+    attrs[1].val.cooperative = 1;
     cfg.attrs = attrs;
-    cfg.numAttrs = dependent_launch_allowed(stream) ? 2 : 1;
-    NB_CUDA(cudaLaunchKernelEx(&cfg, newton_schulz_kernel<Cfg>, *a.A, *a.B, *a.D, *a.T, p));
+    cfg.numAttrs = 1;
+    if (max_clusters[dev] == 0) {  // how many blocks (or pairs) are resident at once
+        NB_CUDA(cudaFuncSetAttribute(newton_schulz_kernel<Cfg>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(Cfg::SMEM_BYTES)));
+        cfg.gridDim = dim3(static_cast<unsigned>(s.num_sms / Cfg::CG * Cfg::CG));
+        int n = 0;
+        NB_CUDA(cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel<Cfg>, &cfg));
+        if (n < 1) return fail(NB_ERR_CUDA, "this kernel does not fit on the device");
+        max_clusters[dev] = n < s.num_sms / Cfg::CG ? n : s.num_sms / Cfg::CG;
+    }
+    const int blocks = (p.m + Cfg::EDGE - 1) / Cfg::EDGE;
+    p.tiles_r = (p.R + Cfg::EDGE - 1) / Cfg::EDGE;
+    p.sym_tiles = blocks * (blocks + 1) / 2 * Cfg::PARTS;
+    p.x_tiles = p.tiles_r * ((p.C + Cfg::BLOCK_N - 1) / Cfg::BLOCK_N);
+    const long long units = 1ll * p.steps * p.n * (2 * p.sym_tiles + p.x_tiles);
+    if (units >= (1ll << 27)) return fail(NB_ERR_UNSUPPORTED, "tile count out of range");
+    p.units = static_cast<int>(units);
+    const int most = p.n * (p.x_tiles > p.sym_tiles ? p.x_tiles : p.sym_tiles);  // tiles of a phase
+    const int clusters = most < max_clusters[dev] ? most : max_clusters[dev];
+    cfg.gridDim = dim3(static_cast<unsigned>(clusters * Cfg::CG));
+    cfg.numAttrs = 2;
+    CUtensorMap x0, x1, sm, pm;
+    int rc;
+    if ((rc = get_batch_tmap(s, &x0, p.x[0], p.n, p.R, p.C)) != NB_OK) return rc;
+    if ((rc = get_batch_tmap(s, &x1, p.x[1], p.n, p.R, p.C)) != NB_OK) return rc;
+    if ((rc = get_batch_tmap(s, &sm, p.s, p.n, p.m, p.m)) != NB_OK) return rc;
+    if ((rc = get_batch_tmap(s, &pm, p.p, p.n, p.m, p.m)) != NB_OK) return rc;
+    NB_CUDA(cudaLaunchKernelEx(&cfg, newton_schulz_kernel<Cfg>, x0, x1, sm, pm, p));
     ++g_launches;
     return NB_OK;
-}
-
-template <bool A_MN, bool B_MN, int EPI>
-int launch_ns_auto(DeviceState &s, const NsArgs &a, cudaStream_t stream)
-{
-    // pairs of CTAs on 256 x 256 tiles where these fill most of the SMs, else a CTA on 128 x 128
-    const int tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
-    const int units = a.n * (EPI == kNsGram || EPI == kNsPoly ? tm * (tm + 1) / 2 : tm * tn);
-    if (2 * units > s.num_sms / 2) return launch_ns<NsCfg<2, 256, A_MN, B_MN, EPI>>(s, a, stream);
-    return launch_ns<NsCfg<1, 128, A_MN, B_MN, EPI>>(s, a, stream);
 }
 
 struct MuonCall {
@@ -1972,6 +1942,7 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
         pr.out[i] = q.update[at + i];
     }
     pr.part = reinterpret_cast<double *>(q.workspace + w.part);
+    pr.done = reinterpret_cast<unsigned *>(q.workspace + w.done);
     pr.x = reinterpret_cast<__half *>(q.workspace + w.x[0]);
     pr.nvec = q.R * q.C / 8;
     pr.parts = muon_parts(pr.nvec);
@@ -1993,36 +1964,36 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
     g_launches += 2;
     if (q.steps == 0) return NB_OK;
 
-    CUtensorMap xl[2], xs[2], sl, ss, st, pl, ps, pt;  // loads, stores, transposed stores
-    for (int i = 0; i < 2; ++i) {
-        if ((rc = get_batch_tmap(s, &xl[i], q.workspace + w.x[i], n, R, C, 64, 64)) != NB_OK) return rc;
-        if ((rc = get_batch_tmap(s, &xs[i], q.workspace + w.x[i], n, R, C, 64, 32)) != NB_OK) return rc;
-    }
-    if ((rc = get_batch_tmap(s, &sl, q.workspace + w.s, n, m, m, 64, 64)) != NB_OK) return rc;
-    if ((rc = get_batch_tmap(s, &ss, q.workspace + w.s, n, m, m, 64, 32)) != NB_OK) return rc;
-    if ((rc = get_batch_tmap(s, &st, q.workspace + w.s, n, m, m, 32, 64)) != NB_OK) return rc;
-    if ((rc = get_batch_tmap(s, &pl, q.workspace + w.p, n, m, m, 64, 64)) != NB_OK) return rc;
-    if ((rc = get_batch_tmap(s, &ps, q.workspace + w.p, n, m, m, 64, 32)) != NB_OK) return rc;
-    if ((rc = get_batch_tmap(s, &pt, q.workspace + w.p, n, m, m, 32, 64)) != NB_OK) return rc;
-    for (int i = 0; i < q.steps; ++i) {
-        const CUtensorMap *x = &xl[i & 1];
-        const bool last = i == q.steps - 1;
-        NsArgs g{x, x, &ss, &st, m, m, k, n, kNsScaleS / (kNsScaleX * kNsScaleX), 0.0f, 0.0f, nullptr, nullptr};
-        rc = tall ? launch_ns_auto<true, true, kNsGram>(s, g, stream) : launch_ns_auto<false, false, kNsGram>(s, g, stream);
-        if (rc != NB_OK) return rc;
-        NsArgs y{&sl, &sl, &ps, &pt, m, m, m, n, q.c / kNsScaleS, q.b, q.a * kNsScaleS,
-                 reinterpret_cast<const __half *>(q.workspace + w.s), nullptr};
-        if ((rc = launch_ns_auto<false, false, kNsPoly>(s, y, stream)) != NB_OK) return rc;
-        // P X from P's rows and X's columns, or X P from X's rows and P's rows (which are its columns)
-        NsArgs u{tall ? x : &pl, tall ? &pl : x, &xs[(i + 1) & 1], &xs[(i + 1) & 1], R, C, m, n,
-                 last ? 1.0f / (kNsScaleS * kNsScaleX) : 1.0f / kNsScaleS, 0.0f, 0.0f, nullptr, last ? q.update + at : nullptr};
-        if (last)
-            rc = tall ? launch_ns_auto<false, false, kNsLast>(s, u, stream) : launch_ns_auto<false, true, kNsLast>(s, u, stream);
-        else
-            rc = tall ? launch_ns_auto<false, false, kNsStep>(s, u, stream) : launch_ns_auto<false, true, kNsStep>(s, u, stream);
-        if (rc != NB_OK) return rc;
-    }
-    return NB_OK;
+    NsParams p{};
+    p.R = R;
+    p.C = C;
+    p.m = m;
+    p.n = n;
+    p.steps = q.steps;
+    p.kb_gram = kblocks_of(k);
+    p.kb_m = kblocks_of(m);
+    p.gram_alpha = kNsScaleS / (kNsScaleX * kNsScaleX);
+    p.poly_alpha = q.c / kNsScaleS;
+    p.poly_beta = q.b;
+    p.poly_diag = q.a * kNsScaleS;
+    p.step_alpha = 1.0f / kNsScaleS;
+    p.last_alpha = 1.0f / (kNsScaleS * kNsScaleX);
+    p.x[0] = pr.x;
+    p.x[1] = reinterpret_cast<__half *>(q.workspace + w.x[1]);
+    p.s = reinterpret_cast<__half *>(q.workspace + w.s);
+    p.p = reinterpret_cast<__half *>(q.workspace + w.p);
+    p.done = pr.done;
+    for (int i = 0; i < n; ++i) p.out[i] = q.update[at + i];
+    p.status = s.status;
+    p.timeout_ns = kDefaultTimeoutNs;
+    // pairs of CTAs on 256 x 256 tiles where these fill half of the SMs, else a CTA on 128 x 128
+    const int tm = (m + 255) / 256, tk = (k + 255) / 256;
+    static const int force = env_int("NB_NS_FORM", 0);
+    if (force == 3) return launch_ns<NsCfg<2, 256>>(s, p, stream);
+    if (force == 2) return launch_ns<NsCfg<2, 128>>(s, p, stream);
+    if (force == 1) return launch_ns<NsCfg<1, 128>>(s, p, stream);
+    if (4 * n * tm * tk > s.num_sms) return launch_ns<NsCfg<2, 256>>(s, p, stream);
+    return launch_ns<NsCfg<1, 128>>(s, p, stream);
 }
 
 // Whether the polynomial keeps everything within what fp16 holds at its scale: singular values start in [0, 1] and step to
@@ -2031,18 +2002,30 @@ bool muon_in_range(int steps, double a, double b, double c)
 {
     double top = 1.001;  // the first rounding may exceed one a little
     for (int i = 0; i < steps; ++i) {
-        if (top * top > 32.0 || !(top <= 8.0)) return false;
-        double next = 0.0, most = 0.0;
-        for (int j = 0; j <= 1000; ++j) {
-            const double x = top * j / 1000.0, s = x * x, p = a + b * s + c * s * s;
-            if (!(std::fabs(p) <= 32.0)) return false;
-            next = std::fmax(next, std::fabs(x * p));
-            most = std::fmax(most, std::fabs(b) * s);
+        const double most = top * top;  // of s = x^2
+        // the factor a + b s + c s^2 and the result x (a + b x^2 + c x^4) are largest at the ends or where their derivatives vanish
+        auto factor = [&](double s) { return std::fabs(a + b * s + c * s * s); };
+        double f = std::fmax(factor(0.0), factor(most)), next = std::sqrt(most) * factor(most);
+        auto inside = [&](double s, bool of_factor) {
+            if (!(s > 0.0 && s < most)) return;
+            if (of_factor) f = std::fmax(f, factor(s));
+            else next = std::fmax(next, std::sqrt(s) * factor(s));
+        };
+        if (c != 0.0) {
+            inside(-b / (2.0 * c), true);
+            const double d = 9.0 * b * b - 20.0 * a * c;  // a + 3 b s + 5 c s^2 = 0
+            if (d >= 0.0) {
+                inside((-3.0 * b + std::sqrt(d)) / (10.0 * c), false);
+                inside((-3.0 * b - std::sqrt(d)) / (10.0 * c), false);
+            }
+        } else if (b != 0.0) {
+            inside(-a / (3.0 * b), false);
         }
-        if (most > 32.0) return false;
+        if (!(most <= 32.0 && f <= 32.0 && std::fabs(b) * most <= 32.0)) return false;
         top = next * 1.01;
+        if (i + 1 < steps && !(top <= 8.0)) return false;  // the last result is bf16
     }
-    return true;  // the last result is bf16
+    return true;
 }
 
 int check_norm(int64_t BT, int64_t C, int stream_dtype)

@@ -1,17 +1,22 @@
-// Products of the Newton-Schulz iteration for a batch of matrices of one shape, on tcgen05:
+// Products of the Newton-Schulz iteration for a batch of matrices of one shape, on tcgen05, in one launch:
 //
 //   S = X X^T (or X^T X for tall X)    P = a I + b S + c S S    X <- P X (or X P)
 //
-// with m = min(R, C): S and P are symmetric [m, m], so only the tiles on and below the diagonal are computed and each is stored twice, as it is and
-// transposed. a X is inside P X: the update is a plain product.
+// with m = min(R, C): S and P are symmetric [m, m], so only their tiles on and below the diagonal are computed and stored. A consumer
+// that needs a tile above it reads the mirrored one in the other major order, which the tensor core takes as it takes the first: no transposed
+// copy exists. a X is inside P X: the update is a plain product.
 //
 // Operands are fp16, accumulators fp32. X, S and P hold values of the order of one and below, and what the iteration amplifies is the
 // rounding of its operands: fp16's eleven bits leave the update 1.1e-3 off (2-norm, gradients with a spectrum as of training), bf16's eight
 // leave it 9e-3 off, at the same speed. Its narrow range is met by powers of two: X is stored times 2^12, S and P times 2^10.
 //
-// The kernel is a persistent one in the manner of gemm_kernel: warp 0 loads tiles by TMA, warp 1 issues the MMAs into one of two accumulators,
-// warps 2..9 run the epilogue of the tile before. Every operand comes as boxes of 64 x 64 elements of one matrix of the batch (3-D
-// maps: what lies outside the matrix reads as zero and is not written), K-major or MN-major by which of the matrix's axes is summed.
+// The work of all steps is one list of tiles, phase by phase (S of every matrix, P of every matrix, X of every matrix, ...), which
+// the CTAs (or CTA pairs) of a cooperative launch walk with the stride of the grid. A matrix's tiles of one phase wait for its tiles of
+// the phase before, counted in global memory; other matrices are not waited for. Inside a CTA it is gemm_kernel's division: warp 0 loads tiles by
+// TMA, warp 1 issues the MMAs into one of two accumulators, warps 2..9 run the epilogue of the tile before. Every operand comes as
+// boxes of 64 x 64 elements of one matrix of the batch (3-D maps: what lies outside the matrix reads as zero).
+//
+// As fifteen launches (three per step) each phase cost 2.5 us more: the drain and the start of a launch.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -20,54 +25,50 @@
 
 namespace nb {
 
-enum NsEpi : int {
-    kNsGram = 0,  // D = alpha acc, symmetric
-    kNsPoly = 1,  // D = alpha acc + beta aux + diag I, symmetric; aux is the operand itself
-    kNsStep = 2,  // D = alpha acc
-    kNsLast = 3   // out (bf16, the caller's) = alpha acc
-};
 constexpr float kNsScaleX = 4096.0f, kNsScaleS = 1024.0f;
 
 struct NsParams {
-    int M, N;              // of D, per matrix
-    int tiles_m, tiles_n;
-    int tiles;             // per matrix: all, or those on and below the diagonal
-    int units;             // tiles of the batch
-    int kblocks;
-    float alpha, beta, diag;
-    const __half *aux;     // kNsPoly: S, [n, M, M]
+    int R, C, m, n;
+    int steps;
+    int tiles_r;             // of X, down its rows
+    int sym_tiles, x_tiles;  // tiles per matrix of S or P, of X
+    int kb_gram, kb_m;     // k-blocks of S = X X^T, and of the other two products
+    int units;             // tiles of all steps and matrices
+    float gram_alpha, poly_alpha, poly_beta, poly_diag, step_alpha, last_alpha;
+    __half *x[2], *s, *p;  // [n, R, C], [n, m, m]
+    unsigned *done;        // [n]: CTAs that have stored their part of a tile, over all phases
+    void *out[kMuonBatch];
     int *status;
     unsigned long long timeout_ns;
-    void *out[kMuonBatch];  // kNsLast
 };
 
-template <int CG_, int BLOCK_N_, bool A_MN_, bool B_MN_, int EPI_>
+constexpr int kNsThreads = kNumThreads + 32;  // and warp 10, which counts finished tiles
+
+template <int CG_, int BLOCK_N_>
 struct NsCfg {
     static constexpr int CG = CG_;
-    static constexpr int TILE_M = kBlockM * CG_;
+    static constexpr int EDGE = kBlockM * CG_;  // rows of a tile; S and P are held in square blocks of this edge, on and below the diagonal
     static constexpr int BLOCK_N = BLOCK_N_;
-    static constexpr bool A_MN = A_MN_;
-    static constexpr bool B_MN = B_MN_;
-    static constexpr int EPI = EPI_;
-    static constexpr bool SYM = EPI_ == kNsGram || EPI_ == kNsPoly;
+    static constexpr int PARTS = EDGE / BLOCK_N_;  // tiles of a square block
     static constexpr uint32_t A_BYTES = kBlockM * kBlockK * 2;
     static constexpr int B_ROWS = BLOCK_N / CG_;
     static constexpr uint32_t B_BYTES = B_ROWS * kBlockK * 2;
-    static constexpr uint32_t BOX_BYTES = 32 * 128;  // 32 rows of 64 elements, or 64 of 32
-    static constexpr uint32_t STG_BYTES = kEpiWarps * BOX_BYTES * (SYM ? 2 : 1);
-    static constexpr int STAGES = SYM ? 5 : 6;
+    static constexpr int PIECES = BLOCK_N / 128;     // of 64 columns per epilogue warp
+    static constexpr uint32_t BOX_BYTES = 32 * 128;  // a piece in staging: 32 rows of 64 elements
+    static constexpr uint32_t STG_BYTES = kEpiWarps * PIECES * BOX_BYTES;
+    static constexpr int STAGES = static_cast<int>((232448 - 512 - STG_BYTES) / (A_BYTES + B_BYTES)) < 7
+                                      ? static_cast<int>((232448 - 512 - STG_BYTES) / (A_BYTES + B_BYTES)) : 7;
     static constexpr uint32_t OFF_B = STAGES * A_BYTES;
     static constexpr uint32_t OFF_STG = STAGES * (A_BYTES + B_BYTES);
     static constexpr uint32_t OFF_BAR = OFF_STG + STG_BYTES;
-    static constexpr uint32_t SMEM_BYTES = OFF_BAR + 256;
+    static constexpr uint32_t SMEM_BYTES = OFF_BAR + 512;
     static constexpr uint32_t TMEM_COLS = 2 * BLOCK_N;
-    static constexpr int STEPS = BLOCK_N / 128;  // pieces of 64 columns per epilogue warp
+    static_assert(EDGE % BLOCK_N == 0, "square blocks");
     static_assert(BLOCK_N == 128 || BLOCK_N == 256, "two accumulators, a power of two of TMEM columns");
-    static_assert(!SYM || TILE_M == BLOCK_N, "tiles below the diagonal mirror onto tiles above it");
     static_assert(SMEM_BYTES <= 232448, "shared memory budget");
 };
 
-// 3-D forms of the tile copies: z is the matrix of the batch.
+// 3-D forms of the tile load: z is the matrix of the batch.
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *m, uint32_t bar, int x, int y, int z)
 {
     asm volatile(
@@ -83,44 +84,132 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z)
         : "memory");
 }
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap *m, uint32_t src, int x, int y, int z)
-{
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
-                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(x), "r"(y), "r"(z)
-                 : "memory");
-}
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-
-// Tile t of a matrix: (row, column) tile. Symmetric results: t runs through the lower triangle row by row.
-template <bool SYM>
-__device__ __forceinline__ void ns_tile(const NsParams &p, int t, int &m_blk, int &n_blk)
+// from L2: what another SM wrote during this launch may lie stale in L1
+__device__ __forceinline__ uint4 ld_global_cg_v4(const void *p)
 {
-    if (SYM) {
-        int i = static_cast<int>((sqrtf(8.0f * static_cast<float>(t) + 1.0f) - 1.0f) * 0.5f);
-        while ((i + 1) * (i + 2) / 2 <= t) ++i;  // the root is off by at most one
-        while (i * (i + 1) / 2 > t) --i;
-        m_blk = i;
-        n_blk = t - i * (i + 1) / 2;
+    uint4 v;
+    asm volatile("ld.global.cg.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ unsigned ld_acquire_gpu(const unsigned *p)
+{
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void red_release_gpu(unsigned *p, unsigned v)
+{
+    asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+// between plain accesses to global memory and those of the TMA unit, in either direction
+__device__ __forceinline__ void fence_proxy_async_all()
+{
+    asm volatile("fence.proxy.async;" ::: "memory");
+}
+
+enum NsPhase : int { kNsGram = 0, kNsPoly = 1, kNsStep = 2 };
+
+// What a unit of the list is: a tile of one phase of one matrix in one step.
+struct NsUnit {
+    int step, phase, z, m_blk, n_blk;
+    unsigned need;  // tiles of this matrix that come before
+};
+template <class Cfg>
+__device__ __forceinline__ NsUnit ns_unit(const NsParams &p, int u)
+{
+    NsUnit t;
+    const int sym = p.n * p.sym_tiles, per_step = 2 * sym + p.n * p.x_tiles;
+    t.step = u / per_step;
+    int r = u - t.step * per_step;
+    t.need = static_cast<unsigned>(t.step) * (2 * p.sym_tiles + p.x_tiles);
+    if (r < 2 * sym) {
+        t.phase = r < sym ? kNsGram : kNsPoly;
+        if (t.phase == kNsPoly) {
+            r -= sym;
+            t.need += p.sym_tiles;
+        }
+        t.z = r / p.sym_tiles;
+        const int part = r - t.z * p.sym_tiles, k = part / Cfg::PARTS;  // blocks through the lower triangle row by row
+        int i = static_cast<int>((sqrtf(8.0f * static_cast<float>(k) + 1.0f) - 1.0f) * 0.5f);
+        while ((i + 1) * (i + 2) / 2 <= k) ++i;  // the root is off by at most one
+        while (i * (i + 1) / 2 > k) --i;
+        t.m_blk = i;
+        t.n_blk = (k - i * (i + 1) / 2) * Cfg::PARTS + part % Cfg::PARTS;
     } else {
-        n_blk = t / p.tiles_m;
-        m_blk = t - n_blk * p.tiles_m;
+        t.phase = kNsStep;
+        t.need += 2 * p.sym_tiles;
+        r -= 2 * sym;
+        t.z = r / p.x_tiles;
+        const int k = r - t.z * p.x_tiles;
+        t.n_blk = k / p.tiles_r;
+        t.m_blk = k - t.n_blk * p.tiles_r;
+    }
+    return t;
+}
+// Whether an operand's box of k-block kb is read MN-major. X: by the side that is summed. S, P: where the box lies in a block above the
+// diagonal and its mirror is read.
+template <class Cfg>
+__device__ __forceinline__ bool ns_a_mn(const NsParams &p, const NsUnit &t, int kb)
+{
+    if (t.phase == kNsGram) return p.R > p.C;
+    if (t.phase == kNsStep && p.R > p.C) return false;  // X's rows
+    return kb * kBlockK / Cfg::EDGE > t.m_blk;
+}
+template <class Cfg>
+__device__ __forceinline__ bool ns_b_mn(const NsParams &p, const NsUnit &t, int kb)
+{
+    if (t.phase == kNsGram) return p.R > p.C;
+    if (t.phase == kNsStep && p.R <= p.C) return true;  // X's columns
+    return kb * kBlockK / Cfg::EDGE > t.n_blk / Cfg::PARTS;
+}
+
+// Whether both operands are the same rows of the same matrix, as on the diagonal of S and P: they are then fetched once.
+template <class Cfg>
+__device__ __forceinline__ bool ns_same_operand(const NsUnit &t)
+{
+    return Cfg::PARTS == 1 && t.phase != kNsStep && t.m_blk == t.n_blk;
+}
+
+// Waits, for a limited time, until `need` tile parts of a matrix are stored.
+// status0: the status word as the launch found it.
+__device__ __forceinline__ bool ns_wait_done(const WaitCtx &w, int status0, const unsigned *done, unsigned need, int where)
+{
+    if (ld_acquire_gpu(done) >= need) return true;
+    const uint64_t t0 = ptx::globaltimer_ns();
+    for (uint32_t it = 1;; ++it) {
+        if (ld_acquire_gpu(done) >= need) return true;
+        if ((it & 15u) == 0) {
+            // another block's failure ends this one too: what it waits for will not come
+            if (ptx::ld_shared_u32_volatile(w.abort_addr) != 0 || *reinterpret_cast<volatile int *>(w.status) != status0) {
+                ptx::st_shared_u32_volatile(w.abort_addr, 1);
+                return false;
+            }
+            if (ptx::globaltimer_ns() - t0 > w.timeout_ns) {
+                ptx::st_shared_u32_volatile(w.abort_addr, 1);
+                if (atomicCAS(w.status, 0, kStatusTimeout) == 0) {
+                    w.status[1] = where;
+                    w.status[2] = static_cast<int>(blockIdx.x);
+                }
+                return false;
+            }
+        }
     }
 }
 
 template <class Cfg>
-__global__ void __launch_bounds__(kNumThreads, 1)
-newton_schulz_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                     const __grid_constant__ CUtensorMap tmD, const __grid_constant__ CUtensorMap tmT,
+__global__ void __launch_bounds__(kNsThreads, 1)
+newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_constant__ CUtensorMap tmX1,
+                     const __grid_constant__ CUtensorMap tmS, const __grid_constant__ CUtensorMap tmP,
                      const __grid_constant__ NsParams p)
 {
     constexpr int BLOCK_N = Cfg::BLOCK_N;
     constexpr int STAGES = Cfg::STAGES;
-    constexpr int EPI = Cfg::EPI;
     constexpr int CG = Cfg::CG;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem = ptx::smem_u32(smem_raw);
@@ -142,6 +231,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
     const uint32_t tmem_slot = bar0 + 240;
     const uint32_t abort_addr = bar0 + 244;
     const uint32_t epi_abort_addr = bar0 + 248;
+    auto stored_word = [&](int w) { return bar0 + 256u + 4u * w; };  // tiles that epilogue warp w has stored
     static_assert(8 * (2 * STAGES + 4) <= 240, "barrier region");
 
     if (warp == 0) {
@@ -152,16 +242,17 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
             ptx::mbar_init(tfull_bar(lane - STAGES), 1);
             ptx::mbar_init(tempty_bar(lane - STAGES), kEpiWarps * CG);
         }
+        if (lane < kEpiWarps) ptx::st_shared_u32_volatile(stored_word(lane), 0);
         if (lane == 31) {
             ptx::st_shared_u32_volatile(abort_addr, 0);
             ptx::st_shared_u32_volatile(epi_abort_addr, 0);
         }
         ptx::fence_barrier_init();
         if (lane == 30) {
-            ptx::prefetch_tmap(&tmA);
-            ptx::prefetch_tmap(&tmB);
-            if (EPI != kNsLast) ptx::prefetch_tmap(&tmD);
-            if (Cfg::SYM) ptx::prefetch_tmap(&tmT);
+            ptx::prefetch_tmap(&tmX0);
+            ptx::prefetch_tmap(&tmX1);
+            ptx::prefetch_tmap(&tmS);
+            ptx::prefetch_tmap(&tmP);
         }
         __syncwarp();
     }
@@ -173,12 +264,10 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
     if (CG == 2) ptx::cluster_sync();
     else __syncthreads();
     ptx::tc_fence_after();
-    // what is above touched this CTA's own memory only and may run while the launch before still drains
-    ptx::grid_launch_dependents();
-    ptx::grid_dependency_wait();
     const uint32_t tmem_base = ptx::ld_shared_u32_volatile(tmem_slot);
     const WaitCtx wctx{abort_addr, p.status, p.timeout_ns};
     const WaitCtx wctx_epi{abort_addr, p.status, 2 * p.timeout_ns};
+    const int status0 = *reinterpret_cast<volatile int *>(p.status);
 
     auto load = [&](uint32_t dst, const CUtensorMap *m, uint32_t bar, int x, int y, int z) {
         if (CG == 2) tma_load_3d_pair(dst, m, bar, x, y, z);
@@ -194,25 +283,34 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
             uint32_t phase = 0;
             bool ok = true;
             for (int u = first_unit; u < p.units && ok; u += unit_stride) {
-                const int z = u / p.tiles;
-                int m_blk, n_blk;
-                ns_tile<Cfg::SYM>(p, u - z * p.tiles, m_blk, n_blk);
-                const int m0 = m_blk * Cfg::TILE_M + static_cast<int>(rank) * kBlockM;
-                const int n0 = n_blk * BLOCK_N + static_cast<int>(rank) * Cfg::B_ROWS;
-                for (int kb = 0; kb < p.kblocks; ++kb) {
+                const NsUnit t = ns_unit<Cfg>(p, u);
+                const CUtensorMap *x = (t.step & 1) ? &tmX1 : &tmX0;
+                const bool tall = p.R > p.C;
+                const CUtensorMap *mapA = t.phase == kNsGram ? x : t.phase == kNsPoly ? &tmS : tall ? x : &tmP;
+                const CUtensorMap *mapB = t.phase == kNsGram ? x : t.phase == kNsPoly ? &tmS : tall ? &tmP : x;
+                const int m0 = t.m_blk * Cfg::EDGE + static_cast<int>(rank) * kBlockM;
+                const int n0 = t.n_blk * BLOCK_N + static_cast<int>(rank) * Cfg::B_ROWS;
+                const int kblocks = t.phase == kNsGram ? p.kb_gram : p.kb_m;
+                const bool same = ns_same_operand<Cfg>(t);
+                ok = ns_wait_done(wctx, status0, p.done + t.z, t.need * CG, 700 + t.phase);
+                if (!ok) break;
+                fence_proxy_async_all();  // the tiles were stored by plain stores
+                for (int kb = 0; kb < kblocks; ++kb) {
                     ok = wait_barrier(wctx, empty_bar(stage), phase ^ 1u, 100 + stage);
                     if (!ok) break;
                     const uint32_t fb = (CG == 2) ? ptx::mapa(full_bar(stage), 0) : full_bar(stage);
-                    if (rank == 0) ptx::mbar_expect_tx(full_bar(stage), CG * (Cfg::A_BYTES + Cfg::B_BYTES));
+                    if (rank == 0) ptx::mbar_expect_tx(full_bar(stage), CG * (Cfg::A_BYTES + (same ? 0u : Cfg::B_BYTES)));
                     const uint32_t sa = smem + stage * Cfg::A_BYTES;
                     const uint32_t sb = smem + Cfg::OFF_B + stage * Cfg::B_BYTES;
                     const int k0 = kb * kBlockK;
+                    const bool a_mn = ns_a_mn<Cfg>(p, t, kb), b_mn = ns_b_mn<Cfg>(p, t, kb);
 #pragma unroll
                     for (int j = 0; j < kBlockM / 64; ++j)
-                        load(sa + j * 8192u, &tmA, fb, Cfg::A_MN ? m0 + j * 64 : k0, Cfg::A_MN ? k0 : m0 + j * 64, z);
+                        load(sa + j * 8192u, mapA, fb, a_mn ? m0 + j * 64 : k0, a_mn ? k0 : m0 + j * 64, t.z);
+                    if (!same)
 #pragma unroll
-                    for (int j = 0; j < Cfg::B_ROWS / 64; ++j)
-                        load(sb + j * 8192u, &tmB, fb, Cfg::B_MN ? n0 + j * 64 : k0, Cfg::B_MN ? k0 : n0 + j * 64, z);
+                        for (int j = 0; j < Cfg::B_ROWS / 64; ++j)
+                            load(sb + j * 8192u, mapB, fb, b_mn ? n0 + j * 64 : k0, b_mn ? k0 : n0 + j * 64, t.z);
                     if (++stage == STAGES) {
                         stage = 0;
                         phase ^= 1u;
@@ -224,27 +322,34 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         // ------------------------------------------------------------ MMA issuer (leader CTA only)
         if (rank == 0 && ptx::elect_one()) {
             // bits 7 and 10 clear: both operands fp16
-            constexpr uint32_t idesc = make_idesc(Cfg::TILE_M, BLOCK_N, Cfg::A_MN, Cfg::B_MN) & ~((1u << 7) | (1u << 10));
+            constexpr uint32_t idesc0 = make_idesc(Cfg::EDGE, BLOCK_N, false, false) & ~((1u << 7) | (1u << 10));
             int stage = 0;
             uint32_t phase = 0;
             int acc = 0;
             uint32_t acc_phase = 0;
             bool ok = true;
             for (int u = first_unit; u < p.units && ok; u += unit_stride) {
+                const NsUnit t = ns_unit<Cfg>(p, u);
+                const int kblocks = t.phase == kNsGram ? p.kb_gram : p.kb_m;
+                const bool same = ns_same_operand<Cfg>(t);
                 ok = wait_barrier(wctx, tempty_bar(acc), acc_phase ^ 1u, 200 + acc);
                 if (!ok) break;
                 ptx::tc_fence_after();
                 const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * BLOCK_N);
-                for (int kb = 0; kb < p.kblocks; ++kb) {
+                for (int kb = 0; kb < kblocks; ++kb) {
                     ok = wait_barrier(wctx, full_bar(stage), phase, 300 + stage);
                     if (!ok) break;
                     ptx::tc_fence_after();
                     const uint32_t sa = smem + stage * Cfg::A_BYTES;
-                    const uint32_t sb = smem + Cfg::OFF_B + stage * Cfg::B_BYTES;
-                    const uint64_t adesc = Cfg::A_MN ? make_smem_desc(sa, 8192, 1024) : make_smem_desc(sa, 16, 1024);
-                    const uint64_t bdesc = Cfg::B_MN ? make_smem_desc(sb, 8192, 1024) : make_smem_desc(sb, 16, 1024);
-                    constexpr uint32_t a_step = Cfg::A_MN ? (2048u >> 4) : (32u >> 4);
-                    constexpr uint32_t b_step = Cfg::B_MN ? (2048u >> 4) : (32u >> 4);
+                    const uint32_t sb = same ? sa : smem + Cfg::OFF_B + stage * Cfg::B_BYTES;
+                    const bool a_mn = ns_a_mn<Cfg>(p, t, kb), b_mn = ns_b_mn<Cfg>(p, t, kb);
+                    // K-major: 8-row groups 1024 B apart, 16 k = 32 B inside the swizzle row.
+                    // MN-major: 64-wide chunks 8192 B apart, 8-k groups 1024 B apart, 16 k = 2048 B.
+                    const uint64_t adesc = make_smem_desc(sa, a_mn ? 8192 : 16, 1024);
+                    const uint64_t bdesc = make_smem_desc(sb, b_mn ? 8192 : 16, 1024);
+                    const uint32_t a_step = a_mn ? (2048u >> 4) : (32u >> 4);
+                    const uint32_t b_step = b_mn ? (2048u >> 4) : (32u >> 4);
+                    const uint32_t idesc = idesc0 | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
 #pragma unroll
                     for (int k = 0; k < kBlockK / kUmmaK; ++k)
                         ptx::umma_bf16<CG>(d_tmem, adesc + static_cast<uint64_t>(k * a_step),
@@ -263,129 +368,163 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
                 }
             }
         }
+    } else if (warp == 10) {
+        // ------------------------------------------------------------ count of finished tiles
+        // A tile part counts once all epilogue warps have issued their stores of it. The release, which waits for the stores to arrive (about a
+        // microsecond), is this warp's business: the epilogue goes on with the next tile meanwhile.
+        uint32_t tile = 0;
+        for (int u = first_unit; u < p.units; u += unit_stride) {
+            const NsUnit t = ns_unit<Cfg>(p, u);
+            if (t.phase == kNsStep && t.step == p.steps - 1) break;  // nobody waits for the results themselves
+            ++tile;
+            bool ok = true;
+            const uint64_t t0 = ptx::globaltimer_ns();
+            for (uint32_t it = 1;; ++it) {
+                const bool here = lane >= kEpiWarps || ptx::ld_shared_u32_volatile(stored_word(lane)) >= tile;
+                if (__all_sync(0xffffffffu, here)) break;
+                if ((it & 63u) == 0) {
+                    const bool gone = ptx::ld_shared_u32_volatile(abort_addr) != 0 || ptx::ld_shared_u32_volatile(epi_abort_addr) != 0 ||
+                                      ptx::globaltimer_ns() - t0 > 3 * p.timeout_ns;  // longer than the others' waits: they report
+                    if (__any_sync(0xffffffffu, gone)) {
+                        ok = false;
+                        break;
+                    }
+                }
+            }
+            if (!ok) break;
+            __threadfence_block();
+            __syncwarp();
+            if (lane == 0) red_release_gpu(p.done + t.z, 1);
+        }
     } else {
         // ------------------------------------------------------------ epilogue (warps 2..9), warp by warp
-        // A warp owns 32 rows (its TMEM lane quarter) and half of the tile's columns, 64 columns at a time.
+        // A warp owns 32 rows (its TMEM lane quarter) and half of the tile's columns, in pieces of 64. It turns them in shared memory of its
+        // own and stores whole pieces of rows with plain stores (TMA stores, which had to be waited for before a box was used again, took
+        // 2000 cycles longer per tile).
         const int q = warp & 3;
         const int hf = (warp - 2) >> 2;
         const int ew = warp - 2;
-        const uint32_t stg = smem + Cfg::OFF_STG + static_cast<uint32_t>(ew) * Cfg::BOX_BYTES * (Cfg::SYM ? 2 : 1);
-        const uint32_t stgT = stg + Cfg::BOX_BYTES;
+        constexpr int PIECES = Cfg::PIECES;
+        const uint32_t stg = smem + Cfg::OFF_STG + static_cast<uint32_t>(ew * PIECES) * Cfg::BOX_BYTES;
+        const uint32_t mine = stg + static_cast<uint32_t>(lane) * 128u;  // this lane's row
         const uint32_t sw = static_cast<uint32_t>(lane & 7);
-        const ptx::f2 al = ptx::make_f2(p.alpha, p.alpha);
+        const int rr0 = lane >> 3, cc = lane & 7;  // eight lanes to 64 columns of a row where memory is accessed
+        const uint32_t flat = stg + static_cast<uint32_t>(rr0) * 128u;
         int acc = 0;
-        uint32_t acc_phase = 0;
+        uint32_t acc_phase = 0, tile = 0;
         for (int u = first_unit; u < p.units; u += unit_stride) {
             if (ptx::ld_shared_u32_volatile(epi_abort_addr) != 0) break;
-            const int z = u / p.tiles;
-            int m_blk, n_blk;
-            ns_tile<Cfg::SYM>(p, u - z * p.tiles, m_blk, n_blk);
-            const int y0 = m_blk * Cfg::TILE_M + static_cast<int>(rank) * kBlockM + q * 32;  // the warp's first row
-            const int x00 = n_blk * BLOCK_N + hf * (BLOCK_N / 2);                            // and first column
-            const int row = y0 + lane;
+            const NsUnit t = ns_unit<Cfg>(p, u);
+            const int y0 = t.m_blk * Cfg::EDGE + static_cast<int>(rank) * kBlockM + q * 32;  // the warp's first row
+            const int x0 = t.n_blk * BLOCK_N + hf * (BLOCK_N / 2);                           // and first column
+            const bool poly = t.phase == kNsPoly, last = t.phase == kNsStep && t.step == p.steps - 1;
+            const int M = t.phase == kNsStep ? p.R : p.m, N = t.phase == kNsStep ? p.C : p.m;
+            const float alpha = t.phase == kNsGram ? p.gram_alpha : poly ? p.poly_alpha : last ? p.last_alpha : p.step_alpha;
+            const ptx::f2 al = ptx::make_f2(alpha, alpha);
+            // eight rows of four lie 4 N apart; the lane's first 16 bytes
+            const long long at = (static_cast<long long>(t.z) * M + y0 + rr0) * N + x0 + cc * 8;
             bool ok = true;
-            if (lane == 0) ok = wait_barrier(wctx_epi, tfull_bar(acc), acc_phase, 400 + acc);
+            auto in_row = [&](int i) { return y0 + rr0 + i * 4 < M; };
+            if (poly) {  // b S is added: the tile's part of S comes into staging while the product is formed
+                if (lane == 0) ok = ns_wait_done(wctx_epi, status0, p.done + t.z, t.need * CG, 710);
+                __syncwarp();
+#pragma unroll 1
+                for (int piece = 0; piece < PIECES; ++piece) {
+                    const bool in_col = x0 + piece * 64 + cc * 8 < N;
+                    uint4 v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        v[i] = in_row(i) && in_col ? ld_global_cg_v4(p.s + at + static_cast<long long>(i) * 4 * N + piece * 64)
+                                                   : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        ptx::st_shared_v4(flat + piece * Cfg::BOX_BYTES + i * 512u +
+                                              (static_cast<uint32_t>(cc ^ ((rr0 + i * 4) & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
+                }
+                __syncwarp();
+            }
+            if (lane == 0) ok = wait_barrier(wctx_epi, tfull_bar(acc), acc_phase, 400 + acc) && ok;
             ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
             if (!ok) ptx::st_shared_u32_volatile(epi_abort_addr, 1);
             ptx::tc_fence_after();
             const uint32_t t_acc = tmem_base + (static_cast<uint32_t>(q * 32) << 16) +
                                    static_cast<uint32_t>(acc * BLOCK_N + hf * (BLOCK_N / 2));
+            uint32_t r[2 * PIECES][32];
 #pragma unroll
-            for (int step = 0; step < Cfg::STEPS; ++step) {
-                const int x0 = x00 + step * 64;
-                uint32_t r[2][32];
-                ptx::tmem_ld_32x32_issue(t_acc + static_cast<uint32_t>(step * 64), r[0]);
-                ptx::tmem_ld_32x32_issue(t_acc + static_cast<uint32_t>(step * 64 + 32), r[1]);
-                uint4 aux[EPI == kNsPoly ? 8 : 1];
-                if constexpr (EPI == kNsPoly) {
-                    const __half *src = p.aux + (static_cast<long long>(z) * p.M + row) * p.N + x0;
+            for (int i = 0; i < 2 * PIECES; ++i) ptx::tmem_ld_32x32_issue(t_acc + static_cast<uint32_t>(i * 32), r[i]);
+            ptx::tmem_ld_wait_32(r[0]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        aux[j] = row < p.M && x0 + j * 8 < p.N ? ptx::ld_global_v4(src + j * 8) : make_uint4(0, 0, 0, 0);
-                }
-                ptx::tmem_ld_wait_32(r[0]);
-                ptx::reg_fence_32(r[1]);
-                if (step == Cfg::STEPS - 1) {  // the accumulator's last column is in registers
-                    ptx::tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (CG == 2) ptx::mbar_arrive_cluster(ptx::mapa(tempty_bar(acc), 0));
-                        else ptx::mbar_arrive(tempty_bar(acc));
+            for (int i = 1; i < 2 * PIECES; ++i) ptx::reg_fence_32(r[i]);
+            ptx::tc_fence_before();  // the accumulator is in registers
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 2) ptx::mbar_arrive_cluster(ptx::mapa(tempty_bar(acc), 0));
+                else ptx::mbar_arrive(tempty_bar(acc));
+            }
+            __half *dst = t.phase == kNsGram ? p.s : poly ? p.p : p.x[(t.step + 1) & 1];
+            uint4 *d4 = reinterpret_cast<uint4 *>(dst + at);
+            if (last) d4 = static_cast<uint4 *>(p.out[t.z]) + (at - static_cast<long long>(t.z) * M * N) / 8;
+#pragma unroll
+            for (int piece = 0; piece < PIECES; ++piece) {
+                const uint32_t box = mine + piece * Cfg::BOX_BYTES;
+                // eight columns at a time: f gives their words from their pairs
+                auto convert = [&](auto &&f) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t (&rj)[32] = r[2 * piece + (j >> 2)];
+                        uint32_t w[4];
+                        f(j, w, [&](int k) { return ptx::make_f2_bits(rj[(j & 3) * 8 + 2 * k], rj[(j & 3) * 8 + 2 * k + 1]); });
+                        ptx::st_shared_v4(box + ((static_cast<uint32_t>(j) ^ sw) << 4), w[0], w[1], w[2], w[3]);
                     }
-                    __syncwarp();
-                }
-                // the staging boxes are free once the copies of the step before have read them
-                ptx::bulk_wait_group_read<0>();
-                __syncwarp();
-                const bool mirror = Cfg::SYM && m_blk != n_blk;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {  // eight columns
-                    uint32_t w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int c = j * 8 + 2 * k;
-                        ptx::f2 v = ptx::make_f2_bits(r[c >> 5][c & 31], r[c >> 5][(c & 31) + 1]);
-                        float lo, hi;
-                        if constexpr (EPI == kNsPoly) {
-                            const uint32_t a2 = k == 0 ? aux[j].x : k == 1 ? aux[j].y : k == 2 ? aux[j].z : aux[j].w;
-                            const float2 s = __half22float2(*reinterpret_cast<const __half2 *>(&a2));
-                            v = ptx::fma2(v, al, ptx::make_f2(s.x * p.beta + (row == x0 + c ? p.diag : 0.0f),
-                                                              s.y * p.beta + (row == x0 + c + 1 ? p.diag : 0.0f)));
-                        } else {
-                            v = ptx::mul2(v, al);
-                        }
-                        ptx::split_f2(v, lo, hi);
-                        w[k] = EPI == kNsLast ? ptx::pack_bf16x2(lo, hi) : pack_f16x2(lo, hi);
-                    }
-                    ptx::st_shared_v4(stg + static_cast<uint32_t>(lane) * 128u + ((static_cast<uint32_t>(j) ^ sw) << 4), w[0], w[1],
-                                      w[2], w[3]);
-                    if (mirror) {
-                        // transposed: 64 rows (the columns) of 32 elements. Neighbouring lanes swap halves, so that each stores
-                        // two rows' values of one column as a word: even lanes of column c, odd lanes of column c + 1.
+                };
+                if (poly) {
+                    convert([&](int j, uint32_t (&w)[4], auto &&pair) {
+                        uint32_t a4[4];
+                        ptx::ld_shared_v4(box + ((static_cast<uint32_t>(j) ^ sw) << 4), a4[0], a4[1], a4[2], a4[3]);
+                        const int d = y0 + lane - (x0 + piece * 64 + j * 8);  // the diagonal's place among the eight
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const uint32_t other = __shfl_xor_sync(0xffffffffu, w[k], 1);
-                            const uint32_t word = (lane & 1) ? __byte_perm(other, w[k], 0x7632) : __byte_perm(w[k], other, 0x5410);
-                            const uint32_t col = static_cast<uint32_t>(j * 8 + 2 * k + (lane & 1));
-                            ptx::st_shared_u32(stgT + col * 64u + static_cast<uint32_t>(lane & 30) * 2u, word);
+                            const float2 s = __half22float2(*reinterpret_cast<const __half2 *>(&a4[k]));
+                            const ptx::f2 add = ptx::make_f2(fmaf(s.x, p.poly_beta, d == 2 * k ? p.poly_diag : 0.0f),
+                                                             fmaf(s.y, p.poly_beta, d == 2 * k + 1 ? p.poly_diag : 0.0f));
+                            float lo, hi;
+                            ptx::split_f2(ptx::fma2(pair(k), al, add), lo, hi);
+                            w[k] = pack_f16x2(lo, hi);
                         }
-                    }
-                }
-                if constexpr (EPI == kNsLast) {
-                    __syncwarp();
-                    // eight lanes to a row: whole 128-byte pieces of the caller's rows
-                    uint4 *out = static_cast<uint4 *>(p.out[z]);
+                    });
+                } else if (last) {
+                    convert([&](int, uint32_t (&w)[4], auto &&pair) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int rr = i * 4 + (lane >> 3), cc = lane & 7;
-                        uint32_t w[4];
-                        ptx::ld_shared_v4(stg + static_cast<uint32_t>(rr) * 128u +
-                                              ((static_cast<uint32_t>(cc) ^ static_cast<uint32_t>(rr & 7)) << 4),
-                                          w[0], w[1], w[2], w[3]);
-                        if (ok && y0 + rr < p.M && x0 + cc * 8 < p.N)
-                            out[(static_cast<long long>(y0 + rr) * p.N + x0) / 8 + cc] = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                    __syncwarp();
+                        for (int k = 0; k < 4; ++k) w[k] = pack_f2_bf16x2(ptx::mul2(pair(k), al));
+                    });
                 } else {
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (ptx::elect_one()) {
-                        if (ok && y0 < p.M && x0 < p.N) {
-                            tma_store_3d(&tmD, stg, x0, y0, z);
-                            if (mirror) tma_store_3d(&tmT, stgT, y0, x0, z);
+                    convert([&](int, uint32_t (&w)[4], auto &&pair) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            float lo, hi;
+                            ptx::split_f2(ptx::mul2(pair(k), al), lo, hi);
+                            w[k] = pack_f16x2(lo, hi);
                         }
-                        ptx::bulk_commit_group();
-                    }
-                    __syncwarp();
+                    });
+                }
+                __syncwarp();
+                const bool in_col = ok && x0 + piece * 64 + cc * 8 < N;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t w[4];
+                    ptx::ld_shared_v4(flat + piece * Cfg::BOX_BYTES + i * 512u + (static_cast<uint32_t>(cc ^ ((rr0 + i * 4) & 7)) << 4),
+                                      w[0], w[1], w[2], w[3]);
+                    if (in_col && in_row(i)) d4[static_cast<long long>(i) * (N / 2) + piece * 8] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
+            __threadfence_block();
+            __syncwarp();
+            if (lane == 0 && ok) ptx::st_shared_u32_volatile(stored_word(ew), ++tile);
             if (++acc == 2) {
                 acc = 0;
                 acc_phase ^= 1u;
             }
         }
-        ptx::bulk_wait_group<0>();
-        __syncwarp();
     }
 
     // ---------------------------------------------------------------- common exit
