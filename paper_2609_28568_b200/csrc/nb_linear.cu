@@ -1897,7 +1897,7 @@ int launch_ns(DeviceState &s, NsParams p, cudaStream_t stream)
     }
     const int blocks = (p.m + Cfg::EDGE - 1) / Cfg::EDGE;
     p.tiles_r = (p.R + Cfg::EDGE - 1) / Cfg::EDGE;
-    p.sym_tiles = blocks * (blocks + 1) / 2 * Cfg::PARTS;
+    p.sym_tiles = blocks * (blocks + 1) / 2;
     p.x_tiles = p.tiles_r * ((p.C + Cfg::BLOCK_N - 1) / Cfg::BLOCK_N);
     const long long units = 1ll * p.steps * p.n * (2 * p.sym_tiles + p.x_tiles);
     if (units >= (1ll << 27)) return fail(NB_ERR_UNSUPPORTED, "tile count out of range");
@@ -1986,14 +1986,12 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
     for (int i = 0; i < n; ++i) p.out[i] = q.update[at + i];
     p.status = s.status;
     p.timeout_ns = kDefaultTimeoutNs;
-    // pairs of CTAs on 256 x 256 tiles where these fill half of the SMs, else a CTA on 128 x 128
-    const int tm = (m + 255) / 256, tk = (k + 255) / 256;
-    static const int force = env_int("NB_NS_FORM", 0);
-    if (force == 3) return launch_ns<NsCfg<2, 256>>(s, p, stream);
-    if (force == 2) return launch_ns<NsCfg<2, 128>>(s, p, stream);
-    if (force == 1) return launch_ns<NsCfg<1, 128>>(s, p, stream);
-    if (4 * n * tm * tk > s.num_sms) return launch_ns<NsCfg<2, 256>>(s, p, stream);
-    return launch_ns<NsCfg<1, 128>>(s, p, stream);
+    // Pairs of CTAs on 256 x 256 tiles where X has two of them for every pair, else CTAs on 128 x 128: a phase then ends sooner, at twice the
+    // reads. Measured, us (128, 256): 10 x 768 x 768 (90 tiles of 256) 136, 156; 4 x 3072 x 768 (144) 202, 215; 16 x 768 x 768 (144) 196, 176;
+    // 6 x 2304 x 768 (162) 202, 204; 6 x 3072 x 768 (216) 247, 238; 28 x 1024 x 1024 (448) 779, 599.
+    const int tr = (R + 255) / 256, tc = (C + 255) / 256;
+    if (static_cast<long long>(n) * tr * tc >= s.num_sms) return launch_ns<NsCfg<2>>(s, p, stream);
+    return launch_ns<NsCfg<1>>(s, p, stream);
 }
 
 // Whether the polynomial keeps everything within what fp16 holds at its scale: singular values start in [0, 1] and step to

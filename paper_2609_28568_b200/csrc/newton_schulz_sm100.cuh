@@ -44,12 +44,11 @@ struct NsParams {
 
 constexpr int kNsThreads = kNumThreads + 32;  // and warp 10, which counts finished tiles
 
-template <int CG_, int BLOCK_N_>
+template <int CG_>
 struct NsCfg {
     static constexpr int CG = CG_;
-    static constexpr int EDGE = kBlockM * CG_;  // rows of a tile; S and P are held in square blocks of this edge, on and below the diagonal
-    static constexpr int BLOCK_N = BLOCK_N_;
-    static constexpr int PARTS = EDGE / BLOCK_N_;  // tiles of a square block
+    static constexpr int EDGE = kBlockM * CG_;  // tiles are square, so those above the diagonal mirror those below
+    static constexpr int BLOCK_N = EDGE;
     static constexpr uint32_t A_BYTES = kBlockM * kBlockK * 2;
     static constexpr int B_ROWS = BLOCK_N / CG_;
     static constexpr uint32_t B_BYTES = B_ROWS * kBlockK * 2;
@@ -63,8 +62,7 @@ struct NsCfg {
     static constexpr uint32_t OFF_BAR = OFF_STG + STG_BYTES;
     static constexpr uint32_t SMEM_BYTES = OFF_BAR + 512;
     static constexpr uint32_t TMEM_COLS = 2 * BLOCK_N;
-    static_assert(EDGE % BLOCK_N == 0, "square blocks");
-    static_assert(BLOCK_N == 128 || BLOCK_N == 256, "two accumulators, a power of two of TMEM columns");
+    static_assert(2 * BLOCK_N <= 512, "two accumulators must fit in TMEM");
     static_assert(SMEM_BYTES <= 232448, "shared memory budget");
 };
 
@@ -108,9 +106,9 @@ __device__ __forceinline__ void red_release_gpu(unsigned *p, unsigned v)
     asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 // between plain accesses to global memory and those of the TMA unit, in either direction
-__device__ __forceinline__ void fence_proxy_async_all()
+__device__ __forceinline__ void fence_proxy_async_global()
 {
-    asm volatile("fence.proxy.async;" ::: "memory");
+    asm volatile("fence.proxy.async.global;" ::: "memory");
 }
 
 enum NsPhase : int { kNsGram = 0, kNsPoly = 1, kNsStep = 2 };
@@ -120,7 +118,6 @@ struct NsUnit {
     int step, phase, z, m_blk, n_blk;
     unsigned need;  // tiles of this matrix that come before
 };
-template <class Cfg>
 __device__ __forceinline__ NsUnit ns_unit(const NsParams &p, int u)
 {
     NsUnit t;
@@ -135,12 +132,12 @@ __device__ __forceinline__ NsUnit ns_unit(const NsParams &p, int u)
             t.need += p.sym_tiles;
         }
         t.z = r / p.sym_tiles;
-        const int part = r - t.z * p.sym_tiles, k = part / Cfg::PARTS;  // blocks through the lower triangle row by row
+        const int k = r - t.z * p.sym_tiles;  // through the lower triangle row by row
         int i = static_cast<int>((sqrtf(8.0f * static_cast<float>(k) + 1.0f) - 1.0f) * 0.5f);
         while ((i + 1) * (i + 2) / 2 <= k) ++i;  // the root is off by at most one
         while (i * (i + 1) / 2 > k) --i;
         t.m_blk = i;
-        t.n_blk = (k - i * (i + 1) / 2) * Cfg::PARTS + part % Cfg::PARTS;
+        t.n_blk = k - i * (i + 1) / 2;
     } else {
         t.phase = kNsStep;
         t.need += 2 * p.sym_tiles;
@@ -166,14 +163,13 @@ __device__ __forceinline__ bool ns_b_mn(const NsParams &p, const NsUnit &t, int 
 {
     if (t.phase == kNsGram) return p.R > p.C;
     if (t.phase == kNsStep && p.R <= p.C) return true;  // X's columns
-    return kb * kBlockK / Cfg::EDGE > t.n_blk / Cfg::PARTS;
+    return kb * kBlockK / Cfg::EDGE > t.n_blk;
 }
 
 // Whether both operands are the same rows of the same matrix, as on the diagonal of S and P: they are then fetched once.
-template <class Cfg>
 __device__ __forceinline__ bool ns_same_operand(const NsUnit &t)
 {
-    return Cfg::PARTS == 1 && t.phase != kNsStep && t.m_blk == t.n_blk;
+    return t.phase != kNsStep && t.m_blk == t.n_blk;
 }
 
 // Waits, for a limited time, until `need` tile parts of a matrix are stored.
@@ -231,7 +227,9 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
     const uint32_t tmem_slot = bar0 + 240;
     const uint32_t abort_addr = bar0 + 244;
     const uint32_t epi_abort_addr = bar0 + 248;
-    auto stored_word = [&](int w) { return bar0 + 256u + 4u * w; };  // tiles that epilogue warp w has stored
+    // Tile i's stores are out (one arrival per epilogue warp). Four barriers in turn: a warp arrives for tile i + 3 at the earliest
+    // when all have released the accumulator of tile i + 1, and so are done with tile i.
+    auto stored_bar = [&](uint32_t i) { return bar0 + 256u + 8u * (i & 3u); };
     static_assert(8 * (2 * STAGES + 4) <= 240, "barrier region");
 
     if (warp == 0) {
@@ -242,7 +240,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             ptx::mbar_init(tfull_bar(lane - STAGES), 1);
             ptx::mbar_init(tempty_bar(lane - STAGES), kEpiWarps * CG);
         }
-        if (lane < kEpiWarps) ptx::st_shared_u32_volatile(stored_word(lane), 0);
+        if (lane >= 20 && lane < 24) ptx::mbar_init(stored_bar(static_cast<uint32_t>(lane)), kEpiWarps);
         if (lane == 31) {
             ptx::st_shared_u32_volatile(abort_addr, 0);
             ptx::st_shared_u32_volatile(epi_abort_addr, 0);
@@ -283,7 +281,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             uint32_t phase = 0;
             bool ok = true;
             for (int u = first_unit; u < p.units && ok; u += unit_stride) {
-                const NsUnit t = ns_unit<Cfg>(p, u);
+                const NsUnit t = ns_unit(p, u);
                 const CUtensorMap *x = (t.step & 1) ? &tmX1 : &tmX0;
                 const bool tall = p.R > p.C;
                 const CUtensorMap *mapA = t.phase == kNsGram ? x : t.phase == kNsPoly ? &tmS : tall ? x : &tmP;
@@ -291,10 +289,10 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 const int m0 = t.m_blk * Cfg::EDGE + static_cast<int>(rank) * kBlockM;
                 const int n0 = t.n_blk * BLOCK_N + static_cast<int>(rank) * Cfg::B_ROWS;
                 const int kblocks = t.phase == kNsGram ? p.kb_gram : p.kb_m;
-                const bool same = ns_same_operand<Cfg>(t);
+                const bool same = ns_same_operand(t);
                 ok = ns_wait_done(wctx, status0, p.done + t.z, t.need * CG, 700 + t.phase);
                 if (!ok) break;
-                fence_proxy_async_all();  // the tiles were stored by plain stores
+                fence_proxy_async_global();  // the tiles were stored by plain stores
                 for (int kb = 0; kb < kblocks; ++kb) {
                     ok = wait_barrier(wctx, empty_bar(stage), phase ^ 1u, 100 + stage);
                     if (!ok) break;
@@ -329,9 +327,9 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             uint32_t acc_phase = 0;
             bool ok = true;
             for (int u = first_unit; u < p.units && ok; u += unit_stride) {
-                const NsUnit t = ns_unit<Cfg>(p, u);
+                const NsUnit t = ns_unit(p, u);
                 const int kblocks = t.phase == kNsGram ? p.kb_gram : p.kb_m;
-                const bool same = ns_same_operand<Cfg>(t);
+                const bool same = ns_same_operand(t);
                 ok = wait_barrier(wctx, tempty_bar(acc), acc_phase ^ 1u, 200 + acc);
                 if (!ok) break;
                 ptx::tc_fence_after();
@@ -372,29 +370,16 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
         // ------------------------------------------------------------ count of finished tiles
         // A tile part counts once all epilogue warps have issued their stores of it. The release, which waits for the stores to arrive (about a
         // microsecond), is this warp's business: the epilogue goes on with the next tile meanwhile.
-        uint32_t tile = 0;
-        for (int u = first_unit; u < p.units; u += unit_stride) {
-            const NsUnit t = ns_unit<Cfg>(p, u);
-            if (t.phase == kNsStep && t.step == p.steps - 1) break;  // nobody waits for the results themselves
-            ++tile;
-            bool ok = true;
-            const uint64_t t0 = ptx::globaltimer_ns();
-            for (uint32_t it = 1;; ++it) {
-                const bool here = lane >= kEpiWarps || ptx::ld_shared_u32_volatile(stored_word(lane)) >= tile;
-                if (__all_sync(0xffffffffu, here)) break;
-                if ((it & 63u) == 0) {
-                    const bool gone = ptx::ld_shared_u32_volatile(abort_addr) != 0 || ptx::ld_shared_u32_volatile(epi_abort_addr) != 0 ||
-                                      ptx::globaltimer_ns() - t0 > 3 * p.timeout_ns;  // longer than the others' waits: they report
-                    if (__any_sync(0xffffffffu, gone)) {
-                        ok = false;
-                        break;
-                    }
-                }
+        if (ptx::elect_one()) {
+            const WaitCtx wctx_count{abort_addr, p.status, 3 * p.timeout_ns};
+            uint32_t tile = 0;
+            for (int u = first_unit; u < p.units; u += unit_stride, ++tile) {
+                const NsUnit t = ns_unit(p, u);
+                if (t.phase == kNsStep && t.step == p.steps - 1) break;  // nobody waits for the results themselves
+                if (!wait_barrier(wctx_count, stored_bar(tile), (tile >> 2) & 1u, 800)) break;
+                if (ptx::ld_shared_u32_volatile(epi_abort_addr) != 0) break;
+                red_release_gpu(p.done + t.z, 1);
             }
-            if (!ok) break;
-            __threadfence_block();
-            __syncwarp();
-            if (lane == 0) red_release_gpu(p.done + t.z, 1);
         }
     } else {
         // ------------------------------------------------------------ epilogue (warps 2..9), warp by warp
@@ -414,7 +399,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
         uint32_t acc_phase = 0, tile = 0;
         for (int u = first_unit; u < p.units; u += unit_stride) {
             if (ptx::ld_shared_u32_volatile(epi_abort_addr) != 0) break;
-            const NsUnit t = ns_unit<Cfg>(p, u);
+            const NsUnit t = ns_unit(p, u);
             const int y0 = t.m_blk * Cfg::EDGE + static_cast<int>(rank) * kBlockM + q * 32;  // the warp's first row
             const int x0 = t.n_blk * BLOCK_N + hf * (BLOCK_N / 2);                           // and first column
             const bool poly = t.phase == kNsPoly, last = t.phase == kNsStep && t.step == p.steps - 1;
@@ -517,9 +502,9 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                     if (in_col && in_row(i)) d4[static_cast<long long>(i) * (N / 2) + piece * 8] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
-            __threadfence_block();
             __syncwarp();
-            if (lane == 0 && ok) ptx::st_shared_u32_volatile(stored_word(ew), ++tile);
+            if (lane == 0) ptx::mbar_arrive(stored_bar(tile));
+            ++tile;
             if (++acc == 2) {
                 acc = 0;
                 acc_phase ^= 1u;
