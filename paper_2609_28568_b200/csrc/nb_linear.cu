@@ -1785,14 +1785,22 @@ NormForm norm_form(int64_t C)
     return {512, 2};
 }
 
-// Blocks of a backward pass, by sizes alone so that the workspace is known before the device is: up to two of
-// eight warps on each of 148 SMs.
-int norm_backward_blocks(int64_t BT, int64_t C)
+// The backward pass: a block on each of 148 SMs, of sixteen warps where there are rows enough for as many teams. By sizes alone, so that
+// the workspace is known before the device is.
+NormForm norm_backward_form(int64_t C)
 {
     const NormForm f = norm_form(C);
-    const int64_t teams = f.threads == 32 ? 8 : 1;
-    const int64_t blocks = (BT + teams - 1) / teams, most = f.threads == 512 ? 148 : 296;
-    return static_cast<int>(blocks < most ? blocks : most);
+    return f.threads == 32 || C <= 2048 ? f : NormForm{512, C <= 4096 ? 1 : 2};
+}
+int norm_backward_teams(int64_t BT, int64_t C)
+{
+    const int most = 512 / norm_backward_form(C).threads;
+    return most > 1 && BT <= most / 2 * kNormMaxBlocks ? most / 2 : most;
+}
+int norm_backward_blocks(int64_t BT, int64_t C)
+{
+    const int64_t teams = norm_backward_teams(BT, C), blocks = (BT + teams - 1) / teams;
+    return static_cast<int>(blocks < kNormMaxBlocks ? blocks : kNormMaxBlocks);
 }
 
 template <bool F32, int T, int NV>
@@ -1805,20 +1813,26 @@ int launch_norm_forward(DeviceState &s, const NormForward &p, cudaStream_t strea
 }
 
 template <bool F32, int T, int NV>
-int launch_norm_backward(DeviceState &s, const NormBackward &p, int blocks, cudaStream_t stream)
+int launch_norm_backward(DeviceState &s, NormBackward p, cudaStream_t stream)
 {
-    const size_t smem = T == 32 && p.part ? static_cast<size_t>(p.nvec) * 8 * 64 : 0;  // eight warps' sums
+    constexpr int kMost = 227 * 1024 - 2048;  // of shared memory, beside what the kernel has of its own
     static bool attr_set[kMaxDevices] = {};
     int dev = 0;
     NB_CUDA(cudaGetDevice(&dev));
-    if (T == 32 && !attr_set[dev]) {
-        NB_CUDA(cudaFuncSetAttribute(layernorm_backward_kernel<F32, T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     NV * 32 * 8 * 64));
+    if (!attr_set[dev]) {
+        NB_CUDA(cudaFuncSetAttribute(layernorm_backward_kernel<F32, T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
         attr_set[dev] = true;
     }
-    (void)s;
-    return launch_chained_smem(layernorm_backward_kernel<F32, T, NV>, dim3(static_cast<unsigned>(blocks)), kNormThreads<T>, smem,
-                               stream, p);
+    int teams = norm_backward_teams(p.BT, 8ll * p.nvec);
+    const int row = norm_row_bytes(F32, p.nvec, p.dres != nullptr);
+    if (teams > 1 && 2 * teams * row > kMost) teams /= 2;  // two rows of each team at least
+    const int fit = kMost / (teams * row);
+    p.slots = fit < kNormMaxSlots ? fit : kNormMaxSlots;
+    const int rows = teams * p.slots * row, sums = teams > 1 && p.part ? teams * p.nvec * 64 : 0;  // one after the other in the same memory
+    p.status = s.status;
+    p.timeout_ns = kDefaultTimeoutNs;
+    return launch_chained_smem(layernorm_backward_kernel<F32, T, NV>, dim3(static_cast<unsigned>(norm_backward_blocks(p.BT, 8ll * p.nvec))),
+                               T * teams, static_cast<size_t>(rows > sums ? rows : sums), stream, p);
 }
 
 template <int V>
@@ -1836,7 +1850,7 @@ int with_norm_form(const NormForm &f, F &&fn)
         }
     }
     if (f.threads == 256) return f.nv == 1 ? fn(IntC<256>{}, IntC<1>{}) : fn(IntC<256>{}, IntC<2>{});
-    return fn(IntC<512>{}, IntC<2>{});
+    return f.nv == 1 ? fn(IntC<512>{}, IntC<1>{}) : fn(IntC<512>{}, IntC<2>{});
 }
 
 // ----------------------------------------------------------------------------- orthogonalised momentum
@@ -2606,14 +2620,14 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
     p.nvec = static_cast<int>(C / 8);
     p.inv_c = static_cast<float>(1.0 / static_cast<double>(C));
     const int blocks = norm_backward_blocks(BT, C);
-    rc = with_norm_form(norm_form(C), [&](auto T, auto NV) {
-        return stream_dtype == NB_DTYPE_F32 ? launch_norm_backward<true, T.value, NV.value>(*s, p, blocks, stream)
-                                            : launch_norm_backward<false, T.value, NV.value>(*s, p, blocks, stream);
+    rc = with_norm_form(norm_backward_form(C), [&](auto T, auto NV) {
+        return stream_dtype == NB_DTYPE_F32 ? launch_norm_backward<true, T.value, NV.value>(*s, p, stream)
+                                            : launch_norm_backward<false, T.value, NV.value>(*s, p, stream);
     });
     if (rc != NB_OK) return rc;
     ++g_launches;
     if (!grads) return NB_OK;
-    rc = launch_chained(layernorm_reduce_kernel, dim3(static_cast<unsigned>((2 * C + 31) / 32)), 256, stream,
+    rc = launch_chained(layernorm_reduce_kernel, dim3(static_cast<unsigned>((2 * C + 31) / 32)), 1024, stream,
                         static_cast<float *>(dweight), static_cast<float *>(dbias), static_cast<const float *>(p.part), blocks,
                         static_cast<int>(C), accumulate);
     if (rc != NB_OK) return rc;

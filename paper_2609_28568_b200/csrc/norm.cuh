@@ -29,43 +29,81 @@ __device__ __forceinline__ Raw8<F32> load8(const void *base, long long vec)
     if constexpr (F32) r.q[1] = ptx::ld_global_v4(p + 1);
     return r;
 }
-__device__ __forceinline__ void unpack_bf16(const uint4 &q, float (&v)[8])
+// Eight values as four packed pairs: these kernels are short of instructions before they are short of bandwidth (one value at a
+// time the forward took 526 per warp and row of 768, the backward 760, at half an instruction per cycle and scheduler).
+struct Pairs {
+    ptx::f2 v[4];
+};
+__device__ __forceinline__ Pairs unpack_bf16(const uint4 &q)
 {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    Pairs r;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        v[2 * k] = ptx::bf16_lo(w[k]);
-        v[2 * k + 1] = ptx::bf16_hi(w[k]);
-    }
+    for (int k = 0; k < 4; ++k) r.v[k] = ptx::make_f2_bits(w[k] << 16, w[k] & 0xffff0000u);
+    return r;
 }
 template <bool F32>
-__device__ __forceinline__ void unpack8(const Raw8<F32> &r, float (&v)[8])
+__device__ __forceinline__ Pairs unpack8(const Raw8<F32> &q)
 {
     if constexpr (F32) {
-        const uint32_t w[8] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w, r.q[1].x, r.q[1].y, r.q[1].z, r.q[1].w};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
+        Pairs r;
+        r.v[0] = ptx::make_f2_bits(q.q[0].x, q.q[0].y);
+        r.v[1] = ptx::make_f2_bits(q.q[0].z, q.q[0].w);
+        r.v[2] = ptx::make_f2_bits(q.q[1].x, q.q[1].y);
+        r.v[3] = ptx::make_f2_bits(q.q[1].z, q.q[1].w);
+        return r;
     } else {
-        unpack_bf16(r.q[0], v);
+        return unpack_bf16(q.q[0]);
     }
 }
-__device__ __forceinline__ uint4 pack_bf16(const float (&v)[8])
+__device__ __forceinline__ uint4 pack_bf16(const Pairs &a)
 {
-    return make_uint4(ptx::pack_bf16x2(v[0], v[1]), ptx::pack_bf16x2(v[2], v[3]), ptx::pack_bf16x2(v[4], v[5]),
-                      ptx::pack_bf16x2(v[6], v[7]));
+    return make_uint4(pack_f2_bf16x2(a.v[0]), pack_f2_bf16x2(a.v[1]), pack_f2_bf16x2(a.v[2]), pack_f2_bf16x2(a.v[3]));
 }
 template <bool F32>
-__device__ __forceinline__ Raw8<F32> pack8(const float (&v)[8])
+__device__ __forceinline__ Raw8<F32> pack8(const Pairs &a)
 {
     Raw8<F32> r;
     if constexpr (F32) {
-        r.q[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        r.q[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ptx::split_f2(a.v[k], f[2 * k], f[2 * k + 1]);
+        r.q[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        r.q[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
     } else {
-        r.q[0] = pack_bf16(v);
+        r.q[0] = pack_bf16(a);
     }
     return r;
 }
+// Stream + branch, rounded to the stream's type. bf16: the packed addition, whose one rounding is that of the fp32 sum rounded to bf16 (the
+// fp32 sum is inexact only where one addend is below 2^-16 of the other, and both then round to that other).
+template <bool F32>
+__device__ __forceinline__ Raw8<F32> add_branch(const Raw8<F32> &x, const uint4 &b)
+{
+    if constexpr (F32) {
+        Pairs s = unpack8<true>(x);
+        const Pairs a = unpack_bf16(b);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s.v[k] = ptx::add2(s.v[k], a.v[k]);
+        return pack8<true>(s);
+    } else {
+        Raw8<F32> r;
+        auto add = [](uint32_t u, uint32_t v) {
+            uint32_t w;
+            asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(w) : "r"(u), "r"(v));
+            return w;
+        };
+        r.q[0] = make_uint4(add(x.q[0].x, b.x), add(x.q[0].y, b.y), add(x.q[0].z, b.z), add(x.q[0].w, b.w));
+        return r;
+    }
+}
+__device__ __forceinline__ float sum2(ptx::f2 a)
+{
+    float lo, hi;
+    ptx::split_f2(a, lo, hi);
+    return lo + hi;
+}
+__device__ __forceinline__ ptx::f2 both(float a) { return ptx::make_f2(a, a); }
 template <bool F32>
 __device__ __forceinline__ void store8(void *base, long long vec, const Raw8<F32> &r)
 {
@@ -74,14 +112,29 @@ __device__ __forceinline__ void store8(void *base, long long vec, const Raw8<F32
     if constexpr (F32) p[1] = r.q[1];
 }
 
+// Consecutive bytes into shared memory, counted on an mbarrier. Both addresses and the size are multiples of 16.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
 // Threads of a block: eight teams of a warp, or one team.
 template <int T>
 constexpr int kNormThreads = T == 32 ? 256 : T;
 
+template <int T>
+__device__ __forceinline__ void team_sync(int team)
+{
+    if (T == 32) __syncwarp();
+    else ptx::named_bar_sync(1u + static_cast<uint32_t>(team), T);
+}
+
 // Sums two values over the team; every thread gets both sums, added in the same order on every call. Teams of several warps meet at ONE
 // barrier: the slots alternate by `turn`, so a slot is rewritten only after the barrier behind its last read.
 template <int T>
-__device__ __forceinline__ float2 team_sum(float2 v, float2 (*slots)[T / 32], int turn)
+__device__ __forceinline__ float2 team_sum(float2 v, float2 (*slots)[T / 32], int turn, int team)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -90,8 +143,8 @@ __device__ __forceinline__ float2 team_sum(float2 v, float2 (*slots)[T / 32], in
     }
     if constexpr (T > 32) {
         float2 *s = slots[turn & 1];
-        if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-        __syncthreads();
+        if ((threadIdx.x & 31) == 0) s[threadIdx.x % T / 32] = v;
+        team_sync<T>(team);
         v = s[0];
 #pragma unroll
         for (int i = 1; i < T / 32; ++i) {
@@ -152,44 +205,40 @@ layernorm_forward_kernel(const NormForward p)
     }
     int turn = 0;
     for (; row < p.BT; row += stride) {
-        float v[NV][8];
-        float sum = 0.0f;
+        Pairs v[NV];
+        ptx::f2 sum = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            unpack8<F32>(x[i], v[i]);
             if (has_branch) {
-                float a[8];
-                unpack_bf16(br[i], a);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[i][k] += a[k];
-                const Raw8<F32> s = pack8<F32>(v[i]);
-                if (t + i * T < p.nvec) store8<F32>(p.sum, row * p.nvec + t + i * T, s);
-                unpack8<F32>(s, v[i]);  // the norm is that of the stored sum
+                x[i] = add_branch<F32>(x[i], br[i]);
+                if (t + i * T < p.nvec) store8<F32>(p.sum, row * p.nvec + t + i * T, x[i]);
             }
-            sum += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
+            v[i] = unpack8<F32>(x[i]);  // the norm is that of the stored sum
+            sum = ptx::add2(sum, ptx::add2(ptx::add2(v[i].v[0], v[i].v[1]), ptx::add2(v[i].v[2], v[i].v[3])));
         }
         if (row + stride < p.BT) load(row + stride);
-        const float mean = team_sum<T>(make_float2(sum, 0.0f), slots, turn++).x * p.inv_c;
-        float sq = 0.0f;
+        const float mean = team_sum<T>(make_float2(sum2(sum), 0.0f), slots, turn++, 0).x * p.inv_c;
+        const ptx::f2 minus = both(-mean);
+        ptx::f2 sq = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (t + i * T >= p.nvec) continue;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[i][k] -= mean;
-                sq = fmaf(v[i][k], v[i][k], sq);
+            for (int k = 0; k < 4; ++k) {
+                v[i].v[k] = ptx::add2(v[i].v[k], minus);
+                sq = ptx::fma2(v[i].v[k], v[i].v[k], sq);
             }
         }
-        const float var = team_sum<T>(make_float2(sq, 0.0f), slots, turn++).x * p.inv_c;
+        const float var = team_sum<T>(make_float2(sum2(sq), 0.0f), slots, turn++, 0).x * p.inv_c;
         const float rstd = 1.0f / sqrtf(var + p.eps);
+        const ptx::f2 rs = both(rstd);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (t + i * T >= p.nvec) continue;
-            float wf[8], bf[8], o[8];
-            unpack_bf16(w[i], wf);
-            unpack_bf16(b[i], bf);
+            const Pairs wf = unpack_bf16(w[i]), bf = unpack_bf16(b[i]);
+            Pairs o;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = fmaf(v[i][k] * rstd, wf[k], bf[k]);
+            for (int k = 0; k < 4; ++k) o.v[k] = ptx::fma2(ptx::mul2(v[i].v[k], rs), wf.v[k], bf.v[k]);
             static_cast<uint4 *>(p.out)[row * p.nvec + t + i * T] = pack_bf16(o);
         }
         if (t == 0 && p.mean) {
@@ -210,111 +259,157 @@ struct NormBackward {
     const void *weight;   // bf16
     long long BT;
     int nvec;
+    int slots;            // rows that a team has in shared memory
     float inv_c;
+    int *status;
+    unsigned long long timeout_ns;
 };
 
+// Shared memory of a row of the backward pass: dout, inp, dres (if there is one).
+__host__ __device__ constexpr int norm_row_bytes(bool f32, int nvec, bool has_res) { return nvec * (16 + (f32 ? 32 : 16) * (has_res ? 2 : 1)); }
+constexpr int kNormMaxSlots = 4;
+
+// Rows come into shared memory by bulk copies, several per team under way, and are read twice from there: once for the two sums of the row and for the
+// columns' sums, which stay in registers, and once for dinp. Held in registers instead, with the next row's loads, a row of 768 took 218 of
+// them, one block of eight warps fitted an SM, and 16384 rows took 28.7 us.
 template <bool F32, int T, int NV>
-__global__ void __launch_bounds__(kNormThreads<T>)
+__global__ void __launch_bounds__(512, 1)
 layernorm_backward_kernel(const NormBackward p)
 {
-    extern __shared__ float4 norm_smem[];  // T == 32: the warps' sums, [8][2 C]
-    __shared__ float2 slots[2][T / 32];
-    chained_start();
+    extern __shared__ __align__(128) uint8_t norm_smem[];  // the teams' rows; then, of several teams, their sums [teams][2 C]
+    __shared__ __align__(8) unsigned long long bars[512 / T * kNormMaxSlots];
+    __shared__ float2 sums[512 / T][2][T / 32];
+    __shared__ uint32_t abort_flag;
     const int t = static_cast<int>(threadIdx.x) % T;
-    constexpr int TEAMS = kNormThreads<T> / T;
-    const long long stride = static_cast<long long>(gridDim.x) * TEAMS;
-    long long row = static_cast<long long>(blockIdx.x) * TEAMS + threadIdx.x / T;
+    const int team = threadIdx.x / T, teams = static_cast<int>(blockDim.x) / T;
     const bool has_res = p.dres != nullptr;
-    uint4 dy[NV], w[NV];
-    Raw8<F32> x[NV], res[NV];
-    float mean = 0.0f, rstd = 0.0f;
-    float dw[NV][8], db[NV][8];
-    auto load = [&](long long r) {
-        mean = __ldcg(p.mean + r);
-        rstd = __ldcg(p.rstd + r);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = t + i * T;
-            if (j < p.nvec) {
-                dy[i] = ptx::ld_global_v4(static_cast<const uint4 *>(p.dout) + r * p.nvec + j);
-                x[i] = load8<F32>(p.inp, r * p.nvec + j);
-                if (has_res) res[i] = load8<F32>(p.dres, r * p.nvec + j);
-            }
-        }
+    const uint32_t row_bytes = static_cast<uint32_t>(norm_row_bytes(F32, p.nvec, has_res));
+    const uint32_t ring = ptx::smem_u32(norm_smem) + static_cast<uint32_t>(team * p.slots) * row_bytes;
+    const uint32_t bar = ptx::smem_u32(bars) + 8u * static_cast<uint32_t>(team * kNormMaxSlots);
+    if (t < p.slots) ptx::mbar_init(bar + 8u * t, 1);
+    if (threadIdx.x == 0) abort_flag = 0;
+    ptx::fence_barrier_init();
+    __syncthreads();
+    chained_start();
+    const WaitCtx wctx{ptx::smem_u32(&abort_flag), p.status, p.timeout_ns};
+    const uint32_t dout_bytes = static_cast<uint32_t>(p.nvec) * 16u, x_bytes = dout_bytes * (F32 ? 2u : 1u);
+
+    const long long stride = static_cast<long long>(gridDim.x) * teams;
+    const long long first = static_cast<long long>(blockIdx.x) * teams + team;
+    auto fetch = [&](long long row, int slot) {  // one thread of the team
+        const uint32_t dst = ring + static_cast<uint32_t>(slot) * row_bytes, b = bar + 8u * slot;
+        ptx::mbar_expect_tx(b, row_bytes);
+        bulk_load(dst, static_cast<const uint8_t *>(p.dout) + row * dout_bytes, dout_bytes, b);
+        bulk_load(dst + dout_bytes, static_cast<const uint8_t *>(p.inp) + row * x_bytes, x_bytes, b);
+        if (has_res) bulk_load(dst + dout_bytes + x_bytes, static_cast<const uint8_t *>(p.dres) + row * x_bytes, x_bytes, b);
     };
+    if (t == 0)
+        for (int i = 0; i < p.slots && first + i * stride < p.BT; ++i) fetch(first + i * stride, i);
+
+    uint4 w[NV];
+    Pairs dw[NV], db[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        dy[i] = w[i] = make_uint4(0, 0, 0, 0);
-        x[i] = res[i] = Raw8<F32>{};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) dw[i][k] = db[i][k] = 0.0f;
-    }
-    if (row < p.BT) load(row);
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
+        w[i] = make_uint4(0, 0, 0, 0);
         if (t + i * T < p.nvec) w[i] = ptx::ld_global_v4(static_cast<const uint4 *>(p.weight) + t + i * T);
-    int turn = 0;
-    for (; row < p.BT; row += stride) {
-        float xh[NV][8], g[NV][8];
-        float2 s = make_float2(0.0f, 0.0f);
-        const float rs = rstd;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float wf[8], d[8];
-            unpack8<F32>(x[i], xh[i]);
-            unpack_bf16(dy[i], d);
-            unpack_bf16(w[i], wf);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                xh[i][k] = (xh[i][k] - mean) * rs;
-                g[i][k] = d[k] * wf[k];
-                // vectors past the end of the row: d = 0 and g = 0, so they add nothing to any sum
-                dw[i][k] = fmaf(d[k], xh[i][k], dw[i][k]);
-                db[i][k] += d[k];
-                s.x += g[i][k];
-                s.y = fmaf(g[i][k], xh[i][k], s.y);
-            }
+        for (int k = 0; k < 4; ++k) dw[i].v[k] = db[i].v[k] = both(0.0f);
+    }
+    float mean = 0.0f, rstd = 0.0f;
+    if (first < p.BT) {
+        mean = __ldcg(p.mean + first);
+        rstd = __ldcg(p.rstd + first);
+    }
+    int slot = 0, turn = 0;
+    uint32_t phase = 0;
+    for (long long row = first; row < p.BT; row += stride) {
+        const float mu = mean, rs = rstd;
+        if (row + stride < p.BT) {
+            mean = __ldcg(p.mean + row + stride);
+            rstd = __ldcg(p.rstd + row + stride);
         }
-        Raw8<F32> cur[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) cur[i] = res[i];
-        if (row + stride < p.BT) load(row + stride);
-        s = team_sum<T>(s, slots, turn++);
-        const float c1 = s.x * p.inv_c, c2 = s.y * p.inv_c;
+        const bool ok = wait_barrier(wctx, bar + 8u * slot, phase, 810);
+        const uint32_t src = ring + static_cast<uint32_t>(slot) * row_bytes;
+        auto shared8 = [&](uint32_t at, int j, bool wide) {  // eight elements of a tensor in the slot
+            Raw8<F32> r;
+            ptx::ld_shared_v4(at + static_cast<uint32_t>(j) * (wide ? 32u : 16u), r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w);
+            if constexpr (F32)
+                if (wide) ptx::ld_shared_v4(at + static_cast<uint32_t>(j) * 32u + 16u, r.q[1].x, r.q[1].y, r.q[1].z, r.q[1].w);
+            return r;
+        };
+        const ptx::f2 minus = both(-mu), rs2 = both(rs);
+        ptx::f2 s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int j = t + i * T;
             if (j >= p.nvec) continue;
-            float o[8];
-            unpack8<F32>(cur[i], o);
+            const Pairs d = unpack_bf16(shared8(src, j, false).q[0]), x = unpack8<F32>(shared8(src + dout_bytes, j, F32)),
+                        wf = unpack_bf16(w[i]);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float dx = rs * (g[i][k] - c1 - xh[i][k] * c2);
-                o[k] = has_res ? dx + o[k] : dx;
+            for (int k = 0; k < 4; ++k) {
+                const ptx::f2 xh = ptx::mul2(ptx::add2(x.v[k], minus), rs2), g = ptx::mul2(d.v[k], wf.v[k]);
+                dw[i].v[k] = ptx::fma2(d.v[k], xh, dw[i].v[k]);
+                db[i].v[k] = ptx::add2(db[i].v[k], d.v[k]);
+                s1 = ptx::add2(s1, g);
+                s2 = ptx::fma2(g, xh, s2);
             }
-            store8<F32>(p.dinp, row * p.nvec + j, pack8<F32>(o));
-            if (p.dbranch) static_cast<uint4 *>(p.dbranch)[row * p.nvec + j] = pack_bf16(o);
+        }
+        const float2 s = team_sum<T>(make_float2(sum2(s1), sum2(s2)), sums[team], turn++, team);
+        const ptx::f2 c1 = both(-(s.x * p.inv_c)), c2 = both(-(s.y * p.inv_c));
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = t + i * T;
+            if (j >= p.nvec) continue;
+            const Pairs d = unpack_bf16(shared8(src, j, false).q[0]), x = unpack8<F32>(shared8(src + dout_bytes, j, F32)),
+                        wf = unpack_bf16(w[i]);
+            Pairs o;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const ptx::f2 xh = ptx::mul2(ptx::add2(x.v[k], minus), rs2);
+                o.v[k] = ptx::fma2(xh, c2, ptx::fma2(d.v[k], wf.v[k], c1));
+            }
+            if (has_res) {
+                const Pairs res = unpack8<F32>(shared8(src + dout_bytes + x_bytes, j, F32));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o.v[k] = ptx::fma2(o.v[k], rs2, res.v[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o.v[k] = ptx::mul2(o.v[k], rs2);
+            }
+            if (ok) {
+                store8<F32>(p.dinp, row * p.nvec + j, pack8<F32>(o));
+                if (p.dbranch) static_cast<uint4 *>(p.dbranch)[row * p.nvec + j] = pack_bf16(o);
+            }
+        }
+        team_sync<T>(team);  // the slot has been read
+        if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, slot);
+        if (++slot == p.slots) {
+            slot = 0;
+            phase ^= 1u;
         }
     }
     if (p.part == nullptr) return;
+    __syncthreads();  // every row has been read: the same memory holds the sums now
     float4 *part = reinterpret_cast<float4 *>(p.part) + static_cast<long long>(blockIdx.x) * 4 * p.nvec;
-    float4 *mine = T == 32 ? norm_smem + (threadIdx.x / 32) * 4 * p.nvec : part;
+    float4 *mine = teams > 1 ? reinterpret_cast<float4 *>(norm_smem) + team * 4 * p.nvec : part;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int j = t + i * T;
         if (j >= p.nvec) continue;
-        mine[2 * j] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
-        mine[2 * j + 1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
-        mine[2 * p.nvec + 2 * j] = make_float4(db[i][0], db[i][1], db[i][2], db[i][3]);
-        mine[2 * p.nvec + 2 * j + 1] = make_float4(db[i][4], db[i][5], db[i][6], db[i][7]);
+        const Raw8<true> a = pack8<true>(dw[i]), b = pack8<true>(db[i]);
+        uint4 *m = reinterpret_cast<uint4 *>(mine);
+        m[2 * j] = a.q[0];
+        m[2 * j + 1] = a.q[1];
+        m[2 * p.nvec + 2 * j] = b.q[0];
+        m[2 * p.nvec + 2 * j + 1] = b.q[1];
     }
-    if constexpr (T == 32) {
+    if (teams > 1) {
         __syncthreads();
-        for (int c = threadIdx.x; c < 4 * p.nvec; c += 256) {
-            float4 a = norm_smem[c];
-#pragma unroll
-            for (int k = 1; k < 8; ++k) {
-                const float4 v = norm_smem[k * 4 * p.nvec + c];
+        for (int c = threadIdx.x; c < 4 * p.nvec; c += blockDim.x) {
+            const float4 *all = reinterpret_cast<const float4 *>(norm_smem);
+            float4 a = all[c];
+            for (int k = 1; k < teams; ++k) {
+                const float4 v = all[k * 4 * p.nvec + c];
                 a.x += v.x;
                 a.y += v.y;
                 a.z += v.z;
@@ -326,32 +421,35 @@ layernorm_backward_kernel(const NormBackward p)
 }
 
 // dweight[c] (+)= sum over the blocks' sums, dbias likewise, in a fixed order: results do not depend on which block ended
-// first. A block owns 32 columns of [dweight | dbias], a warp every eighth part; they meet in shared memory.
-__global__ void __launch_bounds__(256)
+// first. A block owns 32 columns of [dweight | dbias], a warp every 32nd part (at most five, loaded at once); they meet in shared memory.
+constexpr int kNormMaxBlocks = 148;
+__global__ void __launch_bounds__(1024)
 layernorm_reduce_kernel(float *dweight, float *dbias, const float *part, int parts, int C, int accumulate)
 {
-    __shared__ float s[8][32];
+    __shared__ float s[32][33];
     chained_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
-    float a = 0.0f;
-    if (c < 2 * C) {
-        int k = warp;
-        for (; k + 24 < parts; k += 32) {
-            float v[4];
+    float v[(kNormMaxBlocks + 31) / 32];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __ldcg(part + (k + 8ll * i) * 2 * C + c);
-            a += (v[0] + v[1]) + (v[2] + v[3]);
-        }
-        for (; k < parts; k += 8) a += __ldcg(part + static_cast<long long>(k) * 2 * C + c);
+    for (int i = 0; i < (kNormMaxBlocks + 31) / 32; ++i) {
+        const int k = warp + 32 * i;
+        v[i] = c < 2 * C && k < parts ? __ldcg(part + static_cast<long long>(k) * 2 * C + c) : 0.0f;
     }
+    float a = 0.0f;
+#pragma unroll
+    for (int i = 0; i < (kNormMaxBlocks + 31) / 32; ++i) a += v[i];
     s[warp][lane] = a;
     __syncthreads();
-    if (warp == 0 && c < 2 * C) {
-        float *dst = c < C ? dweight + c : dbias + (c - C);
-        if ((c < C ? dweight : dbias) == nullptr) return;
+    // warp w adds column w's 32 values, lane by lane, pairwise
+    a = s[lane][warp];
 #pragma unroll
-        for (int k = 1; k < 8; ++k) a += s[k][lane];
+    for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    const int mine = blockIdx.x * 32 + warp;
+    if (lane == 0 && mine < 2 * C) {
+        float *dst = mine < C ? dweight : dbias;
+        if (dst == nullptr) return;
+        dst += mine < C ? mine : mine - C;
         *dst = accumulate ? *dst + a : a;
     }
 }
