@@ -193,11 +193,12 @@ int get_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t rows, u
     return NB_OK;
 }
 
-// n dense fp16 matrices [rows, cols] one after the other, read as boxes of 64 x 64 of one of them with the 128-byte
-// swizzle. What lies outside a matrix reads as zero.
-int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n, uint64_t rows, uint64_t cols)
+// n dense fp16 matrices [rows, cols] one after the other, in boxes of box_rows x 64 of one of them with the
+// 128-byte swizzle. What lies outside a matrix reads as zero and is not written.
+int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n, uint64_t rows, uint64_t cols,
+                   uint32_t box_rows)
 {
-    TmapKey key{ptr, rows, cols, cols, 64, 64, 2, n};
+    TmapKey key{ptr, rows, cols, cols, 64, box_rows, 2, n};
     auto it = s.tmaps.find(key);
     if (it != s.tmaps.end()) {
         *out = it->second;
@@ -205,7 +206,7 @@ int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n
     }
     cuuint64_t dims[3] = {cols, rows, n};
     cuuint64_t strides[2] = {cols * 2, rows * cols * 2};
-    cuuint32_t box[3] = {64, 64, 1};
+    cuuint32_t box[3] = {64, box_rows, 1};
     cuuint32_t estr[3] = {1, 1, 1};
     alignas(64) CUtensorMap m;
     memset(&m, 0, sizeof(m));
@@ -1920,13 +1921,15 @@ int launch_ns(DeviceState &s, NsParams p, cudaStream_t stream)
     const int clusters = most < max_clusters[dev] ? most : max_clusters[dev];
     cfg.gridDim = dim3(static_cast<unsigned>(clusters * Cfg::CG));
     cfg.numAttrs = 2;
-    CUtensorMap x0, x1, sm, pm;
-    int rc;
-    if ((rc = get_batch_tmap(s, &x0, p.x[0], p.n, p.R, p.C)) != NB_OK) return rc;
-    if ((rc = get_batch_tmap(s, &x1, p.x[1], p.n, p.R, p.C)) != NB_OK) return rc;
-    if ((rc = get_batch_tmap(s, &sm, p.s, p.n, p.m, p.m)) != NB_OK) return rc;
-    if ((rc = get_batch_tmap(s, &pm, p.p, p.n, p.m, p.m)) != NB_OK) return rc;
-    NB_CUDA(cudaLaunchKernelEx(&cfg, newton_schulz_kernel<Cfg>, x0, x1, sm, pm, p));
+    CUtensorMap in[4], out[4];
+    const void *at[4] = {p.x[0], p.x[1], p.s, p.p};
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t rows = i < 2 ? p.R : p.m, cols = i < 2 ? p.C : p.m;
+        int rc;
+        if ((rc = get_batch_tmap(s, &in[i], at[i], p.n, rows, cols, 64)) != NB_OK) return rc;
+        if ((rc = get_batch_tmap(s, &out[i], at[i], p.n, rows, cols, 32)) != NB_OK) return rc;
+    }
+    NB_CUDA(cudaLaunchKernelEx(&cfg, newton_schulz_kernel<Cfg>, in[0], in[1], in[2], in[3], out[0], out[1], out[2], out[3], p));
     ++g_launches;
     return NB_OK;
 }

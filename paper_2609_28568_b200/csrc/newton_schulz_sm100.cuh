@@ -82,6 +82,12 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z)
         : "memory");
 }
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *m, uint32_t src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
     uint32_t r;
@@ -202,6 +208,8 @@ template <class Cfg>
 __global__ void __launch_bounds__(kNsThreads, 1)
 newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_constant__ CUtensorMap tmX1,
                      const __grid_constant__ CUtensorMap tmS, const __grid_constant__ CUtensorMap tmP,
+                     const __grid_constant__ CUtensorMap tmX0out, const __grid_constant__ CUtensorMap tmX1out,
+                     const __grid_constant__ CUtensorMap tmSout, const __grid_constant__ CUtensorMap tmPout,
                      const __grid_constant__ NsParams p)
 {
     constexpr int BLOCK_N = Cfg::BLOCK_N;
@@ -251,6 +259,10 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             ptx::prefetch_tmap(&tmX1);
             ptx::prefetch_tmap(&tmS);
             ptx::prefetch_tmap(&tmP);
+            ptx::prefetch_tmap(&tmX0out);
+            ptx::prefetch_tmap(&tmX1out);
+            ptx::prefetch_tmap(&tmSout);
+            ptx::prefetch_tmap(&tmPout);
         }
         __syncwarp();
     }
@@ -368,8 +380,8 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
         }
     } else if (warp == 10) {
         // ------------------------------------------------------------ count of finished tiles
-        // A tile part counts once all epilogue warps have issued their stores of it. The release, which waits for the stores to arrive (about a
-        // microsecond), is this warp's business: the epilogue goes on with the next tile meanwhile.
+        // A tile part counts once all epilogue warps have seen their copies of it completed. One release per tile, by a warp that has nothing
+        // else to wait for.
         if (ptx::elect_one()) {
             const WaitCtx wctx_count{abort_addr, p.status, 3 * p.timeout_ns};
             uint32_t tile = 0;
@@ -383,9 +395,8 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
         }
     } else {
         // ------------------------------------------------------------ epilogue (warps 2..9), warp by warp
-        // A warp owns 32 rows (its TMEM lane quarter) and half of the tile's columns, in pieces of 64. It turns them in shared memory of its
-        // own and stores whole pieces of rows with plain stores (TMA stores, which had to be waited for before a box was used again, took
-        // 2000 cycles longer per tile).
+        // A warp owns 32 rows (its TMEM lane quarter) and half of the tile's columns, in pieces of 64 with a staging box each, which it
+        // stores by TMA copies of its own.
         const int q = warp & 3;
         const int hf = (warp - 2) >> 2;
         const int ew = warp - 2;
@@ -446,9 +457,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 if (CG == 2) ptx::mbar_arrive_cluster(ptx::mapa(tempty_bar(acc), 0));
                 else ptx::mbar_arrive(tempty_bar(acc));
             }
-            __half *dst = t.phase == kNsGram ? p.s : poly ? p.p : p.x[(t.step + 1) & 1];
-            uint4 *d4 = reinterpret_cast<uint4 *>(dst + at);
-            if (last) d4 = static_cast<uint4 *>(p.out[t.z]) + (at - static_cast<long long>(t.z) * M * N) / 8;
+            const CUtensorMap *out = t.phase == kNsGram ? &tmSout : poly ? &tmPout : (t.step & 1) ? &tmX0out : &tmX1out;
 #pragma unroll
             for (int piece = 0; piece < PIECES; ++piece) {
                 const uint32_t box = mine + piece * Cfg::BOX_BYTES;
@@ -492,7 +501,19 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                         }
                     });
                 }
+                if (!last) {
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (ptx::elect_one()) {
+                        if (ok && y0 < M && x0 + piece * 64 < N) tma_store_3d(out, stg + piece * Cfg::BOX_BYTES, x0 + piece * 64, y0, t.z);
+                        ptx::bulk_commit_group();
+                    }
+                    __syncwarp();
+                    continue;
+                }
+                // The results: whole pieces of the caller's rows, by plain stores.
                 __syncwarp();
+                uint4 *d4 = static_cast<uint4 *>(p.out[t.z]) + (at - static_cast<long long>(t.z) * M * N) / 8;
                 const bool in_col = ok && x0 + piece * 64 + cc * 8 < N;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -502,6 +523,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                     if (in_col && in_row(i)) d4[static_cast<long long>(i) * (N / 2) + piece * 8] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
+            ptx::bulk_wait_group<0>();  // in memory; every lane: only the one that issued copies has any to wait for
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(stored_bar(tile));
             ++tile;
