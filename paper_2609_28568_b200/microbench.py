@@ -10,7 +10,10 @@ bwd_fused_zero (the same from zero instead of accumulating), cast (fp32 -> bf16
 master-weight cast of OC*C elements; reports GB/s), head_ce (head forward with the fused softmax
 statistics, vocabulary OC with the last 47 columns as padding), ce_bwd (dlogits from logits, GB/s),
 ce_bwd_inplace (over the logits),
-lora_fwd / lora_bwd (rank-16 adapter beside a frozen weight; TFLOP/s counts base + adapter flops).
+lora_fwd / lora_bwd (rank-16 adapter beside a frozen weight; TFLOP/s counts base + adapter flops),
+norm / norm_bwd (layer norm of [BT, C] bf16 with the residual add in front of it, and its backward with the stream's gradient;
+GB/s, OC is not used), muon / muon_apply (update of BT matrices [OC, C] by orthogonalised momentum, TFLOP/s of its products with half of
+the symmetric ones; and its application to the master weights, GB/s).
 Prints microseconds per call and TFLOP/s from CUDA events around REPS back-to-back calls.
 
 With the word `energy` after REPS (GEMM kinds only) the call is instead replayed from a CUDA graph for
@@ -117,6 +120,53 @@ def replayed(kind: str, BT: int, C: int, OC: int, chain: int = 0) -> int:
     return 0
 
 
+def timed(call, reps: int) -> float:
+    """Microseconds per call, back to back."""
+    for _ in range(2):
+        call()
+    torch.cuda.synchronize()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record()
+    for _ in range(reps):
+        call()
+    e1.record()
+    torch.cuda.synchronize()
+    nb.nb_check_status()
+    return e0.elapsed_time(e1) * 1e3 / reps
+
+
+def beside_linears(kind: str, BT: int, C: int, OC: int, reps: int) -> int:
+    """The operators next to the linear layers: see the module docstring."""
+    dev, bf, f32 = "cuda", torch.bfloat16, torch.float32
+    if kind.startswith("norm"):
+        x, branch, dout, dres = (synth.normal(1 + i, (BT, C), 1.0, dev) for i in range(4))
+        w, b = synth.normal(5, (C,), 0.2, dev), synth.normal(6, (C,), 0.1, dev)
+        out, total, dinp = (torch.empty((BT, C), dtype=bf, device=dev) for _ in range(3))
+        mean, rstd = (torch.empty(BT, dtype=f32, device=dev) for _ in range(2))
+        dw, db = (torch.zeros(C, dtype=f32, device=dev) for _ in range(2))
+        ws = torch.empty(nb.nb_layernorm_workspace(BT, C), dtype=torch.uint8, device=dev)
+        forward = lambda: nb.nb_layernorm_forward(out, total, mean, rstd, x, branch, w, b, BT, C, 1e-5, nb.DTYPE_BF16)  # noqa: E731
+        forward()
+        us = timed(forward if kind == "norm" else lambda: nb.nb_layernorm_backward(
+            dinp, None, dw, db, dout, dres, total, mean, rstd, w, BT, C, 1, nb.DTYPE_BF16, ws, ws.numel()), reps)
+        print(f"{kind} BT={BT} C={C}: {us:.1f} us/call  {8 * BT * C / us / 1e3:.1f} GB/s")
+        return 0
+    update = [synth.normal(10 + i, (OC, C), 0.03, dev) for i in range(BT)]
+    if kind == "muon_apply":
+        master = [synth.normal(100 + i, (OC, C), 0.02, dev).float() for i in range(BT)]
+        weight = [m.to(bf) for m in master]
+        us = timed(lambda: nb.nb_muon_apply(master, weight, update, BT, OC * C, 0.999, 1e-3), reps)
+        print(f"{kind} n={BT} [{OC}, {C}]: {us:.1f} us/call  {12 * BT * OC * C / us / 1e3:.1f} GB/s")
+        return 0
+    grad, momentum = ([synth.normal(s + i, (OC, C), 1e-3, dev).float() for i in range(BT)] for s in (200, 300))
+    ws = torch.empty(nb.nb_muon_workspace(BT, OC, C), dtype=torch.uint8, device=dev)
+    us = timed(lambda: nb.nb_muon_update(update, momentum, grad, BT, OC, C, 0.95, 1, 5, *nb.MUON_COEFFICIENTS, 1e-7, nb.DTYPE_F32, ws,
+                                         ws.numel()), reps)
+    m, k = min(OC, C), max(OC, C)
+    print(f"{kind} n={BT} [{OC}, {C}]: {us:.1f} us/call  {5 * BT * (3 * m * m * k + m ** 3) / us / 1e6:.1f} TFLOP/s")
+    return 0
+
+
 def main(argv) -> int:
     if len(argv) < 5:
         print(__doc__)
@@ -127,6 +177,8 @@ def main(argv) -> int:
         return replayed(kind, BT, C, OC)
     if len(argv) > 6 and argv[6] == "chain":
         return replayed(kind, BT, C, OC, reps)
+    if kind in ("norm", "norm_bwd", "muon", "muon_apply"):
+        return beside_linears(kind, BT, C, OC, reps)
     dev = "cuda"
     bf, f32 = torch.bfloat16, torch.float32
     inp = synth.normal(1, (BT, C), 1.0, dev)
