@@ -294,7 +294,7 @@ int nb_cast_f32_to_bf16(void *dst, const void *src, int64_t n, void *stream);
  *   weight [in]  [C] bf16;  bias [C] bf16 or NULL (16-byte aligned)
  *   stream_dtype NB_DTYPE_BF16 or NB_DTYPE_F32
  * Statistics, deviations and products are held in fp32; s and out are rounded once each. sum may be inp, and out may be branch.
- * Any other overlap of an output with an input is not allowed.
+ * Any other overlap of an output with another argument is refused.
  * A row with an infinity or a NaN gives NaN in that row alone. BT == 0 does nothing.
  *
  * nb_layernorm_backward, with s, mean and rstd of the forward pass, xh = (s - mean) * rstd and g = dout * weight:
@@ -307,7 +307,7 @@ int nb_cast_f32_to_bf16(void *dst, const void *src, int64_t n, void *stream);
  *   inp     [in]  [BT, C] stream_dtype: s (the forward's sum, or its inp where there was no branch)
  *   workspace     device memory of nb_layernorm_workspace(BT, C) bytes, 16-byte aligned, the caller's: calls that may run at the same
  *                 time (on two streams, in two graphs) take one each. NULL is enough where dweight and dbias are NULL.
- * dinp may be dres, and dbranch may be dout. BT == 0: dinp untouched, dweight and dbias zeroed when accumulate == 0.
+ * dinp may be dres, and dbranch may be dout; any other overlap of an output is refused. BT == 0: dinp untouched, dweight and dbias zeroed when accumulate == 0.
  * nb_layernorm_workspace returns -1 for sizes that the call would refuse.
  */
 #define NB_LAYERNORM_MAX_C 8192
@@ -333,7 +333,7 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
  *   workspace     device memory of nb_muon_workspace(n, R, C) bytes, 128-byte aligned, the caller's: calls that may run at the same time (on
  *                 two streams, in two graphs) take one each. Matrices are worked off 32 at a time; the size grows no further from there.
  * update, momentum and grad are host arrays of n device pointers, each 16-byte aligned and dense; the arrays are read before the call returns.
- * No tensor may be given twice. R and C are multiples of 8 and at most NB_MUON_MAX_DIM, n at most NB_MUON_MAX_N, steps at most 32.
+ * An update or a momentum that overlaps another tensor or the workspace is refused. R and C are multiples of 8 and at most NB_MUON_MAX_DIM, n at most NB_MUON_MAX_N, steps at most 32.
  * m, v and the norm are held in fp32 and more; x, y and the polynomial between the products in fp16 at fixed powers of two, products
  * are accumulated in fp32. Rounding errors grow as small singular values do (485 times in five steps): against 64 bits the update is 1.2e-3 off
  * before its own rounding to bf16 for gradients of full rank (as of training: a few strong directions over noise), 2e-2 where singular values fall off
@@ -354,7 +354,8 @@ int nb_muon_update(void *const *update, void *const *momentum, const void *const
  *     master <- decay * master - step * update;  weight <- bf16(master)
  *   master [i/o] n fp32 tensors;  weight [out] n bf16 tensors, or NULL for none;  update [in] n bf16 tensors
  * The three are host arrays of n device pointers, each 16-byte aligned; the arrays are read before the call returns. With learning rate lr
- * and weight decay wd, decay = 1 - lr * wd and step = lr times the update's scale. n at most NB_MUON_MAX_N. No tensor may be given twice.
+ * and weight decay wd, decay = 1 - lr * wd and step = lr times the update's scale. n at most NB_MUON_MAX_N. A master or a copy that
+ * overlaps another tensor is refused; an update may be given more than once.
  */
 int nb_muon_apply(void *const *master, void *const *weight, const void *const *update, int64_t n,
                   int64_t count, float decay, float step, void *stream);

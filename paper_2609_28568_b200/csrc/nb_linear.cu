@@ -5,6 +5,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdarg>
@@ -1772,6 +1773,31 @@ int run_lora_backward(DeviceState &s, const LoraBwd &l, cudaStream_t stream)
     return want_a ? run_wgrad_f32(s, l.u, l.inp, l.dlora_a, nullptr, BT, r, C, l.accumulate, stream) : NB_OK;
 }
 
+// ----------------------------------------------------------------------------- overlapping arguments
+struct Span {
+    const void *p;
+    int64_t bytes;
+    bool written;
+};
+bool overlap(const Span &a, const Span &b)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && x < y + static_cast<uintptr_t>(b.bytes) && y < x + static_cast<uintptr_t>(a.bytes);
+}
+// Of up to 3 n + 1 spans, in any order: whether one that is written overlaps another. Sorted in place, so that neighbours tell.
+bool any_overlap(Span *v, int64_t n)
+{
+    std::sort(v, v + n, [](const Span &a, const Span &b) { return reinterpret_cast<uintptr_t>(a.p) < reinterpret_cast<uintptr_t>(b.p); });
+    uintptr_t end = 0, written_end = 0;  // of what comes before
+    for (int64_t i = 0; i < n; ++i) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(v[i].p), to = at + static_cast<uintptr_t>(v[i].bytes);
+        if (at < (v[i].written ? end : written_end)) return true;
+        if (to > end) end = to;
+        if (v[i].written && to > written_end) written_end = to;
+    }
+    return false;
+}
+
 // ----------------------------------------------------------------------------- layer norm
 // Threads of a row's team and vectors per thread by the row's length: a warp up to 1024 elements, where its
 // shuffles are all the meeting it needs, a block above.
@@ -2053,6 +2079,19 @@ int check_norm(int64_t BT, int64_t C, int stream_dtype)
                     NB_LAYERNORM_MAX_C);
     if (BT >= (1ll << 31) || BT * C >= (1ll << 40)) return fail(NB_ERR_UNSUPPORTED, "dimension too large");
     return NB_OK;
+}
+
+// Whether an output overlaps another output or an input, other than the two pairs that may be the same tensor.
+bool norm_overlap(const Span *w, int nw, const Span *r, int nr, const void *a, const void *a_in, const void *b, const void *b_in)
+{
+    for (int i = 0; i < nw; ++i) {
+        for (int j = i + 1; j < nw; ++j)
+            if (overlap(w[i], w[j])) return true;
+        for (int j = 0; j < nr; ++j)
+            if (overlap(w[i], r[j]) && !((w[i].p == a && r[j].p == a_in && a == a_in) || (w[i].p == b && r[j].p == b_in && b == b_in)))
+                return true;
+    }
+    return false;
 }
 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -2553,6 +2592,11 @@ int nb_layernorm_forward(void *out, void *sum, void *mean, void *rstd, const voi
     if (!aligned16(out) || !aligned16(sum) || !aligned16(inp) || !aligned16(branch) || !aligned16(weight) || !aligned16(bias) ||
         !aligned4(mean) || !aligned4(rstd))
         return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, mean and rstd 4-byte aligned");
+    const int64_t wide = BT * C * (stream_dtype == NB_DTYPE_F32 ? 4 : 2), narrow = BT * C * 2;
+    const Span w[] = {{out, narrow, true}, {sum, wide, true}, {mean, 4 * BT, true}, {rstd, 4 * BT, true}},
+               r[] = {{inp, wide, false}, {branch, narrow, false}, {weight, 2 * C, false}, {bias, 2 * C, false}};
+    if (norm_overlap(w, 4, r, 4, sum, inp, out, branch))
+        return fail(NB_ERR_INVALID_ARG, "an output overlaps another argument (only sum may be inp, and out may be branch)");
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *s;
     if ((rc = get_state(&s)) != NB_OK) return rc;
@@ -2600,6 +2644,13 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
     if (grads && BT > 0 && (!workspace || workspace_bytes < nb_layernorm_workspace(BT, C)))
         return fail(NB_ERR_INVALID_ARG, "dweight and dbias need a workspace of %lld bytes (nb_layernorm_workspace)",
                     static_cast<long long>(nb_layernorm_workspace(BT, C)));
+    const int64_t wide = BT * C * (stream_dtype == NB_DTYPE_F32 ? 4 : 2), narrow = BT * C * 2;
+    const Span w[] = {{dinp, wide, true}, {dbranch, narrow, true}, {dweight, 4 * C, true}, {dbias, 4 * C, true},
+                      {grads ? workspace : nullptr, nb_layernorm_workspace(BT, C), true}},
+               r[] = {{dout, narrow, false}, {dres, wide, false}, {inp, wide, false}, {mean, 4 * BT, false}, {rstd, 4 * BT, false},
+                      {weight, 2 * C, false}};
+    if (BT > 0 && norm_overlap(w, 5, r, 6, dinp, dres, dbranch, dout))
+        return fail(NB_ERR_INVALID_ARG, "an output overlaps another argument (only dinp may be dres, and dbranch may be dout)");
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *s;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
@@ -2671,6 +2722,15 @@ int nb_muon_update(void *const *update, void *const *momentum, const void *const
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 127u) || workspace_bytes < muon_space(n, R, C).bytes)
         return fail(NB_ERR_INVALID_ARG, "a 128-byte aligned workspace of %lld bytes is needed (nb_muon_workspace)",
                     static_cast<long long>(muon_space(n, R, C).bytes));
+    Span v[3 * NB_MUON_MAX_N + 1];
+    int64_t spans = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        v[spans++] = {update[i], R * C * 2, true};
+        if (momentum) v[spans++] = {momentum[i], R * C * 4, true};
+        v[spans++] = {grad[i], R * C * (grad_dtype == NB_DTYPE_F32 ? 4 : 2), false};
+    }
+    v[spans++] = {workspace, muon_space(n, R, C).bytes, true};
+    if (any_overlap(v, spans)) return fail(NB_ERR_INVALID_ARG, "an update, a momentum or the workspace overlaps another argument");
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *s;
     int rc = get_state(&s);
@@ -2695,6 +2755,14 @@ int nb_muon_apply(void *const *master, void *const *weight, const void *const *u
             return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
     }
     if (n == 0 || count == 0) return NB_OK;
+    Span v[3 * NB_MUON_MAX_N];
+    int64_t spans = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        v[spans++] = {master[i], count * 4, true};
+        if (weight) v[spans++] = {weight[i], count * 2, true};
+        v[spans++] = {update[i], count * 2, false};
+    }
+    if (any_overlap(v, spans)) return fail(NB_ERR_INVALID_ARG, "a master weight or a copy overlaps another argument");
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *s;
     int rc = get_state(&s);

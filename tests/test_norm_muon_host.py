@@ -11,6 +11,11 @@ from norm_reference import norm_backward, norm_forward
 P = 0x10000  # a fake aligned device address: a refused call never touches it
 
 
+def at(i):
+    """The i-th of fake tensors that lie apart."""
+    return P + (i << 20)
+
+
 @pytest.fixture(scope="module")
 def L():
     build.build()
@@ -18,7 +23,7 @@ def L():
 
 
 def test_norm_forward_refusals(L):
-    def call(out=P, total=P, mean=P, rstd=P, inp=P, branch=P, w=P, b=P, BT=4, C=64, eps=1e-5, dtype=nb.DTYPE_BF16):
+    def call(out=at(0), total=at(1), mean=at(2), rstd=at(3), inp=at(4), branch=at(5), w=at(6), b=at(7), BT=4, C=64, eps=1e-5, dtype=nb.DTYPE_BF16):
         return L.nb_layernorm_forward(out, total, mean, rstd, inp, branch, w, b, BT, C, eps, dtype, None)
     bad = nb.NB_ERR_INVALID_ARG
     for kw in (dict(out=None), dict(inp=None), dict(w=None), dict(total=None), dict(branch=None), dict(mean=None), dict(rstd=None),
@@ -26,6 +31,9 @@ def test_norm_forward_refusals(L):
                dict(inp=P + 4), dict(branch=P + 2), dict(w=P + 2), dict(b=P + 2), dict(mean=P + 2), dict(rstd=P + 1)):
         assert call(**kw) == bad, kw
         assert nb.nb_last_error()
+    for kw in (dict(out=at(4)), dict(out=at(1)), dict(total=at(5)), dict(out=at(5) + 16), dict(total=at(4) + 16), dict(mean=at(3) + 8), dict(rstd=at(4) + 32),
+               dict(out=at(6)), dict(total=at(7), branch=at(7))):  # overlaps
+        assert call(**kw) == bad and b"overlap" in L.nb_last_error(), kw
     for kw in (dict(C=12), dict(C=8200), dict(BT=1 << 31), dict(BT=(1 << 31) - 1, C=8192)):
         assert call(**kw) == nb.NB_ERR_UNSUPPORTED, kw
     assert call(BT=0) == nb.NB_OK
@@ -34,14 +42,17 @@ def test_norm_forward_refusals(L):
 def test_norm_backward_refusals(L):
     need = nb.nb_layernorm_workspace(4, 64)
 
-    def call(dinp=P, dbranch=P, dw=P, db=P, dout=P, dres=P, inp=P, mean=P, rstd=P, w=P, BT=4, C=64, acc=0, dtype=nb.DTYPE_F32, ws=P,
-             size=need):
+    def call(dinp=at(0), dbranch=at(1), dw=at(2), db=at(3), dout=at(4), dres=at(5), inp=at(6), mean=at(7), rstd=at(8), w=at(9), BT=4,
+             C=64, acc=0, dtype=nb.DTYPE_F32, ws=at(10), size=need):
         return L.nb_layernorm_backward(dinp, dbranch, dw, db, dout, dres, inp, mean, rstd, w, BT, C, acc, dtype, ws, size, None)
     for kw in (dict(dinp=None), dict(dout=None), dict(inp=None), dict(mean=None), dict(rstd=None), dict(w=None), dict(ws=None),
                dict(size=need - 1), dict(size=0), dict(dw=None, size=0), dict(BT=-4), dict(C=-8), dict(dtype=7), dict(dinp=P + 4), dict(dbranch=P + 2), dict(dw=P + 4),
                dict(db=P + 8), dict(dout=P + 2), dict(dres=P + 4), dict(inp=P + 8), dict(w=P + 2), dict(ws=P + 8), dict(mean=P + 3),
                dict(rstd=P + 2)):
         assert call(**kw) == nb.NB_ERR_INVALID_ARG, kw
+    for kw in (dict(dinp=at(6)), dict(dinp=at(5) + 16), dict(dbranch=at(0)), dict(dbranch=at(5)), dict(dw=at(3) + 16), dict(ws=at(4)), dict(ws=at(2)),
+               dict(dw=at(9))):
+        assert call(**kw) == nb.NB_ERR_INVALID_ARG and b"overlap" in L.nb_last_error(), kw
     for kw in (dict(C=20), dict(C=8200)):
         assert call(**kw) == nb.NB_ERR_UNSUPPORTED, kw
     assert call(BT=0, acc=1) == nb.NB_OK
@@ -65,8 +76,8 @@ def _array(*addresses):
 def test_update_refusals(L):
     need = nb.nb_muon_workspace(2, 64, 128)
 
-    def call(u=_array(P, P + 64), m=_array(P, P + 64), g=_array(P, P + 64), n=2, R=64, C=128, mu=0.95, nesterov=1, steps=5,
-             co=nb.MUON_COEFFICIENTS, eps=1e-7, dtype=nb.DTYPE_F32, ws=P, size=need):
+    def call(u=_array(at(0), at(1)), m=_array(at(2), at(3)), g=_array(at(4), at(5)), n=2, R=64, C=128, mu=0.95, nesterov=1, steps=5,
+             co=nb.MUON_COEFFICIENTS, eps=1e-7, dtype=nb.DTYPE_F32, ws=at(9), size=need):
         return L.nb_muon_update(u, m, g, n, R, C, mu, nesterov, steps, *co, eps, dtype, ws, size, None)
     for kw in (dict(u=None), dict(g=None), dict(n=-1), dict(R=0), dict(C=-8), dict(mu=float("nan")), dict(eps=-1.0), dict(eps=float("nan")),
                dict(steps=-1), dict(steps=33), dict(co=(1.0, float("inf"), 0.0)), dict(dtype=3), dict(ws=None), dict(ws=P + 64),
@@ -76,6 +87,9 @@ def test_update_refusals(L):
         assert nb.nb_last_error()
     for kw in (dict(R=12), dict(C=100), dict(n=1025), dict(R=32776), dict(co=(40.0, 0.0, 0.0)), dict(co=(3.0, 0.0, 0.0)), dict(co=(1.0, 50.0, -50.0))):
         assert call(**kw) == nb.NB_ERR_UNSUPPORTED, kw
+    for kw in (dict(u=_array(at(0), at(0))), dict(u=_array(at(0), at(4))), dict(m=_array(at(2), at(2) + 16)), dict(m=_array(at(4), at(3))),
+               dict(u=_array(at(2) + 1024, at(1))), dict(g=_array(at(9) + 128, at(5))), dict(u=_array(at(9), at(1)))):
+        assert call(**kw) == nb.NB_ERR_INVALID_ARG and b"overlap" in L.nb_last_error(), kw
     assert call(n=0) == nb.NB_OK
     # polynomials in use: they keep [0, 1] near itself
     for co in (nb.MUON_COEFFICIENTS, (2.0, -1.5, 0.5), (1.5, -0.5, 0.0), (1.875, -1.25, 0.375)):
@@ -106,11 +120,14 @@ def test_update_binding_refusals(L):
 
 
 def test_apply_refusals(L):
-    def call(m=_array(P, P + 64), w=_array(P, P + 32), u=_array(P, P + 32), n=2, count=10):
+    def call(m=_array(at(0), at(1)), w=_array(at(2), at(3)), u=_array(at(4), at(5)), n=2, count=10):
         return L.nb_muon_apply(m, w, u, n, count, 0.9, 0.1, None)
     for kw in (dict(m=None), dict(u=None), dict(n=-1), dict(count=-1), dict(m=_array(P, None)), dict(u=_array(None, P)),
                dict(w=_array(P, None)), dict(m=_array(P, P + 4)), dict(u=_array(P + 2, P)), dict(w=_array(P, P + 8))):
         assert call(**kw) == nb.NB_ERR_INVALID_ARG, kw
+    for kw in (dict(m=_array(at(0), at(0))), dict(w=_array(at(2), at(2) + 16)), dict(w=_array(at(0), at(3))), dict(u=_array(at(4), at(1) + 32)),
+               dict(m=_array(at(0), at(0) + 32))):
+        assert call(**kw) == nb.NB_ERR_INVALID_ARG and b"overlap" in L.nb_last_error(), kw
     assert call(n=1025) == nb.NB_ERR_UNSUPPORTED
     assert call(count=1 << 40) == nb.NB_ERR_UNSUPPORTED
     assert call(n=0) == nb.NB_OK and call(count=0) == nb.NB_OK
