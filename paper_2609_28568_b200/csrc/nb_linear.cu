@@ -1800,7 +1800,7 @@ bool any_overlap(Span *v, int64_t n)
 
 // ----------------------------------------------------------------------------- layer norm
 // Threads of a row's team and vectors per thread by the row's length: a warp up to 1024 elements, where its
-// shuffles are all the meeting it needs, a block above.
+// shuffles are all the meeting it needs, four to sixteen warps above.
 struct NormForm {
     int threads, nv;
 };
@@ -1808,58 +1808,57 @@ NormForm norm_form(int64_t C)
 {
     const int nvec = static_cast<int>(C / 8);
     if (nvec <= 128) return {32, (nvec + 31) / 32};
-    if (nvec <= 512) return {256, (nvec + 255) / 256};
-    return {512, 2};
+    if (nvec <= 256) return {128, 2};
+    return {nvec <= 512 ? 256 : 512, 2};
 }
-
-// The backward pass: a block on each of 148 SMs, of sixteen warps where there are rows enough for as many teams. By sizes alone, so that
-// the workspace is known before the device is.
-NormForm norm_backward_form(int64_t C)
+// A block on each of 148 SMs, of sixteen warps where there are rows enough for as many teams. By sizes alone, so that the backward's
+// workspace is known before the device is.
+int norm_teams(int64_t BT, int64_t C)
 {
-    const NormForm f = norm_form(C);
-    return f.threads == 32 || C <= 2048 ? f : NormForm{512, C <= 4096 ? 1 : 2};
-}
-int norm_backward_teams(int64_t BT, int64_t C)
-{
-    const int most = 512 / norm_backward_form(C).threads;
+    const int most = kNormMaxThreads / norm_form(C).threads;
     return most > 1 && BT <= most / 2 * kNormMaxBlocks ? most / 2 : most;
 }
-int norm_backward_blocks(int64_t BT, int64_t C)
+int norm_blocks(int64_t BT, int64_t C)
 {
-    const int64_t teams = norm_backward_teams(BT, C), blocks = (BT + teams - 1) / teams;
+    const int64_t teams = norm_teams(BT, C), blocks = (BT + teams - 1) / teams;
     return static_cast<int>(blocks < kNormMaxBlocks ? blocks : kNormMaxBlocks);
 }
 
-template <bool F32, int T, int NV>
-int launch_norm_forward(DeviceState &s, const NormForward &p, cudaStream_t stream)
-{
-    constexpr int teams = kNormThreads<T> / T;
-    const long long blocks = (p.BT + teams - 1) / teams, most = 8ll * s.num_sms;
-    return launch_chained(layernorm_forward_kernel<F32, T, NV>, dim3(static_cast<unsigned>(blocks < most ? blocks : most)),
-                          kNormThreads<T>, stream, p);
-}
-
-template <bool F32, int T, int NV>
-int launch_norm_backward(DeviceState &s, NormBackward p, cudaStream_t stream)
+// Fills in the ring and launches. `sums`: bytes per team that follow the rows in the same memory.
+template <int T, class P>
+int launch_norm(DeviceState &s, void (*kernel)(P), P p, int row_bytes, int sums, bool (&attr_set)[kMaxDevices], cudaStream_t stream)
 {
     constexpr int kMost = 227 * 1024 - 2048;  // of shared memory, beside what the kernel has of its own
-    static bool attr_set[kMaxDevices] = {};
     int dev = 0;
     NB_CUDA(cudaGetDevice(&dev));
     if (!attr_set[dev]) {
-        NB_CUDA(cudaFuncSetAttribute(layernorm_backward_kernel<F32, T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
+        NB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
         attr_set[dev] = true;
     }
-    int teams = norm_backward_teams(p.BT, 8ll * p.nvec);
-    const int row = norm_row_bytes(F32, p.nvec, p.dres != nullptr);
-    if (teams > 1 && 2 * teams * row > kMost) teams /= 2;  // two rows of each team at least
-    const int fit = kMost / (teams * row);
+    int teams = norm_teams(p.BT, 8ll * p.nvec);
+    if (teams > 1 && 2 * teams * row_bytes > kMost) teams /= 2;  // two rows of each team at least
+    const int fit = kMost / (teams * row_bytes);
     p.slots = fit < kNormMaxSlots ? fit : kNormMaxSlots;
-    const int rows = teams * p.slots * row, sums = teams > 1 && p.part ? teams * p.nvec * 64 : 0;  // one after the other in the same memory
+    const int rows = teams * p.slots * row_bytes;
+    if (teams == 1) sums = 0;
     p.status = s.status;
     p.timeout_ns = kDefaultTimeoutNs;
-    return launch_chained_smem(layernorm_backward_kernel<F32, T, NV>, dim3(static_cast<unsigned>(norm_backward_blocks(p.BT, 8ll * p.nvec))),
-                               T * teams, static_cast<size_t>(rows > sums ? rows : sums), stream, p);
+    return launch_chained_smem(kernel, dim3(static_cast<unsigned>(norm_blocks(p.BT, 8ll * p.nvec))), T * teams,
+                               static_cast<size_t>(rows > teams * sums ? rows : teams * sums), stream, p);
+}
+template <bool F32, int T, int NV>
+int launch_norm_forward(DeviceState &s, const NormForward &p, cudaStream_t stream)
+{
+    static bool attr_set[kMaxDevices] = {};
+    return launch_norm<T>(s, layernorm_forward_kernel<F32, T, NV>, p, norm_forward_row_bytes(F32, p.nvec, p.branch != nullptr), 0,
+                          attr_set, stream);
+}
+template <bool F32, int T, int NV>
+int launch_norm_backward(DeviceState &s, const NormBackward &p, cudaStream_t stream)
+{
+    static bool attr_set[kMaxDevices] = {};
+    return launch_norm<T>(s, layernorm_backward_kernel<F32, T, NV>, p, norm_row_bytes(F32, p.nvec, p.dres != nullptr),
+                          p.part ? p.nvec * 64 : 0, attr_set, stream);
 }
 
 template <int V>
@@ -1876,8 +1875,7 @@ int with_norm_form(const NormForm &f, F &&fn)
             default: return fn(IntC<32>{}, IntC<4>{});
         }
     }
-    if (f.threads == 256) return f.nv == 1 ? fn(IntC<256>{}, IntC<1>{}) : fn(IntC<256>{}, IntC<2>{});
-    return f.nv == 1 ? fn(IntC<512>{}, IntC<1>{}) : fn(IntC<512>{}, IntC<2>{});
+    return f.threads == 128 ? fn(IntC<128>{}, IntC<2>{}) : f.threads == 256 ? fn(IntC<256>{}, IntC<2>{}) : fn(IntC<512>{}, IntC<2>{});
 }
 
 // ----------------------------------------------------------------------------- orthogonalised momentum
@@ -2626,7 +2624,7 @@ int nb_layernorm_forward(void *out, void *sum, void *mean, void *rstd, const voi
 int64_t nb_layernorm_workspace(int64_t BT, int64_t C)
 {
     if (BT < 0 || C <= 0 || C % 8 != 0 || C > NB_LAYERNORM_MAX_C) return -1;
-    return static_cast<int64_t>(norm_backward_blocks(BT, C)) * 2 * C * static_cast<int64_t>(sizeof(float));
+    return static_cast<int64_t>(norm_blocks(BT, C)) * 2 * C * static_cast<int64_t>(sizeof(float));
 }
 
 int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias, const void *dout, const void *dres, const void *inp,
@@ -2673,8 +2671,8 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
     p.BT = BT;
     p.nvec = static_cast<int>(C / 8);
     p.inv_c = static_cast<float>(1.0 / static_cast<double>(C));
-    const int blocks = norm_backward_blocks(BT, C);
-    rc = with_norm_form(norm_backward_form(C), [&](auto T, auto NV) {
+    const int blocks = norm_blocks(BT, C);
+    rc = with_norm_form(norm_form(C), [&](auto T, auto NV) {
         return stream_dtype == NB_DTYPE_F32 ? launch_norm_backward<true, T.value, NV.value>(*s, p, stream)
                                             : launch_norm_backward<false, T.value, NV.value>(*s, p, stream);
     });

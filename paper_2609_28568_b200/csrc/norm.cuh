@@ -6,10 +6,9 @@
 //   xh = (s - mean) rstd    g = dout w    dinp = dres + rstd (g - mean(g) - xh mean(g xh))
 //   dweight = sum over rows of dout xh    dbias = sum over rows of dout
 //
-// A team of T threads owns a row and holds it in registers (NV vectors of eight elements per thread), so the
-// deviations are summed from the mean itself and every tensor crosses the memory bus once: both passes are bound by
-// HBM. Teams walk the rows with the stride of the grid; the next row's loads are issued as soon as this
-// row's have been unpacked. All links of the dependent-launch chain: no read-only loads (ptx::ld_global_*).
+// A team of T threads owns a row (NV vectors of eight elements per thread), so the deviations are summed from the mean itself
+// and every tensor crosses the memory bus once: both passes are bound by HBM. Teams walk the rows with the stride of the
+// grid. All links of the dependent-launch chain: no read-only loads (ptx::ld_global_*).
 #pragma once
 #include "elementwise.cuh"
 
@@ -120,10 +119,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  : "memory");
 }
 
-// Threads of a block: eight teams of a warp, or one team.
-template <int T>
-constexpr int kNormThreads = T == 32 ? 256 : T;
-
 template <int T>
 __device__ __forceinline__ void team_sync(int team)
 {
@@ -155,6 +150,36 @@ __device__ __forceinline__ float2 team_sum(float2 v, float2 (*slots)[T / 32], in
     return v;
 }
 
+constexpr int kNormMaxSlots = 4;
+constexpr int kNormMaxThreads = 512;
+
+// What the passes share: rows come into shared memory by bulk copies, up to kNormMaxSlots per team under way, whatever registers the
+// arithmetic needs. (By loads into registers, with the next row's ahead, a backward row of 768 took 218 registers and one of
+// 1024 forward 158: one block of eight warps on an SM, 28.7 us for 16384 x 768 and 32.7 us for 16384 x 1024.)
+struct NormRing {
+    uint32_t at, bar, row_bytes;
+    int slots, slot;
+    uint32_t phase;
+    __device__ __forceinline__ uint32_t row() const { return at + static_cast<uint32_t>(slot) * row_bytes; }
+    __device__ __forceinline__ uint32_t full() const { return bar + 8u * static_cast<uint32_t>(slot); }
+    __device__ __forceinline__ void next()
+    {
+        if (++slot == slots) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+};
+template <bool F32>
+__device__ __forceinline__ Raw8<F32> shared8(uint32_t base, int vec)
+{
+    Raw8<F32> r;
+    const uint32_t at = base + static_cast<uint32_t>(vec) * (F32 ? 32u : 16u);
+    ptx::ld_shared_v4(at, r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w);
+    if constexpr (F32) ptx::ld_shared_v4(at + 16u, r.q[1].x, r.q[1].y, r.q[1].z, r.q[1].w);
+    return r;
+}
+
 struct NormForward {
     void *out;           // bf16
     void *sum;           // stream's type, or null where there is no branch
@@ -165,35 +190,46 @@ struct NormForward {
     const void *bias;    // bf16, or null
     long long BT;
     int nvec;            // C / 8
+    int slots;           // rows that a team has in shared memory
     float inv_c, eps;
+    int *status;
+    unsigned long long timeout_ns;
 };
+// Shared memory of a row of the forward pass: inp, branch (if there is one).
+__host__ __device__ constexpr int norm_forward_row_bytes(bool f32, int nvec, bool has_branch) { return nvec * ((f32 ? 32 : 16) + (has_branch ? 16 : 0)); }
 
 template <bool F32, int T, int NV>
-__global__ void __launch_bounds__(kNormThreads<T>)
+__global__ void __launch_bounds__(kNormMaxThreads, 1)
 layernorm_forward_kernel(const NormForward p)
 {
-    __shared__ float2 slots[2][T / 32];
-    chained_start();
+    extern __shared__ __align__(128) uint8_t norm_smem[];  // the teams' rows
+    __shared__ __align__(8) unsigned long long bars[kNormMaxThreads / T * kNormMaxSlots];
+    __shared__ float2 sums[kNormMaxThreads / T][2][T / 32];
+    __shared__ uint32_t abort_flag;
     const int t = static_cast<int>(threadIdx.x) % T;
-    constexpr int TEAMS = kNormThreads<T> / T;
-    const long long stride = static_cast<long long>(gridDim.x) * TEAMS;
-    long long row = static_cast<long long>(blockIdx.x) * TEAMS + threadIdx.x / T;
+    const int team = threadIdx.x / T, teams = static_cast<int>(blockDim.x) / T;
     const bool has_branch = p.branch != nullptr;
-    Raw8<F32> x[NV];
-    uint4 br[NV], w[NV], b[NV];
-    auto load = [&](long long r) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = t + i * T;
-            x[i] = Raw8<F32>{};
-            br[i] = make_uint4(0, 0, 0, 0);
-            if (j < p.nvec) {
-                x[i] = load8<F32>(p.inp, r * p.nvec + j);
-                if (has_branch) br[i] = ptx::ld_global_v4(static_cast<const uint4 *>(p.branch) + r * p.nvec + j);
-            }
-        }
+    const uint32_t branch_bytes = static_cast<uint32_t>(p.nvec) * 16u, x_bytes = branch_bytes * (F32 ? 2u : 1u);
+    const uint32_t row_bytes = static_cast<uint32_t>(norm_forward_row_bytes(F32, p.nvec, has_branch));
+    NormRing ring{ptx::smem_u32(norm_smem) + static_cast<uint32_t>(team * p.slots) * row_bytes,
+                  ptx::smem_u32(bars) + 8u * static_cast<uint32_t>(team * kNormMaxSlots), row_bytes, p.slots, 0, 0};
+    if (t < p.slots) ptx::mbar_init(ring.bar + 8u * t, 1);
+    if (threadIdx.x == 0) abort_flag = 0;
+    ptx::fence_barrier_init();
+    __syncthreads();
+    chained_start();
+    const WaitCtx wctx{ptx::smem_u32(&abort_flag), p.status, p.timeout_ns};
+    const long long stride = static_cast<long long>(gridDim.x) * teams;
+    const long long first = static_cast<long long>(blockIdx.x) * teams + team;
+    auto fetch = [&](long long row, int slot) {  // one thread of the team
+        const uint32_t dst = ring.at + static_cast<uint32_t>(slot) * row_bytes, b = ring.bar + 8u * slot;
+        ptx::mbar_expect_tx(b, row_bytes);
+        bulk_load(dst, static_cast<const uint8_t *>(p.inp) + row * x_bytes, x_bytes, b);
+        if (has_branch) bulk_load(dst + x_bytes, static_cast<const uint8_t *>(p.branch) + row * branch_bytes, branch_bytes, b);
     };
-    if (row < p.BT) load(row);
+    if (t == 0)
+        for (int i = 0; i < p.slots && first + i * stride < p.BT; ++i) fetch(first + i * stride, i);
+    uint4 w[NV], b[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int j = t + i * T;
@@ -204,20 +240,28 @@ layernorm_forward_kernel(const NormForward p)
         }
     }
     int turn = 0;
-    for (; row < p.BT; row += stride) {
+    for (long long row = first; row < p.BT; row += stride) {
+        const bool ok = wait_barrier(wctx, ring.full(), ring.phase, 811);
         Pairs v[NV];
         ptx::f2 sum = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+            const int j = t + i * T;
+            v[i] = Pairs{{both(0.0f), both(0.0f), both(0.0f), both(0.0f)}};
+            if (j >= p.nvec) continue;
+            Raw8<F32> x = shared8<F32>(ring.row(), j);
             if (has_branch) {
-                x[i] = add_branch<F32>(x[i], br[i]);
-                if (t + i * T < p.nvec) store8<F32>(p.sum, row * p.nvec + t + i * T, x[i]);
+                x = add_branch<F32>(x, shared8<false>(ring.row() + x_bytes, j).q[0]);
+                if (ok) store8<F32>(p.sum, row * p.nvec + j, x);
             }
-            v[i] = unpack8<F32>(x[i]);  // the norm is that of the stored sum
+            v[i] = unpack8<F32>(x);  // the norm is that of the stored sum
             sum = ptx::add2(sum, ptx::add2(ptx::add2(v[i].v[0], v[i].v[1]), ptx::add2(v[i].v[2], v[i].v[3])));
         }
-        if (row + stride < p.BT) load(row + stride);
-        const float mean = team_sum<T>(make_float2(sum2(sum), 0.0f), slots, turn++, 0).x * p.inv_c;
+        const float mean = team_sum<T>(make_float2(sum2(sum), 0.0f), sums[team], turn++, team).x * p.inv_c;
+        if (T == 32) __syncwarp();
+        // the whole team has read the slot
+        if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, ring.slot);
+        ring.next();
         const ptx::f2 minus = both(-mean);
         ptx::f2 sq = both(0.0f);
 #pragma unroll
@@ -229,9 +273,10 @@ layernorm_forward_kernel(const NormForward p)
                 sq = ptx::fma2(v[i].v[k], v[i].v[k], sq);
             }
         }
-        const float var = team_sum<T>(make_float2(sum2(sq), 0.0f), slots, turn++, 0).x * p.inv_c;
+        const float var = team_sum<T>(make_float2(sum2(sq), 0.0f), sums[team], turn++, team).x * p.inv_c;
         const float rstd = 1.0f / sqrtf(var + p.eps);
         const ptx::f2 rs = both(rstd);
+        if (!ok) continue;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (t + i * T >= p.nvec) continue;
@@ -267,26 +312,23 @@ struct NormBackward {
 
 // Shared memory of a row of the backward pass: dout, inp, dres (if there is one).
 __host__ __device__ constexpr int norm_row_bytes(bool f32, int nvec, bool has_res) { return nvec * (16 + (f32 ? 32 : 16) * (has_res ? 2 : 1)); }
-constexpr int kNormMaxSlots = 4;
 
-// Rows come into shared memory by bulk copies, several per team under way, and are read twice from there: once for the two sums of the row and for the
-// columns' sums, which stay in registers, and once for dinp. Held in registers instead, with the next row's loads, a row of 768 took 218 of
-// them, one block of eight warps fitted an SM, and 16384 rows took 28.7 us.
+// A row is read twice from shared memory: once for its two sums and for the columns' sums, which stay in registers, and once for dinp.
 template <bool F32, int T, int NV>
-__global__ void __launch_bounds__(512, 1)
+__global__ void __launch_bounds__(kNormMaxThreads, 1)
 layernorm_backward_kernel(const NormBackward p)
 {
     extern __shared__ __align__(128) uint8_t norm_smem[];  // the teams' rows; then, of several teams, their sums [teams][2 C]
-    __shared__ __align__(8) unsigned long long bars[512 / T * kNormMaxSlots];
-    __shared__ float2 sums[512 / T][2][T / 32];
+    __shared__ __align__(8) unsigned long long bars[kNormMaxThreads / T * kNormMaxSlots];
+    __shared__ float2 sums[kNormMaxThreads / T][2][T / 32];
     __shared__ uint32_t abort_flag;
     const int t = static_cast<int>(threadIdx.x) % T;
     const int team = threadIdx.x / T, teams = static_cast<int>(blockDim.x) / T;
     const bool has_res = p.dres != nullptr;
     const uint32_t row_bytes = static_cast<uint32_t>(norm_row_bytes(F32, p.nvec, has_res));
-    const uint32_t ring = ptx::smem_u32(norm_smem) + static_cast<uint32_t>(team * p.slots) * row_bytes;
-    const uint32_t bar = ptx::smem_u32(bars) + 8u * static_cast<uint32_t>(team * kNormMaxSlots);
-    if (t < p.slots) ptx::mbar_init(bar + 8u * t, 1);
+    NormRing ring{ptx::smem_u32(norm_smem) + static_cast<uint32_t>(team * p.slots) * row_bytes,
+                  ptx::smem_u32(bars) + 8u * static_cast<uint32_t>(team * kNormMaxSlots), row_bytes, p.slots, 0, 0};
+    if (t < p.slots) ptx::mbar_init(ring.bar + 8u * t, 1);
     if (threadIdx.x == 0) abort_flag = 0;
     ptx::fence_barrier_init();
     __syncthreads();
@@ -297,7 +339,7 @@ layernorm_backward_kernel(const NormBackward p)
     const long long stride = static_cast<long long>(gridDim.x) * teams;
     const long long first = static_cast<long long>(blockIdx.x) * teams + team;
     auto fetch = [&](long long row, int slot) {  // one thread of the team
-        const uint32_t dst = ring + static_cast<uint32_t>(slot) * row_bytes, b = bar + 8u * slot;
+        const uint32_t dst = ring.at + static_cast<uint32_t>(slot) * row_bytes, b = ring.bar + 8u * slot;
         ptx::mbar_expect_tx(b, row_bytes);
         bulk_load(dst, static_cast<const uint8_t *>(p.dout) + row * dout_bytes, dout_bytes, b);
         bulk_load(dst + dout_bytes, static_cast<const uint8_t *>(p.inp) + row * x_bytes, x_bytes, b);
@@ -320,30 +362,22 @@ layernorm_backward_kernel(const NormBackward p)
         mean = __ldcg(p.mean + first);
         rstd = __ldcg(p.rstd + first);
     }
-    int slot = 0, turn = 0;
-    uint32_t phase = 0;
+    int turn = 0;
     for (long long row = first; row < p.BT; row += stride) {
         const float mu = mean, rs = rstd;
         if (row + stride < p.BT) {
             mean = __ldcg(p.mean + row + stride);
             rstd = __ldcg(p.rstd + row + stride);
         }
-        const bool ok = wait_barrier(wctx, bar + 8u * slot, phase, 810);
-        const uint32_t src = ring + static_cast<uint32_t>(slot) * row_bytes;
-        auto shared8 = [&](uint32_t at, int j, bool wide) {  // eight elements of a tensor in the slot
-            Raw8<F32> r;
-            ptx::ld_shared_v4(at + static_cast<uint32_t>(j) * (wide ? 32u : 16u), r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w);
-            if constexpr (F32)
-                if (wide) ptx::ld_shared_v4(at + static_cast<uint32_t>(j) * 32u + 16u, r.q[1].x, r.q[1].y, r.q[1].z, r.q[1].w);
-            return r;
-        };
+        const bool ok = wait_barrier(wctx, ring.full(), ring.phase, 810);
+        const uint32_t src = ring.row();
         const ptx::f2 minus = both(-mu), rs2 = both(rs);
         ptx::f2 s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int j = t + i * T;
             if (j >= p.nvec) continue;
-            const Pairs d = unpack_bf16(shared8(src, j, false).q[0]), x = unpack8<F32>(shared8(src + dout_bytes, j, F32)),
+            const Pairs d = unpack_bf16(shared8<false>(src, j).q[0]), x = unpack8<F32>(shared8<F32>(src + dout_bytes, j)),
                         wf = unpack_bf16(w[i]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -360,7 +394,7 @@ layernorm_backward_kernel(const NormBackward p)
         for (int i = 0; i < NV; ++i) {
             const int j = t + i * T;
             if (j >= p.nvec) continue;
-            const Pairs d = unpack_bf16(shared8(src, j, false).q[0]), x = unpack8<F32>(shared8(src + dout_bytes, j, F32)),
+            const Pairs d = unpack_bf16(shared8<false>(src, j).q[0]), x = unpack8<F32>(shared8<F32>(src + dout_bytes, j)),
                         wf = unpack_bf16(w[i]);
             Pairs o;
 #pragma unroll
@@ -369,7 +403,7 @@ layernorm_backward_kernel(const NormBackward p)
                 o.v[k] = ptx::fma2(xh, c2, ptx::fma2(d.v[k], wf.v[k], c1));
             }
             if (has_res) {
-                const Pairs res = unpack8<F32>(shared8(src + dout_bytes + x_bytes, j, F32));
+                const Pairs res = unpack8<F32>(shared8<F32>(src + dout_bytes + x_bytes, j));
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o.v[k] = ptx::fma2(o.v[k], rs2, res.v[k]);
             } else {
@@ -382,11 +416,8 @@ layernorm_backward_kernel(const NormBackward p)
             }
         }
         team_sync<T>(team);  // the slot has been read
-        if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, slot);
-        if (++slot == p.slots) {
-            slot = 0;
-            phase ^= 1u;
-        }
+        if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, ring.slot);
+        ring.next();
     }
     if (p.part == nullptr) return;
     __syncthreads();  // every row has been read: the same memory holds the sums now
