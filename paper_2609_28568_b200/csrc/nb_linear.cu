@@ -1913,7 +1913,7 @@ int launch_ns(DeviceState &s, NsParams p, cudaStream_t stream)
     int dev = 0;
     NB_CUDA(cudaGetDevice(&dev));
     cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(kNsThreads);
+    cfg.blockDim = dim3(Cfg::THREADS);
     cfg.dynamicSmemBytes = Cfg::SMEM_BYTES;
     cfg.stream = stream;
     cudaLaunchAttribute attrs[2];
@@ -1937,7 +1937,7 @@ int launch_ns(DeviceState &s, NsParams p, cudaStream_t stream)
     const int blocks = (p.m + Cfg::EDGE - 1) / Cfg::EDGE;
     p.tiles_r = (p.R + Cfg::EDGE - 1) / Cfg::EDGE;
     p.sym_tiles = blocks * (blocks + 1) / 2;
-    p.x_tiles = p.tiles_r * ((p.C + Cfg::BLOCK_N - 1) / Cfg::BLOCK_N);
+    p.x_tiles = p.tiles_r * ((p.C + Cfg::EDGE - 1) / Cfg::EDGE);
     const long long units = 1ll * p.steps * p.n * (2 * p.sym_tiles + p.x_tiles);
     if (units >= (1ll << 27)) return fail(NB_ERR_UNSUPPORTED, "tile count out of range");
     p.units = static_cast<int>(units);
@@ -1951,7 +1951,7 @@ int launch_ns(DeviceState &s, NsParams p, cudaStream_t stream)
         const uint64_t rows = i < 2 ? p.R : p.m, cols = i < 2 ? p.C : p.m;
         int rc;
         if ((rc = get_batch_tmap(s, &in[i], at[i], p.n, rows, cols, 64)) != NB_OK) return rc;
-        if ((rc = get_batch_tmap(s, &out[i], at[i], p.n, rows, cols, 32)) != NB_OK) return rc;
+        if ((rc = get_batch_tmap(s, &out[i], at[i], p.n, rows, cols, Cfg::WARP_ROWS)) != NB_OK) return rc;
     }
     NB_CUDA(cudaLaunchKernelEx(&cfg, newton_schulz_kernel<Cfg>, in[0], in[1], in[2], in[3], out[0], out[1], out[2], out[3], p));
     ++g_launches;
@@ -2027,12 +2027,15 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
     for (int i = 0; i < n; ++i) p.out[i] = q.update[at + i];
     p.status = s.status;
     p.timeout_ns = kDefaultTimeoutNs;
-    // Pairs of CTAs on 256 x 256 tiles where X has two of them for every pair, else CTAs on 128 x 128: a phase then ends sooner, at twice the
-    // reads. Measured, us (128, 256): 10 x 768 x 768 (90 tiles of 256) 136, 156; 4 x 3072 x 768 (144) 202, 215; 16 x 768 x 768 (144) 196, 176;
-    // 6 x 2304 x 768 (162) 202, 204; 6 x 3072 x 768 (216) 247, 238; 28 x 1024 x 1024 (448) 779, 599.
-    const int tr = (R + 255) / 256, tc = (C + 255) / 256;
-    if (static_cast<long long>(n) * tr * tc >= s.num_sms) return launch_ns<NsCfg<2>>(s, p, stream);
-    return launch_ns<NsCfg<1>>(s, p, stream);
+    // Pairs of CTAs on 256 x 256 tiles where X has two of them for every pair. Below that the chain of a phase counts, which is shorter with
+    // CTAs on 128 x 128 tiles (at twice the reads), and shorter yet on 64 x 64 (at four times) where these are two per SM at most. Measured, us (64,
+    // 128, 256): 768 x 768 (144 tiles of 64) 86, 97, 130; 12 x 128 x 512 (192) 62, 68, 91; 2 x 768 x 768 (288) 97, 99, 132; 28 x 256 x 256 (448)
+    // 77, 75, 97; 4 x 768 x 768 (576) 150, 106, 135; (128, 256): 4 x 3072 x 768 (144 tiles of 256) 206, 216; 16 x 768 x 768 (144) 199, 177;
+    // 6 x 2304 x 768 (162) 205, 206; 6 x 3072 x 768 (216) 251, 239; 28 x 1024 x 1024 (448) 775, 610.
+    auto tiles = [&](int edge) { return static_cast<long long>(n) * ((R + edge - 1) / edge) * ((C + edge - 1) / edge); };
+    if (tiles(256) >= s.num_sms) return launch_ns<NsCfg<2, 256>>(s, p, stream);
+    if (tiles(64) <= 2 * s.num_sms) return launch_ns<NsCfg<1, 64>>(s, p, stream);
+    return launch_ns<NsCfg<1, 128>>(s, p, stream);
 }
 
 // Whether the polynomial keeps everything within what fp16 holds at its scale: singular values start in [0, 1] and step to

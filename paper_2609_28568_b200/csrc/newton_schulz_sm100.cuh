@@ -13,7 +13,7 @@
 // The work of all steps is one list of tiles, phase by phase (S of every matrix, P of every matrix, X of every matrix, ...), which
 // the CTAs (or CTA pairs) of a cooperative launch walk with the stride of the grid. A matrix's tiles of one phase wait for its tiles of
 // the phase before, counted in global memory; other matrices are not waited for. Inside a CTA it is gemm_kernel's division: warp 0 loads tiles by
-// TMA, warp 1 issues the MMAs into one of two accumulators, warps 2..9 run the epilogue of the tile before. Every operand comes as
+// TMA, warp 1 issues the MMAs into one of two accumulators, the others run the epilogue of the tile before. Every operand comes as
 // boxes of 64 x 64 elements of one matrix of the batch (3-D maps: what lies outside the matrix reads as zero).
 //
 // As fifteen launches (three per step) each phase cost 2.5 us more: the drain and the start of a launch.
@@ -42,27 +42,30 @@ struct NsParams {
     unsigned long long timeout_ns;
 };
 
-constexpr int kNsThreads = kNumThreads + 32;  // and warp 10, which counts finished tiles
-
-template <int CG_>
+template <int CG_, int EDGE_>
 struct NsCfg {
     static constexpr int CG = CG_;
-    static constexpr int EDGE = kBlockM * CG_;  // tiles are square, so those above the diagonal mirror those below
-    static constexpr int BLOCK_N = EDGE;
-    static constexpr uint32_t A_BYTES = kBlockM * kBlockK * 2;
-    static constexpr int B_ROWS = BLOCK_N / CG_;
-    static constexpr uint32_t B_BYTES = B_ROWS * kBlockK * 2;
-    static constexpr int PIECES = BLOCK_N / 128;     // of 64 columns per epilogue warp
-    static constexpr uint32_t BOX_BYTES = 32 * 128;  // a piece in staging: 32 rows of 64 elements
-    static constexpr uint32_t STG_BYTES = kEpiWarps * PIECES * BOX_BYTES;
-    static constexpr int STAGES = static_cast<int>((232448 - 512 - STG_BYTES) / (A_BYTES + B_BYTES)) < 7
-                                      ? static_cast<int>((232448 - 512 - STG_BYTES) / (A_BYTES + B_BYTES)) : 7;
-    static constexpr uint32_t OFF_B = STAGES * A_BYTES;
-    static constexpr uint32_t OFF_STG = STAGES * (A_BYTES + B_BYTES);
+    static constexpr int EDGE = EDGE_;       // tiles are square, so those above the diagonal mirror those below
+    static constexpr int ROWS = EDGE / CG_;  // of either operand in one CTA
+    static constexpr uint32_t OP_BYTES = ROWS * kBlockK * 2;
+    // Epilogue: a warp reads the TMEM lanes of its quarter, which hold a quarter of the CTA's rows (64-row tiles: in the first 16 of 32
+    // lanes), and half of the columns, or all of a 64-column tile, in pieces of 64.
+    static constexpr int EPI_WARPS = EDGE_ == 64 ? 4 : 8;
+    static constexpr int WARP_ROWS = ROWS / 4;
+    static constexpr int WARP_COLS = EDGE_ / (EPI_WARPS / 4);
+    static constexpr int PIECES = WARP_COLS / 64;
+    static constexpr int COUNT_WARP = 2 + EPI_WARPS;  // counts finished tiles
+    static constexpr int THREADS = (3 + EPI_WARPS) * 32;
+    static constexpr uint32_t BOX_BYTES = WARP_ROWS * 128;  // a piece in staging
+    static constexpr uint32_t STG_BYTES = EPI_WARPS * PIECES * BOX_BYTES;
+    static constexpr int FIT = static_cast<int>((232448 - 512 - STG_BYTES) / (2 * OP_BYTES));
+    static constexpr int STAGES = FIT < 12 ? FIT : 12;
+    static constexpr uint32_t OFF_B = STAGES * OP_BYTES;
+    static constexpr uint32_t OFF_STG = 2 * STAGES * OP_BYTES;
     static constexpr uint32_t OFF_BAR = OFF_STG + STG_BYTES;
     static constexpr uint32_t SMEM_BYTES = OFF_BAR + 512;
-    static constexpr uint32_t TMEM_COLS = 2 * BLOCK_N;
-    static_assert(2 * BLOCK_N <= 512, "two accumulators must fit in TMEM");
+    static constexpr uint32_t TMEM_COLS = 2 * EDGE;
+    static_assert((CG_ == 2 && EDGE_ == 256) || (CG_ == 1 && (EDGE_ == 128 || EDGE_ == 64)), "tile");
     static_assert(SMEM_BYTES <= 232448, "shared memory budget");
 };
 
@@ -205,14 +208,13 @@ __device__ __forceinline__ bool ns_wait_done(const WaitCtx &w, int status0, cons
 }
 
 template <class Cfg>
-__global__ void __launch_bounds__(kNsThreads, 1)
+__global__ void __launch_bounds__(Cfg::THREADS, 1)
 newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_constant__ CUtensorMap tmX1,
                      const __grid_constant__ CUtensorMap tmS, const __grid_constant__ CUtensorMap tmP,
                      const __grid_constant__ CUtensorMap tmX0out, const __grid_constant__ CUtensorMap tmX1out,
                      const __grid_constant__ CUtensorMap tmSout, const __grid_constant__ CUtensorMap tmPout,
                      const __grid_constant__ NsParams p)
 {
-    constexpr int BLOCK_N = Cfg::BLOCK_N;
     constexpr int STAGES = Cfg::STAGES;
     constexpr int CG = Cfg::CG;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -246,9 +248,9 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             ptx::mbar_init(empty_bar(lane), 1);
         } else if (lane < STAGES + 2) {
             ptx::mbar_init(tfull_bar(lane - STAGES), 1);
-            ptx::mbar_init(tempty_bar(lane - STAGES), kEpiWarps * CG);
+            ptx::mbar_init(tempty_bar(lane - STAGES), Cfg::EPI_WARPS * CG);
         }
-        if (lane >= 20 && lane < 24) ptx::mbar_init(stored_bar(static_cast<uint32_t>(lane)), kEpiWarps);
+        if (lane >= 20 && lane < 24) ptx::mbar_init(stored_bar(static_cast<uint32_t>(lane)), Cfg::EPI_WARPS);
         if (lane == 31) {
             ptx::st_shared_u32_volatile(abort_addr, 0);
             ptx::st_shared_u32_volatile(epi_abort_addr, 0);
@@ -298,8 +300,8 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 const bool tall = p.R > p.C;
                 const CUtensorMap *mapA = t.phase == kNsGram ? x : t.phase == kNsPoly ? &tmS : tall ? x : &tmP;
                 const CUtensorMap *mapB = t.phase == kNsGram ? x : t.phase == kNsPoly ? &tmS : tall ? &tmP : x;
-                const int m0 = t.m_blk * Cfg::EDGE + static_cast<int>(rank) * kBlockM;
-                const int n0 = t.n_blk * BLOCK_N + static_cast<int>(rank) * Cfg::B_ROWS;
+                const int m0 = t.m_blk * Cfg::EDGE + static_cast<int>(rank) * Cfg::ROWS;
+                const int n0 = t.n_blk * Cfg::EDGE + static_cast<int>(rank) * Cfg::ROWS;
                 const int kblocks = t.phase == kNsGram ? p.kb_gram : p.kb_m;
                 const bool same = ns_same_operand(t);
                 ok = ns_wait_done(wctx, status0, p.done + t.z, t.need * CG, 700 + t.phase);
@@ -309,17 +311,17 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                     ok = wait_barrier(wctx, empty_bar(stage), phase ^ 1u, 100 + stage);
                     if (!ok) break;
                     const uint32_t fb = (CG == 2) ? ptx::mapa(full_bar(stage), 0) : full_bar(stage);
-                    if (rank == 0) ptx::mbar_expect_tx(full_bar(stage), CG * (Cfg::A_BYTES + (same ? 0u : Cfg::B_BYTES)));
-                    const uint32_t sa = smem + stage * Cfg::A_BYTES;
-                    const uint32_t sb = smem + Cfg::OFF_B + stage * Cfg::B_BYTES;
+                    if (rank == 0) ptx::mbar_expect_tx(full_bar(stage), CG * Cfg::OP_BYTES * (same ? 1u : 2u));
+                    const uint32_t sa = smem + stage * Cfg::OP_BYTES;
+                    const uint32_t sb = smem + Cfg::OFF_B + stage * Cfg::OP_BYTES;
                     const int k0 = kb * kBlockK;
                     const bool a_mn = ns_a_mn<Cfg>(p, t, kb), b_mn = ns_b_mn<Cfg>(p, t, kb);
 #pragma unroll
-                    for (int j = 0; j < kBlockM / 64; ++j)
+                    for (int j = 0; j < Cfg::ROWS / 64; ++j)
                         load(sa + j * 8192u, mapA, fb, a_mn ? m0 + j * 64 : k0, a_mn ? k0 : m0 + j * 64, t.z);
                     if (!same)
 #pragma unroll
-                        for (int j = 0; j < Cfg::B_ROWS / 64; ++j)
+                        for (int j = 0; j < Cfg::ROWS / 64; ++j)
                             load(sb + j * 8192u, mapB, fb, b_mn ? n0 + j * 64 : k0, b_mn ? k0 : n0 + j * 64, t.z);
                     if (++stage == STAGES) {
                         stage = 0;
@@ -332,7 +334,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
         // ------------------------------------------------------------ MMA issuer (leader CTA only)
         if (rank == 0 && ptx::elect_one()) {
             // bits 7 and 10 clear: both operands fp16
-            constexpr uint32_t idesc0 = make_idesc(Cfg::EDGE, BLOCK_N, false, false) & ~((1u << 7) | (1u << 10));
+            constexpr uint32_t idesc0 = make_idesc(Cfg::EDGE, Cfg::EDGE, false, false) & ~((1u << 7) | (1u << 10));
             int stage = 0;
             uint32_t phase = 0;
             int acc = 0;
@@ -345,13 +347,13 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 ok = wait_barrier(wctx, tempty_bar(acc), acc_phase ^ 1u, 200 + acc);
                 if (!ok) break;
                 ptx::tc_fence_after();
-                const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * BLOCK_N);
+                const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * Cfg::EDGE);
                 for (int kb = 0; kb < kblocks; ++kb) {
                     ok = wait_barrier(wctx, full_bar(stage), phase, 300 + stage);
                     if (!ok) break;
                     ptx::tc_fence_after();
-                    const uint32_t sa = smem + stage * Cfg::A_BYTES;
-                    const uint32_t sb = same ? sa : smem + Cfg::OFF_B + stage * Cfg::B_BYTES;
+                    const uint32_t sa = smem + stage * Cfg::OP_BYTES;
+                    const uint32_t sb = same ? sa : smem + Cfg::OFF_B + stage * Cfg::OP_BYTES;
                     const bool a_mn = ns_a_mn<Cfg>(p, t, kb), b_mn = ns_b_mn<Cfg>(p, t, kb);
                     // K-major: 8-row groups 1024 B apart, 16 k = 32 B inside the swizzle row.
                     // MN-major: 64-wide chunks 8192 B apart, 8-k groups 1024 B apart, 16 k = 2048 B.
@@ -378,7 +380,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 }
             }
         }
-    } else if (warp == 10) {
+    } else if (warp == Cfg::COUNT_WARP) {
         // ------------------------------------------------------------ count of finished tiles
         // A tile part counts once all epilogue warps have seen their copies of it completed. One release per tile, by a warp that has nothing
         // else to wait for.
@@ -394,16 +396,17 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             }
         }
     } else {
-        // ------------------------------------------------------------ epilogue (warps 2..9), warp by warp
-        // A warp owns 32 rows (its TMEM lane quarter) and half of the tile's columns, in pieces of 64 with a staging box each, which it
-        // stores by TMA copies of its own.
+        // ------------------------------------------------------------ epilogue, warp by warp
+        // A warp's pieces have a staging box each, which it stores by TMA copies of its own.
         const int q = warp & 3;
-        const int hf = (warp - 2) >> 2;
         const int ew = warp - 2;
+        const int column = (ew >> 2) * Cfg::WARP_COLS;  // the warp's first, in the tile
+        constexpr int WR = Cfg::WARP_ROWS;
         constexpr int PIECES = Cfg::PIECES;
         const uint32_t stg = smem + Cfg::OFF_STG + static_cast<uint32_t>(ew * PIECES) * Cfg::BOX_BYTES;
         const uint32_t mine = stg + static_cast<uint32_t>(lane) * 128u;  // this lane's row
         const uint32_t sw = static_cast<uint32_t>(lane & 7);
+        const bool has_row = lane < WR;
         const int rr0 = lane >> 3, cc = lane & 7;  // eight lanes to 64 columns of a row where memory is accessed
         const uint32_t flat = stg + static_cast<uint32_t>(rr0) * 128u;
         int acc = 0;
@@ -411,13 +414,13 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
         for (int u = first_unit; u < p.units; u += unit_stride) {
             if (ptx::ld_shared_u32_volatile(epi_abort_addr) != 0) break;
             const NsUnit t = ns_unit(p, u);
-            const int y0 = t.m_blk * Cfg::EDGE + static_cast<int>(rank) * kBlockM + q * 32;  // the warp's first row
-            const int x0 = t.n_blk * BLOCK_N + hf * (BLOCK_N / 2);                           // and first column
+            const int y0 = t.m_blk * Cfg::EDGE + static_cast<int>(rank) * Cfg::ROWS + q * WR;  // the warp's first row
+            const int x0 = t.n_blk * Cfg::EDGE + column;                           // and first column
             const bool poly = t.phase == kNsPoly, last = t.phase == kNsStep && t.step == p.steps - 1;
             const int M = t.phase == kNsStep ? p.R : p.m, N = t.phase == kNsStep ? p.C : p.m;
             const float alpha = t.phase == kNsGram ? p.gram_alpha : poly ? p.poly_alpha : last ? p.last_alpha : p.step_alpha;
             const ptx::f2 al = ptx::make_f2(alpha, alpha);
-            // eight rows of four lie 4 N apart; the lane's first 16 bytes
+            // the lane's first 16 bytes; its rows lie 4 N apart
             const long long at = (static_cast<long long>(t.z) * M + y0 + rr0) * N + x0 + cc * 8;
             bool ok = true;
             auto in_row = [&](int i) { return y0 + rr0 + i * 4 < M; };
@@ -427,13 +430,13 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
 #pragma unroll 1
                 for (int piece = 0; piece < PIECES; ++piece) {
                     const bool in_col = x0 + piece * 64 + cc * 8 < N;
-                    uint4 v[8];
+                    uint4 v[WR / 4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                    for (int i = 0; i < WR / 4; ++i)
                         v[i] = in_row(i) && in_col ? ld_global_cg_v4(p.s + at + static_cast<long long>(i) * 4 * N + piece * 64)
                                                    : make_uint4(0, 0, 0, 0);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                    for (int i = 0; i < WR / 4; ++i)
                         ptx::st_shared_v4(flat + piece * Cfg::BOX_BYTES + i * 512u +
                                               (static_cast<uint32_t>(cc ^ ((rr0 + i * 4) & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
                 }
@@ -444,7 +447,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             if (!ok) ptx::st_shared_u32_volatile(epi_abort_addr, 1);
             ptx::tc_fence_after();
             const uint32_t t_acc = tmem_base + (static_cast<uint32_t>(q * 32) << 16) +
-                                   static_cast<uint32_t>(acc * BLOCK_N + hf * (BLOCK_N / 2));
+                                   static_cast<uint32_t>(acc * Cfg::EDGE + column);
             uint32_t r[2 * PIECES][32];
 #pragma unroll
             for (int i = 0; i < 2 * PIECES; ++i) ptx::tmem_ld_32x32_issue(t_acc + static_cast<uint32_t>(i * 32), r[i]);
@@ -468,13 +471,14 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                         const uint32_t (&rj)[32] = r[2 * piece + (j >> 2)];
                         uint32_t w[4];
                         f(j, w, [&](int k) { return ptx::make_f2_bits(rj[(j & 3) * 8 + 2 * k], rj[(j & 3) * 8 + 2 * k + 1]); });
-                        ptx::st_shared_v4(box + ((static_cast<uint32_t>(j) ^ sw) << 4), w[0], w[1], w[2], w[3]);
+                        if (WR == 32 || has_row) ptx::st_shared_v4(box + ((static_cast<uint32_t>(j) ^ sw) << 4), w[0], w[1], w[2], w[3]);
                     }
                 };
                 if (poly) {
                     convert([&](int j, uint32_t (&w)[4], auto &&pair) {
                         uint32_t a4[4];
-                        ptx::ld_shared_v4(box + ((static_cast<uint32_t>(j) ^ sw) << 4), a4[0], a4[1], a4[2], a4[3]);
+                        a4[0] = a4[1] = a4[2] = a4[3] = 0;
+                        if (WR == 32 || has_row) ptx::ld_shared_v4(box + ((static_cast<uint32_t>(j) ^ sw) << 4), a4[0], a4[1], a4[2], a4[3]);
                         const int d = y0 + lane - (x0 + piece * 64 + j * 8);  // the diagonal's place among the eight
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
@@ -516,7 +520,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 uint4 *d4 = static_cast<uint4 *>(p.out[t.z]) + (at - static_cast<long long>(t.z) * M * N) / 8;
                 const bool in_col = ok && x0 + piece * 64 + cc * 8 < N;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < WR / 4; ++i) {
                     uint32_t w[4];
                     ptx::ld_shared_v4(flat + piece * Cfg::BOX_BYTES + i * 512u + (static_cast<uint32_t>(cc ^ ((rr0 + i * 4) & 7)) << 4),
                                       w[0], w[1], w[2], w[3]);
