@@ -1826,7 +1826,8 @@ int norm_blocks(int64_t BT, int64_t C)
 
 // Fills in the ring and launches. `sums`: bytes per team that follow the rows in the same memory.
 template <int T, class P>
-int launch_norm(DeviceState &s, void (*kernel)(P), P p, int row_bytes, int sums, bool (&attr_set)[kMaxDevices], cudaStream_t stream)
+int launch_norm(DeviceState &s, void (*kernel)(P), P p, bool direct, int row_bytes, int sums,
+                bool (&attr_set)[kMaxDevices], cudaStream_t stream)
 {
     constexpr int kMost = 227 * 1024 - 2048;  // of shared memory, beside what the kernel has of its own
     int dev = 0;
@@ -1836,29 +1837,42 @@ int launch_norm(DeviceState &s, void (*kernel)(P), P p, int row_bytes, int sums,
         attr_set[dev] = true;
     }
     int teams = norm_teams(p.BT, 8ll * p.nvec);
-    if (teams > 1 && 2 * teams * row_bytes > kMost) teams /= 2;  // two rows of each team at least
-    const int fit = kMost / (teams * row_bytes);
-    p.slots = fit < kNormMaxSlots ? fit : kNormMaxSlots;
-    const int rows = teams * p.slots * row_bytes;
+    int rows = 0;
+    if (!direct) {
+        if (teams > 1 && 2 * teams * row_bytes > kMost) teams /= 2;  // two rows of each team at least
+        const int fit = kMost / (teams * row_bytes);
+        p.slots = fit < kNormMaxSlots ? fit : kNormMaxSlots;
+        rows = teams * p.slots * row_bytes;
+    }
     if (teams == 1) sums = 0;
     p.status = s.status;
     p.timeout_ns = kDefaultTimeoutNs;
     return launch_chained_smem(kernel, dim3(static_cast<unsigned>(norm_blocks(p.BT, 8ll * p.nvec))), T * teams,
                                static_cast<size_t>(rows > teams * sums ? rows : teams * sums), stream, p);
 }
+// Whether every team has one row at most, in blocks of half the largest size.
+template <int T>
+bool norm_direct(int64_t BT)
+{
+    return T < kNormMaxThreads && BT <= kNormMaxThreads / 2 / T * kNormMaxBlocks;
+}
 template <bool F32, int T, int NV>
 int launch_norm_forward(DeviceState &s, const NormForward &p, cudaStream_t stream)
 {
-    static bool attr_set[kMaxDevices] = {};
-    return launch_norm<T>(s, layernorm_forward_kernel<F32, T, NV>, p, norm_forward_row_bytes(F32, p.nvec, p.branch != nullptr), 0,
-                          attr_set, stream);
+    static bool attr_set[2][kMaxDevices] = {};
+    const int row = norm_forward_row_bytes(F32, p.nvec, p.branch != nullptr);
+    if constexpr (T < kNormMaxThreads)
+        if (norm_direct<T>(p.BT)) return launch_norm<T>(s, layernorm_forward_kernel<F32, T, NV, true>, p, true, row, 0, attr_set[1], stream);
+    return launch_norm<T>(s, layernorm_forward_kernel<F32, T, NV, false>, p, false, row, 0, attr_set[0], stream);
 }
 template <bool F32, int T, int NV>
 int launch_norm_backward(DeviceState &s, const NormBackward &p, cudaStream_t stream)
 {
-    static bool attr_set[kMaxDevices] = {};
-    return launch_norm<T>(s, layernorm_backward_kernel<F32, T, NV>, p, norm_row_bytes(F32, p.nvec, p.dres != nullptr),
-                          p.part ? p.nvec * 64 : 0, attr_set, stream);
+    static bool attr_set[2][kMaxDevices] = {};
+    const int row = norm_row_bytes(F32, p.nvec, p.dres != nullptr), sums = p.part ? p.nvec * 64 : 0;
+    if constexpr (T < kNormMaxThreads)
+        if (norm_direct<T>(p.BT)) return launch_norm<T>(s, layernorm_backward_kernel<F32, T, NV, true>, p, true, row, sums, attr_set[1], stream);
+    return launch_norm<T>(s, layernorm_backward_kernel<F32, T, NV, false>, p, false, row, sums, attr_set[0], stream);
 }
 
 template <int V>
@@ -2682,7 +2696,7 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
     if (rc != NB_OK) return rc;
     ++g_launches;
     if (!grads) return NB_OK;
-    rc = launch_chained(layernorm_reduce_kernel, dim3(static_cast<unsigned>((2 * C + 31) / 32)), 1024, stream,
+    rc = launch_chained(layernorm_reduce_kernel, dim3(static_cast<unsigned>((2 * C + 31) / 32)), 512, stream,
                         static_cast<float *>(dweight), static_cast<float *>(dbias), static_cast<const float *>(p.part), blocks,
                         static_cast<int>(C), accumulate);
     if (rc != NB_OK) return rc;

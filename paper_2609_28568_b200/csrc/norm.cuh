@@ -198,8 +198,10 @@ struct NormForward {
 // Shared memory of a row of the forward pass: inp, branch (if there is one).
 __host__ __device__ constexpr int norm_forward_row_bytes(bool f32, int nvec, bool has_branch) { return nvec * ((f32 ? 32 : 16) + (has_branch ? 16 : 0)); }
 
-template <bool F32, int T, int NV>
-__global__ void __launch_bounds__(kNormMaxThreads, 1)
+// DIRECT: no team has more than one row, which it loads into registers instead: a bulk copy and its barrier take 0.4 us longer, a tenth of a
+// call on few rows.
+template <bool F32, int T, int NV, bool DIRECT>
+__global__ void __launch_bounds__(DIRECT ? kNormMaxThreads / 2 : kNormMaxThreads, 1)
 layernorm_forward_kernel(const NormForward p)
 {
     extern __shared__ __align__(128) uint8_t norm_smem[];  // the teams' rows
@@ -213,10 +215,12 @@ layernorm_forward_kernel(const NormForward p)
     const uint32_t row_bytes = static_cast<uint32_t>(norm_forward_row_bytes(F32, p.nvec, has_branch));
     NormRing ring{ptx::smem_u32(norm_smem) + static_cast<uint32_t>(team * p.slots) * row_bytes,
                   ptx::smem_u32(bars) + 8u * static_cast<uint32_t>(team * kNormMaxSlots), row_bytes, p.slots, 0, 0};
-    if (t < p.slots) ptx::mbar_init(ring.bar + 8u * t, 1);
-    if (threadIdx.x == 0) abort_flag = 0;
-    ptx::fence_barrier_init();
-    __syncthreads();
+    if constexpr (!DIRECT) {
+        if (t < p.slots) ptx::mbar_init(ring.bar + 8u * t, 1);
+        if (threadIdx.x == 0) abort_flag = 0;
+        ptx::fence_barrier_init();
+        __syncthreads();
+    }
     chained_start();
     const WaitCtx wctx{ptx::smem_u32(&abort_flag), p.status, p.timeout_ns};
     const long long stride = static_cast<long long>(gridDim.x) * teams;
@@ -227,7 +231,17 @@ layernorm_forward_kernel(const NormForward p)
         bulk_load(dst, static_cast<const uint8_t *>(p.inp) + row * x_bytes, x_bytes, b);
         if (has_branch) bulk_load(dst + x_bytes, static_cast<const uint8_t *>(p.branch) + row * branch_bytes, branch_bytes, b);
     };
-    if (t == 0)
+    Raw8<F32> xd[DIRECT ? NV : 1];
+    uint4 bd[DIRECT ? NV : 1];
+    if constexpr (DIRECT) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = t + i * T;
+            if (j >= p.nvec || first >= p.BT) continue;
+            xd[i] = load8<F32>(p.inp, first * p.nvec + j);
+            if (has_branch) bd[i] = ptx::ld_global_v4(static_cast<const uint4 *>(p.branch) + first * p.nvec + j);
+        }
+    } else if (t == 0)
         for (int i = 0; i < p.slots && first + i * stride < p.BT; ++i) fetch(first + i * stride, i);
     uint4 w[NV], b[NV];
 #pragma unroll
@@ -241,7 +255,8 @@ layernorm_forward_kernel(const NormForward p)
     }
     int turn = 0;
     for (long long row = first; row < p.BT; row += stride) {
-        const bool ok = wait_barrier(wctx, ring.full(), ring.phase, 811);
+        bool ok = true;
+        if constexpr (!DIRECT) ok = wait_barrier(wctx, ring.full(), ring.phase, 811);
         Pairs v[NV];
         ptx::f2 sum = both(0.0f);
 #pragma unroll
@@ -249,19 +264,24 @@ layernorm_forward_kernel(const NormForward p)
             const int j = t + i * T;
             v[i] = Pairs{{both(0.0f), both(0.0f), both(0.0f), both(0.0f)}};
             if (j >= p.nvec) continue;
-            Raw8<F32> x = shared8<F32>(ring.row(), j);
+            Raw8<F32> x;
+            if constexpr (DIRECT) x = xd[i];
+            else x = shared8<F32>(ring.row(), j);
             if (has_branch) {
-                x = add_branch<F32>(x, shared8<false>(ring.row() + x_bytes, j).q[0]);
+                if constexpr (DIRECT) x = add_branch<F32>(x, bd[i]);
+                else x = add_branch<F32>(x, shared8<false>(ring.row() + x_bytes, j).q[0]);
                 if (ok) store8<F32>(p.sum, row * p.nvec + j, x);
             }
             v[i] = unpack8<F32>(x);  // the norm is that of the stored sum
             sum = ptx::add2(sum, ptx::add2(ptx::add2(v[i].v[0], v[i].v[1]), ptx::add2(v[i].v[2], v[i].v[3])));
         }
         const float mean = team_sum<T>(make_float2(sum2(sum), 0.0f), sums[team], turn++, team).x * p.inv_c;
-        if (T == 32) __syncwarp();
-        // the whole team has read the slot
-        if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, ring.slot);
-        ring.next();
+        if constexpr (!DIRECT) {
+            if (T == 32) __syncwarp();
+            // the whole team has read the slot
+            if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, ring.slot);
+            ring.next();
+        }
         const ptx::f2 minus = both(-mean);
         ptx::f2 sq = both(0.0f);
 #pragma unroll
@@ -314,8 +334,9 @@ struct NormBackward {
 __host__ __device__ constexpr int norm_row_bytes(bool f32, int nvec, bool has_res) { return nvec * (16 + (f32 ? 32 : 16) * (has_res ? 2 : 1)); }
 
 // A row is read twice from shared memory: once for its two sums and for the columns' sums, which stay in registers, and once for dinp.
-template <bool F32, int T, int NV>
-__global__ void __launch_bounds__(kNormMaxThreads, 1)
+// DIRECT: as in the forward pass; the row stays in registers.
+template <bool F32, int T, int NV, bool DIRECT>
+__global__ void __launch_bounds__(DIRECT ? kNormMaxThreads / 2 : kNormMaxThreads, 1)
 layernorm_backward_kernel(const NormBackward p)
 {
     extern __shared__ __align__(128) uint8_t norm_smem[];  // the teams' rows; then, of several teams, their sums [teams][2 C]
@@ -328,10 +349,12 @@ layernorm_backward_kernel(const NormBackward p)
     const uint32_t row_bytes = static_cast<uint32_t>(norm_row_bytes(F32, p.nvec, has_res));
     NormRing ring{ptx::smem_u32(norm_smem) + static_cast<uint32_t>(team * p.slots) * row_bytes,
                   ptx::smem_u32(bars) + 8u * static_cast<uint32_t>(team * kNormMaxSlots), row_bytes, p.slots, 0, 0};
-    if (t < p.slots) ptx::mbar_init(ring.bar + 8u * t, 1);
-    if (threadIdx.x == 0) abort_flag = 0;
-    ptx::fence_barrier_init();
-    __syncthreads();
+    if constexpr (!DIRECT) {
+        if (t < p.slots) ptx::mbar_init(ring.bar + 8u * t, 1);
+        if (threadIdx.x == 0) abort_flag = 0;
+        ptx::fence_barrier_init();
+        __syncthreads();
+    }
     chained_start();
     const WaitCtx wctx{ptx::smem_u32(&abort_flag), p.status, p.timeout_ns};
     const uint32_t dout_bytes = static_cast<uint32_t>(p.nvec) * 16u, x_bytes = dout_bytes * (F32 ? 2u : 1u);
@@ -345,7 +368,18 @@ layernorm_backward_kernel(const NormBackward p)
         bulk_load(dst + dout_bytes, static_cast<const uint8_t *>(p.inp) + row * x_bytes, x_bytes, b);
         if (has_res) bulk_load(dst + dout_bytes + x_bytes, static_cast<const uint8_t *>(p.dres) + row * x_bytes, x_bytes, b);
     };
-    if (t == 0)
+    uint4 dd[DIRECT ? NV : 1];
+    Raw8<F32> xd[DIRECT ? NV : 1], rd[DIRECT ? NV : 1];
+    if constexpr (DIRECT) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = t + i * T;
+            if (j >= p.nvec || first >= p.BT) continue;
+            dd[i] = ptx::ld_global_v4(static_cast<const uint4 *>(p.dout) + first * p.nvec + j);
+            xd[i] = load8<F32>(p.inp, first * p.nvec + j);
+            if (has_res) rd[i] = load8<F32>(p.dres, first * p.nvec + j);
+        }
+    } else if (t == 0)
         for (int i = 0; i < p.slots && first + i * stride < p.BT; ++i) fetch(first + i * stride, i);
 
     uint4 w[NV];
@@ -369,15 +403,24 @@ layernorm_backward_kernel(const NormBackward p)
             mean = __ldcg(p.mean + row + stride);
             rstd = __ldcg(p.rstd + row + stride);
         }
-        const bool ok = wait_barrier(wctx, ring.full(), ring.phase, 810);
+        bool ok = true;
+        if constexpr (!DIRECT) ok = wait_barrier(wctx, ring.full(), ring.phase, 810);
         const uint32_t src = ring.row();
+        auto get_dout = [&](int i) {
+            if constexpr (DIRECT) return dd[i];
+            else return shared8<false>(src, t + i * T).q[0];
+        };
+        auto get_inp = [&](int i) {
+            if constexpr (DIRECT) return xd[i];
+            else return shared8<F32>(src + dout_bytes, t + i * T);
+        };
         const ptx::f2 minus = both(-mu), rs2 = both(rs);
         ptx::f2 s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int j = t + i * T;
             if (j >= p.nvec) continue;
-            const Pairs d = unpack_bf16(shared8<false>(src, j).q[0]), x = unpack8<F32>(shared8<F32>(src + dout_bytes, j)),
+            const Pairs d = unpack_bf16(get_dout(i)), x = unpack8<F32>(get_inp(i)),
                         wf = unpack_bf16(w[i]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -394,7 +437,7 @@ layernorm_backward_kernel(const NormBackward p)
         for (int i = 0; i < NV; ++i) {
             const int j = t + i * T;
             if (j >= p.nvec) continue;
-            const Pairs d = unpack_bf16(shared8<false>(src, j).q[0]), x = unpack8<F32>(shared8<F32>(src + dout_bytes, j)),
+            const Pairs d = unpack_bf16(get_dout(i)), x = unpack8<F32>(get_inp(i)),
                         wf = unpack_bf16(w[i]);
             Pairs o;
 #pragma unroll
@@ -403,7 +446,10 @@ layernorm_backward_kernel(const NormBackward p)
                 o.v[k] = ptx::fma2(xh, c2, ptx::fma2(d.v[k], wf.v[k], c1));
             }
             if (has_res) {
-                const Pairs res = unpack8<F32>(shared8<F32>(src + dout_bytes + x_bytes, j));
+                Raw8<F32> raw;
+                if constexpr (DIRECT) raw = rd[i];
+                else raw = shared8<F32>(src + dout_bytes + x_bytes, j);
+                const Pairs res = unpack8<F32>(raw);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o.v[k] = ptx::fma2(o.v[k], rs2, res.v[k]);
             } else {
@@ -415,6 +461,7 @@ layernorm_backward_kernel(const NormBackward p)
                 if (p.dbranch) static_cast<uint4 *>(p.dbranch)[row * p.nvec + j] = pack_bf16(o);
             }
         }
+        if constexpr (DIRECT) break;
         team_sync<T>(team);  // the slot has been read
         if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, ring.slot);
         ring.next();
@@ -452,37 +499,36 @@ layernorm_backward_kernel(const NormBackward p)
 }
 
 // dweight[c] (+)= sum over the blocks' sums, dbias likewise, in a fixed order: results do not depend on which block ended
-// first. A block owns 32 columns of [dweight | dbias], a warp every 32nd part (at most five, loaded at once); they meet in shared memory.
+// first. A block owns 32 columns of [dweight | dbias], a warp every sixteenth part, all of them (ten at most) loaded at once, as is what
+// the result is added to: one trip to memory.
 constexpr int kNormMaxBlocks = 148;
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(512)
 layernorm_reduce_kernel(float *dweight, float *dbias, const float *part, int parts, int C, int accumulate)
 {
-    __shared__ float s[32][33];
+    constexpr int N = (kNormMaxBlocks + 15) / 16;
+    __shared__ float s[16][32];
     chained_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
-    float v[(kNormMaxBlocks + 31) / 32];
+    float *dst = c < C ? dweight : dbias;
+    if (dst != nullptr && c < 2 * C) dst += c < C ? c : c - C;
+    else dst = nullptr;
+    const float old = warp == 0 && accumulate && dst != nullptr ? __ldcg(dst) : 0.0f;
+    float v[N];
 #pragma unroll
-    for (int i = 0; i < (kNormMaxBlocks + 31) / 32; ++i) {
-        const int k = warp + 32 * i;
-        v[i] = c < 2 * C && k < parts ? __ldcg(part + static_cast<long long>(k) * 2 * C + c) : 0.0f;
+    for (int i = 0; i < N; ++i) {
+        const int k = warp + 16 * i;
+        v[i] = dst != nullptr && k < parts ? __ldcg(part + static_cast<long long>(k) * 2 * C + c) : 0.0f;
     }
-    float a = 0.0f;
+    float a = v[0];
 #pragma unroll
-    for (int i = 0; i < (kNormMaxBlocks + 31) / 32; ++i) a += v[i];
+    for (int i = 1; i < N; ++i) a += v[i];
     s[warp][lane] = a;
     __syncthreads();
-    // warp w adds column w's 32 values, lane by lane, pairwise
-    a = s[lane][warp];
+    if (warp != 0 || dst == nullptr) return;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-    const int mine = blockIdx.x * 32 + warp;
-    if (lane == 0 && mine < 2 * C) {
-        float *dst = mine < C ? dweight : dbias;
-        if (dst == nullptr) return;
-        dst += mine < C ? mine : mine - C;
-        *dst = accumulate ? *dst + a : a;
-    }
+    for (int k = 1; k < 16; ++k) a += s[k][lane];
+    *dst = old + a;
 }
 
 }  // namespace nb
