@@ -374,14 +374,23 @@ def _stream_dtype(t) -> int:
     return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
 
 
+def _want(t, dtype, shape, name: str) -> None:
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: {dtype} {tuple(shape)} is wanted, not {t.dtype} {tuple(t.shape)}")
+
+
 def layernorm_forward(inp, weight, bias=None, branch=None, eps=1e-5, train=True):
     """Allocate the outputs and call nb_layernorm_forward. inp [BT, C] is the residual stream (bf16 or fp32), branch what it takes
     up (bf16). Returns (out, sum, mean, rstd): sum is inp where there is no branch; mean and rstd are None unless train."""
     BT, C = inp.shape
+    dtype = _stream_dtype(inp)
+    _want(branch, torch.bfloat16, (BT, C), "branch")
+    _want(weight, torch.bfloat16, (C,), "weight")
+    _want(bias, torch.bfloat16, (C,), "bias")
     out = torch.empty((BT, C), dtype=torch.bfloat16, device=inp.device)
     total = None if branch is None else torch.empty_like(inp)
     mean, rstd = (torch.empty(BT, dtype=torch.float32, device=inp.device) for _ in range(2)) if train else (None, None)
-    nb_layernorm_forward(out, total, mean, rstd, inp, branch, weight, bias, BT, C, eps, _stream_dtype(inp))
+    nb_layernorm_forward(out, total, mean, rstd, inp, branch, weight, bias, BT, C, eps, dtype)
     return out, inp if branch is None else total, mean, rstd
 
 
@@ -391,6 +400,13 @@ def layernorm_backward(dout, inp, mean, rstd, weight, dres=None, dweight=None, d
     dweight, dbias): dinp in the stream's type, dbranch the same in bf16 (dinp itself where the stream is bf16)."""
     BT, C = inp.shape
     dtype = _stream_dtype(inp)
+    _want(dout, torch.bfloat16, (BT, C), "dout")
+    _want(dres, inp.dtype, (BT, C), "dres")
+    _want(weight, torch.bfloat16, (C,), "weight")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        _want(t, torch.float32, (BT,), name)
+    for t, name in ((dweight, "dweight"), (dbias, "dbias")):
+        _want(t, torch.float32, (C,), name)
     dinp = torch.empty_like(inp)
     dbranch = dinp if dtype == DTYPE_BF16 else torch.empty((BT, C), dtype=torch.bfloat16, device=inp.device)
     if need_dweight and dweight is None:

@@ -60,6 +60,7 @@ bool by_python(PyObject *convert, PyObject *o, void *&p)
 // A device pointer from None, an address, a contiguous CUDA tensor, or (by Python) what behaves like one.
 bool to_pointer(PyObject *o, void *&p)
 {
+    if (o == Py_None || PyLong_Check(o)) return to_address(o, p);  // first: to find that something is no tensor takes long
     if (THPVariable_Check(o)) {
         const at::Tensor &t = THPVariable_Unpack(o);
         if (!t.is_cuda() || !t.is_contiguous()) {
@@ -69,7 +70,6 @@ bool to_pointer(PyObject *o, void *&p)
         p = t.data_ptr();
         return true;
     }
-    if (o == Py_None || PyLong_Check(o)) return to_address(o, p);
     return by_python(g_pointer_of, o, p);
 }
 // A stream from an address or (by Python) a stream object.
@@ -99,15 +99,20 @@ bool convert(PyObject *o, T &v)
 
 // Whether a tensor lies on the device that the call will launch on. The operators that came with this check refuse another
 // device's tensors; the older calls leave that to the caller.
-bool on_current_device(PyObject *o)
-{
-    if (!THPVariable_Check(o)) return true;  // an address: the caller's own business
-    const at::Tensor &t = THPVariable_Unpack(o);
-    if (!t.is_cuda() || t.get_device() == c10::cuda::current_device()) return true;
-    PyErr_Format(PyExc_ValueError, "a tensor lies on device %d, the current device is %d", static_cast<int>(t.get_device()),
-                 static_cast<int>(c10::cuda::current_device()));
-    return false;
-}
+struct CurrentDevice {
+    int index = -1;  // asked for with the first tensor, once per call
+    bool has(PyObject *o)
+    {
+        // a number, or an address: the caller's own business
+        if (o == Py_None || PyLong_Check(o) || PyFloat_Check(o) || !THPVariable_Check(o)) return true;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda()) return true;
+        if (index < 0) index = static_cast<int>(c10::cuda::current_device());
+        if (t.get_device() == index) return true;
+        PyErr_Format(PyExc_ValueError, "a tensor lies on device %d, the current device is %d", static_cast<int>(t.get_device()), index);
+        return false;
+    }
+};
 
 // fn(args..., stream): the last argument may be left out or None, for the current stream.
 template <bool DEVICE_CHECKED, class... A, size_t... I>
@@ -129,9 +134,11 @@ PyObject *call(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, std::index_
         return convert(args[i], dst);
     };
     if (!(one(std::get<I>(v), I) && ...)) return nullptr;
-    if constexpr (DEVICE_CHECKED)
+    if constexpr (DEVICE_CHECKED) {
+        CurrentDevice device;
         for (Py_ssize_t i = 0; i < N - 1; ++i)
-            if (!on_current_device(args[i])) return nullptr;
+            if (!device.has(args[i])) return nullptr;
+    }
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = std::apply(fn, v);
@@ -245,7 +252,7 @@ struct Pointers {
     bool given = false;
     void **data() { return given ? p.data() : nullptr; }
 };
-bool to_pointers(PyObject *o, Pointers &v, int64_t n, const char *name)
+bool to_pointers(PyObject *o, Pointers &v, int64_t n, const char *name, CurrentDevice &device)
 {
     if (o == Py_None) return true;
     PyObject *seq = PySequence_Fast(o, "a sequence of tensors is wanted");
@@ -255,7 +262,7 @@ bool to_pointers(PyObject *o, Pointers &v, int64_t n, const char *name)
     if (ok) v.p.resize(static_cast<size_t>(n));
     for (int64_t i = 0; ok && i < n; ++i) {
         PyObject *t = PySequence_Fast_GET_ITEM(seq, i);
-        ok = to_pointer(t, v.p[static_cast<size_t>(i)]) && on_current_device(t);
+        ok = to_pointer(t, v.p[static_cast<size_t>(i)]) && device.has(t);
     }
     Py_DECREF(seq);
     v.given = ok;
@@ -273,6 +280,7 @@ PyObject *muon_update(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
     Pointers update, momentum, grad;
+    CurrentDevice device;
     int64_t n = 0, R = 0, C = 0, bytes = 0;
     float mu = 0, a = 0, b = 0, c = 0, eps = 0;
     int nesterov = 0, steps = 0, dtype = 0;
@@ -280,9 +288,9 @@ PyObject *muon_update(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     if (nargs != 16 && nargs != 17) return PyErr_Format(PyExc_TypeError, "16 or 17 arguments are wanted, not %zd", nargs);
     if (!convert(args[3], n) || !convert(args[4], R) || !convert(args[5], C) || !convert(args[6], mu) || !convert(args[7], nesterov) ||
         !convert(args[8], steps) || !convert(args[9], a) || !convert(args[10], b) || !convert(args[11], c) || !convert(args[12], eps) ||
-        !convert(args[13], dtype) || !to_pointer(args[14], ws) || !on_current_device(args[14]) || !convert(args[15], bytes) ||
-        !to_pointers(args[0], update, n, "update") || !to_pointers(args[1], momentum, n, "momentum") ||
-        !to_pointers(args[2], grad, n, "grad") || !to_stream_or_current(args, nargs, 16, stream))
+        !convert(args[13], dtype) || !to_pointer(args[14], ws) || !device.has(args[14]) || !convert(args[15], bytes) ||
+        !to_pointers(args[0], update, n, "update", device) || !to_pointers(args[1], momentum, n, "momentum", device) ||
+        !to_pointers(args[2], grad, n, "grad", device) || !to_stream_or_current(args, nargs, 16, stream))
         return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -299,13 +307,14 @@ PyObject *muon_apply(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
     Pointers master, weight, update;
+    CurrentDevice device;
     int64_t n = 0, count = 0;
     float decay = 0, step = 0;
     void *stream = nullptr;
     if (nargs != 7 && nargs != 8) return PyErr_Format(PyExc_TypeError, "7 or 8 arguments are wanted, not %zd", nargs);
     if (!convert(args[3], n) || !convert(args[4], count) || !convert(args[5], decay) || !convert(args[6], step) ||
-        !to_pointers(args[0], master, n, "master") || !to_pointers(args[1], weight, n, "weight") ||
-        !to_pointers(args[2], update, n, "update") || !to_stream_or_current(args, nargs, 7, stream))
+        !to_pointers(args[0], master, n, "master", device) || !to_pointers(args[1], weight, n, "weight", device) ||
+        !to_pointers(args[2], update, n, "update", device) || !to_stream_or_current(args, nargs, 7, stream))
         return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS

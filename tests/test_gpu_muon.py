@@ -179,3 +179,23 @@ def test_apply_keeps_what_is_not_finite_where_it_is():
     bad = ~torch.isfinite(m)
     assert bad.nonzero().view(-1).tolist() == [5, 6, 4095] and torch.equal(~torch.isfinite(w), bad)
     assert m[5] == float("inf") and torch.isnan(m[6]) and m[4095] == float("inf")
+
+
+def test_apply_past_32_bits():
+    count = (1 << 31) + 13
+    m = torch.zeros(count, dtype=F32, device=DEV)
+    u = torch.zeros(count, dtype=BF16, device=DEV)
+    u[-9:] = torch.arange(1, 10, device=DEV)
+    u[5] = 3.0
+    nb.nb_muon_apply([m], None, [u], 1, count, 0.5, 2.0)
+    assert torch.equal(m[-9:], -2.0 * torch.arange(1, 10, device=DEV).float()) and m[5] == -6.0
+    assert int((m != 0).sum()) == 10
+
+
+def test_workspace_past_32_bits():
+    """Thirty-two matrices whose iterates take 4 GB each way: the first one again as the last gives the same bits."""
+    grad = gradients(95, 2, 8192, 8192, 1e-4, BF16)
+    grad = grad[:1] + [grad[1].clone() for _ in range(30)] + [grad[0].clone()]
+    update = nb.muon_update(grad, steps=2)
+    assert torch.equal(update[0], update[31]) and torch.equal(update[1], update[30]) and not torch.equal(update[0], update[1])
+    close(update[31], newton_schulz(grad[31].double(), 2, COEFFICIENTS, 1e-7), "the last")

@@ -119,6 +119,21 @@ def test_update_binding_refusals(L):
     assert nb.muon_update([]) == []
 
 
+def test_norm_conveniences_refuse_other_types_and_shapes(L):
+    """Before anything is launched: none of these tensors is on a device."""
+    x, w, b16 = torch.zeros(4, 16), torch.zeros(16, dtype=torch.bfloat16), torch.zeros(4, 16, dtype=torch.bfloat16)
+    m = torch.zeros(4)
+    for kw in (dict(weight=w.float()), dict(weight=w[:8]), dict(weight=w, bias=w.float()), dict(weight=w, branch=x), dict(weight=w, branch=b16[:2])):
+        with pytest.raises(ValueError, match="is wanted"):
+            nb.layernorm_forward(x, **kw)
+    good = dict(dout=b16, inp=x, mean=m, rstd=m, weight=w)
+    for kw in (dict(dout=x), dict(mean=m.double()), dict(rstd=m[:3]), dict(weight=w.float()), dict(dres=b16), dict(dweight=w), dict(dbias=torch.zeros(8))):
+        with pytest.raises(ValueError, match="is wanted"):
+            nb.layernorm_backward(**{**good, **kw})
+    with pytest.raises(TypeError):
+        nb.layernorm_forward(x.half(), w)
+
+
 def test_apply_refusals(L):
     def call(m=_array(at(0), at(1)), w=_array(at(2), at(3)), u=_array(at(4), at(5)), n=2, count=10):
         return L.nb_muon_apply(m, w, u, n, count, 0.9, 0.1, None)
