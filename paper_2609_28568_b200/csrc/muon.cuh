@@ -83,31 +83,15 @@ struct MuonPrepare {
     void *out[kMuonBatch];         // muon_normalise_kernel with no step to follow: bf16 results
     double *part;                  // [n][parts]
     unsigned *done;                // [n], zeroed for the products' counts
-    __half *x;                     // [n][count], times `scale`
+    __half *x;                     // [n][rows][8 pitch], times `scale`
     long long nvec;                // elements / 8
+    int row_vec, pitch;            // vectors of eight in a row, and from one row of x to the next
     int parts;
     int nesterov;
     float mu, scale;
     double eps;
 };
 
-template <bool G32>
-__device__ __forceinline__ void muon_load_grad(const void *grad, long long i, float (&g)[8])
-{
-    if constexpr (G32) {
-        const float4 a = ptx::ld_global_f32x4(static_cast<const float4 *>(grad) + 2 * i);
-        const float4 b = ptx::ld_global_f32x4(static_cast<const float4 *>(grad) + 2 * i + 1);
-        g[0] = a.x, g[1] = a.y, g[2] = a.z, g[3] = a.w, g[4] = b.x, g[5] = b.y, g[6] = b.z, g[7] = b.w;
-    } else {
-        const uint4 a = ptx::ld_global_v4(static_cast<const uint4 *>(grad) + i);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            g[2 * k] = ptx::bf16_lo(w[k]);
-            g[2 * k + 1] = ptx::bf16_hi(w[k]);
-        }
-    }
-}
 // Sum over the block's 256 threads, in a fixed order; every thread gets it.
 __device__ __forceinline__ double block_sum_256(double v)
 {
@@ -119,6 +103,43 @@ __device__ __forceinline__ double block_sum_256(double v)
     return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
 }
 
+// v of vector i, from the gradient's and the momentum's eight values as they were loaded.
+template <bool G32>
+struct MuonVec {
+    float4 m[2];
+    uint4 g[G32 ? 2 : 1];
+    __device__ __forceinline__ void load_grad(const void *grad, long long i)
+    {
+        g[0] = ptx::ld_global_v4(static_cast<const uint4 *>(grad) + i * (G32 ? 2 : 1));
+        if constexpr (G32) g[1] = ptx::ld_global_v4(static_cast<const uint4 *>(grad) + i * 2 + 1);
+    }
+    __device__ __forceinline__ void load_momentum(const float *mom, long long i)
+    {
+        m[0] = ptx::ld_global_f32x4(mom + 8 * i);
+        m[1] = ptx::ld_global_f32x4(mom + 8 * i + 4);
+    }
+    __device__ __forceinline__ void momentum(float (&v)[8]) const
+    {
+        v[0] = m[0].x, v[1] = m[0].y, v[2] = m[0].z, v[3] = m[0].w, v[4] = m[1].x, v[5] = m[1].y, v[6] = m[1].z, v[7] = m[1].w;
+    }
+    __device__ __forceinline__ void grad(float (&v)[8]) const
+    {
+        if constexpr (G32) {
+            const uint32_t w[8] = {g[0].x, g[0].y, g[0].z, g[0].w, g[1].x, g[1].y, g[1].z, g[1].w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
+        } else {
+            const uint32_t w[4] = {g[0].x, g[0].y, g[0].z, g[0].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[2 * k] = ptx::bf16_lo(w[k]);
+                v[2 * k + 1] = ptx::bf16_hi(w[k]);
+            }
+        }
+    }
+};
+constexpr int kMuonUnroll = 2;  // vectors of a thread under way at once
+
 template <bool G32>
 __global__ void __launch_bounds__(256)
 muon_momentum_kernel(const __grid_constant__ MuonPrepare p)
@@ -127,25 +148,37 @@ muon_momentum_kernel(const __grid_constant__ MuonPrepare p)
     const void *grad = p.grad[blockIdx.y];
     float *mom = p.momentum[blockIdx.y];
     double sq = 0.0;
-    for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < p.nvec; i += 256ll * gridDim.x) {
-        float v[8];
-        if (mom) {
-            float4 m0 = ptx::ld_global_f32x4(mom + 8 * i), m1 = ptx::ld_global_f32x4(mom + 8 * i + 4);
-            muon_load_grad<G32>(grad, i, v);
-            float m[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
+    const long long stride = 256ll * gridDim.x;
+    for (long long i0 = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i0 < p.nvec; i0 += kMuonUnroll * stride) {
+        MuonVec<G32> x[kMuonUnroll];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                m[k] = fmaf(p.mu, m[k], v[k]);
-                v[k] = p.nesterov ? fmaf(p.mu, m[k], v[k]) : m[k];
-            }
-            float4 *dst = reinterpret_cast<float4 *>(mom + 8 * i);
-            dst[0] = make_float4(m[0], m[1], m[2], m[3]);
-            dst[1] = make_float4(m[4], m[5], m[6], m[7]);
-        } else {
-            muon_load_grad<G32>(grad, i, v);
+        for (int h = 0; h < kMuonUnroll; ++h) {
+            const long long i = i0 + h * stride;
+            if (i >= p.nvec) continue;
+            x[h].load_grad(grad, i);
+            if (mom) x[h].load_momentum(mom, i);
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sq = fma(static_cast<double>(v[k]), static_cast<double>(v[k]), sq);
+        for (int h = 0; h < kMuonUnroll; ++h) {
+            const long long i = i0 + h * stride;
+            if (i >= p.nvec) continue;
+            float v[8];
+            x[h].grad(v);
+            if (mom) {
+                float m[8];
+                x[h].momentum(m);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    m[k] = fmaf(p.mu, m[k], v[k]);
+                    v[k] = p.nesterov ? fmaf(p.mu, m[k], v[k]) : m[k];
+                }
+                float4 *dst = reinterpret_cast<float4 *>(mom + 8 * i);
+                dst[0] = make_float4(m[0], m[1], m[2], m[3]);
+                dst[1] = make_float4(m[4], m[5], m[6], m[7]);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sq = fma(static_cast<double>(v[k]), static_cast<double>(v[k]), sq);
+        }
     }
     sq = block_sum_256(sq);
     if (threadIdx.x == 0) {
@@ -163,35 +196,57 @@ muon_normalise_kernel(const __grid_constant__ MuonPrepare p)
     chained_start();
     const void *grad = p.grad[blockIdx.y];
     const float *mom = p.momentum[blockIdx.y];
-    const double *part = p.part + static_cast<long long>(blockIdx.y) * p.parts;
-    const double sq = block_sum_256(static_cast<int>(threadIdx.x) < p.parts ? __ldcg(part + threadIdx.x) : 0.0);
-    const double f = static_cast<double>(LAST ? 1.0f : p.scale) / (sqrt(sq) + p.eps);
+    const bool with_grad = !mom || p.nesterov;
+    const long long stride = 256ll * gridDim.x;
+    double f = 0.0;
     uint4 *dst = LAST ? static_cast<uint4 *>(p.out[blockIdx.y])
-                      : reinterpret_cast<uint4 *>(p.x) + static_cast<long long>(blockIdx.y) * p.nvec;
-    for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < p.nvec; i += 256ll * gridDim.x) {
-        float v[8];
-        if (mom) {
-            const float4 m0 = ptx::ld_global_f32x4(mom + 8 * i), m1 = ptx::ld_global_f32x4(mom + 8 * i + 4);
-            const float m[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
-            if (p.nesterov) muon_load_grad<G32>(grad, i, v);
+                      : reinterpret_cast<uint4 *>(p.x) + static_cast<long long>(blockIdx.y) * (p.nvec / p.row_vec) * p.pitch;
+    const double *part = p.part + static_cast<long long>(blockIdx.y) * p.parts;
+    const double share = static_cast<int>(threadIdx.x) < p.parts ? __ldcg(part + threadIdx.x) : 0.0;
+    bool first = true;
+    const long long start = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    // every thread goes through the first round: the norm is added up while its values are on their way
+    for (long long i0 = start; first || i0 < p.nvec; i0 += kMuonUnroll * stride) {
+        MuonVec<G32> x[kMuonUnroll];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = p.nesterov ? fmaf(p.mu, m[k], v[k]) : m[k];
-        } else {
-            muon_load_grad<G32>(grad, i, v);
+        for (int h = 0; h < kMuonUnroll; ++h) {
+            const long long i = i0 + h * stride;
+            if (i >= p.nvec) continue;
+            if (with_grad) x[h].load_grad(grad, i);
+            if (mom) x[h].load_momentum(mom, i);
         }
-        uint32_t w[4];
+        if (first) {
+            f = static_cast<double>(LAST ? 1.0f : p.scale) / (sqrt(block_sum_256(share)) + p.eps);
+            first = false;
+        }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float lo = static_cast<float>(static_cast<double>(v[2 * k]) * f);
-            const float hi = static_cast<float>(static_cast<double>(v[2 * k + 1]) * f);
-            if constexpr (LAST) {
-                w[k] = ptx::pack_bf16x2(lo, hi);
-            } else {
-                const __half2 h = __floats2half2_rn(lo, hi);
-                w[k] = *reinterpret_cast<const uint32_t *>(&h);
+        for (int h = 0; h < kMuonUnroll; ++h) {
+            const long long i = i0 + h * stride;
+            if (i >= p.nvec) continue;
+            float v[8];
+            if (with_grad) x[h].grad(v);
+            if (mom) {
+                float m[8];
+                x[h].momentum(m);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = p.nesterov ? fmaf(p.mu, m[k], v[k]) : m[k];
             }
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float lo = static_cast<float>(static_cast<double>(v[2 * k]) * f);
+                const float hi = static_cast<float>(static_cast<double>(v[2 * k + 1]) * f);
+                if constexpr (LAST) {
+                    w[k] = ptx::pack_bf16x2(lo, hi);
+                } else {
+                    const __half2 h2 = __floats2half2_rn(lo, hi);
+                    w[k] = *reinterpret_cast<const uint32_t *>(&h2);
+                }
+            }
+            const uint32_t row = static_cast<uint32_t>(i) / static_cast<uint32_t>(p.row_vec);  // i is below 2^27
+            const long long to = LAST ? i : i + static_cast<long long>(row) * (p.pitch - p.row_vec);
+            dst[to] = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 

@@ -194,19 +194,19 @@ int get_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t rows, u
     return NB_OK;
 }
 
-// n dense fp16 matrices [rows, cols] one after the other, in boxes of box_rows x 64 of one of them with the
+// n fp16 matrices [rows, cols] one after the other, ld elements from one row to the next, in boxes of box_rows x 64 of one of them with the
 // 128-byte swizzle. What lies outside a matrix reads as zero and is not written.
-int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n, uint64_t rows, uint64_t cols,
+int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n, uint64_t rows, uint64_t cols, uint64_t ld,
                    uint32_t box_rows)
 {
-    TmapKey key{ptr, rows, cols, cols, 64, box_rows, 2, n};
+    TmapKey key{ptr, rows, cols, ld, 64, box_rows, 2, n};
     auto it = s.tmaps.find(key);
     if (it != s.tmaps.end()) {
         *out = it->second;
         return NB_OK;
     }
     cuuint64_t dims[3] = {cols, rows, n};
-    cuuint64_t strides[2] = {cols * 2, rows * cols * 2};
+    cuuint64_t strides[2] = {ld * 2, rows * ld * 2};
     cuuint32_t box[3] = {64, box_rows, 1};
     cuuint32_t estr[3] = {1, 1, 1};
     alignas(64) CUtensorMap m;
@@ -1898,11 +1898,12 @@ int with_norm_form(const NormForm &f, F &&fn)
 struct MuonSpace {
     int64_t x[2], s, p, part, done, bytes;
 };
-int muon_parts(int64_t nvec)  // blocks that read a matrix: about four vectors of eight per thread, 256 at most
+int muon_parts(int64_t nvec)  // blocks that read a matrix: about two vectors of eight per thread, 256 at most
 {
-    const int64_t b = (nvec + 1023) / 1024;
+    const int64_t b = (nvec + 511) / 512;
     return static_cast<int>(b < 256 ? b : 256);
 }
+int64_t muon_pitch(int64_t cols) { return (cols + 63) & ~int64_t{63}; }  // whole 128-byte pieces
 MuonSpace muon_space(int64_t n, int64_t R, int64_t C)
 {
     if (n > kMuonBatch) n = kMuonBatch;
@@ -1910,10 +1911,10 @@ MuonSpace muon_space(int64_t n, int64_t R, int64_t C)
     auto up = [](int64_t b) { return (b + 1023) & ~int64_t{1023}; };
     MuonSpace w;
     w.x[0] = 0;
-    w.x[1] = up(n * R * C * 2);
-    w.s = w.x[1] + up(n * R * C * 2);
-    w.p = w.s + up(n * m * m * 2);
-    w.part = w.p + up(n * m * m * 2);
+    w.x[1] = up(n * R * muon_pitch(C) * 2);
+    w.s = w.x[1] + up(n * R * muon_pitch(C) * 2);
+    w.p = w.s + up(n * m * muon_pitch(m) * 2);
+    w.part = w.p + up(n * m * muon_pitch(m) * 2);
     w.done = w.part + up(n * muon_parts(R * C / 8) * 8);
     w.bytes = w.done + up(n * 4);
     return w;
@@ -1962,10 +1963,10 @@ int launch_ns(DeviceState &s, NsParams p, cudaStream_t stream)
     CUtensorMap in[4], out[4];
     const void *at[4] = {p.x[0], p.x[1], p.s, p.p};
     for (int i = 0; i < 4; ++i) {
-        const uint64_t rows = i < 2 ? p.R : p.m, cols = i < 2 ? p.C : p.m;
+        const uint64_t rows = i < 2 ? p.R : p.m, cols = i < 2 ? p.C : p.m, ld = i < 2 ? p.ldx : p.lds;
         int rc;
-        if ((rc = get_batch_tmap(s, &in[i], at[i], p.n, rows, cols, 64)) != NB_OK) return rc;
-        if ((rc = get_batch_tmap(s, &out[i], at[i], p.n, rows, cols, Cfg::WARP_ROWS)) != NB_OK) return rc;
+        if ((rc = get_batch_tmap(s, &in[i], at[i], p.n, rows, cols, ld, 64)) != NB_OK) return rc;
+        if ((rc = get_batch_tmap(s, &out[i], at[i], p.n, rows, cols, ld, Cfg::WARP_ROWS)) != NB_OK) return rc;
     }
     NB_CUDA(cudaLaunchKernelEx(&cfg, newton_schulz_kernel<Cfg>, in[0], in[1], in[2], in[3], out[0], out[1], out[2], out[3], p));
     ++g_launches;
@@ -2001,6 +2002,8 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
     pr.x = reinterpret_cast<__half *>(q.workspace + w.x[0]);
     pr.nvec = q.R * q.C / 8;
     pr.parts = muon_parts(pr.nvec);
+    pr.row_vec = C / 8;
+    pr.pitch = static_cast<int>(muon_pitch(C)) / 8;
     pr.nesterov = q.nesterov;
     pr.mu = q.mu;
     pr.scale = kNsScaleX;
@@ -2024,6 +2027,8 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
     p.C = C;
     p.m = m;
     p.n = n;
+    p.ldx = static_cast<int>(muon_pitch(C));
+    p.lds = static_cast<int>(muon_pitch(m));
     p.steps = q.steps;
     p.kb_gram = kblocks_of(k);
     p.kb_m = kblocks_of(m);

@@ -35,7 +35,8 @@ struct NsParams {
     int kb_gram, kb_m;     // k-blocks of S = X X^T, and of the other two products
     int units;             // tiles of all steps and matrices
     float gram_alpha, poly_alpha, poly_beta, poly_diag, step_alpha, last_alpha;
-    __half *x[2], *s, *p;  // [n, R, C], [n, m, m]
+    __half *x[2], *s, *p;  // [n, R, ldx], [n, m, lds]
+    int ldx, lds;          // of whole 128-byte pieces: rows of 776 as they are straddle the lines that their boxes are read from
     unsigned *done;        // [n]: CTAs that have stored their part of a tile, over all phases
     void *out[kMuonBatch];
     int *status;
@@ -420,20 +421,20 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             const int M = t.phase == kNsStep ? p.R : p.m, N = t.phase == kNsStep ? p.C : p.m;
             const float alpha = t.phase == kNsGram ? p.gram_alpha : poly ? p.poly_alpha : last ? p.last_alpha : p.step_alpha;
             const ptx::f2 al = ptx::make_f2(alpha, alpha);
-            // the lane's first 16 bytes; its rows lie 4 N apart
-            const long long at = (static_cast<long long>(t.z) * M + y0 + rr0) * N + x0 + cc * 8;
             bool ok = true;
             auto in_row = [&](int i) { return y0 + rr0 + i * 4 < M; };
             if (poly) {  // b S is added: the tile's part of S comes into staging while the product is formed
                 if (lane == 0) ok = ns_wait_done(wctx_epi, status0, p.done + t.z, t.need * CG, 710);
                 __syncwarp();
+                // the lane's first 16 bytes; its rows lie 4 lds apart
+                const __half *src = p.s + (static_cast<long long>(t.z) * M + y0 + rr0) * p.lds + x0 + cc * 8;
 #pragma unroll 1
                 for (int piece = 0; piece < PIECES; ++piece) {
                     const bool in_col = x0 + piece * 64 + cc * 8 < N;
                     uint4 v[WR / 4];
 #pragma unroll
                     for (int i = 0; i < WR / 4; ++i)
-                        v[i] = in_row(i) && in_col ? ld_global_cg_v4(p.s + at + static_cast<long long>(i) * 4 * N + piece * 64)
+                        v[i] = in_row(i) && in_col ? ld_global_cg_v4(src + static_cast<long long>(i) * 4 * p.lds + piece * 64)
                                                    : make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int i = 0; i < WR / 4; ++i)
@@ -517,7 +518,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 }
                 // The results: whole pieces of the caller's rows, by plain stores.
                 __syncwarp();
-                uint4 *d4 = static_cast<uint4 *>(p.out[t.z]) + (at - static_cast<long long>(t.z) * M * N) / 8;
+                uint4 *d4 = static_cast<uint4 *>(p.out[t.z]) + (static_cast<long long>(y0 + rr0) * N + x0) / 8 + cc;
                 const bool in_col = ok && x0 + piece * 64 + cc * 8 < N;
 #pragma unroll
                 for (int i = 0; i < WR / 4; ++i) {
