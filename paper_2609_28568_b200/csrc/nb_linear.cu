@@ -2701,7 +2701,7 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
     if (rc != NB_OK) return rc;
     ++g_launches;
     if (!grads) return NB_OK;
-    rc = launch_chained(layernorm_reduce_kernel, dim3(static_cast<unsigned>((2 * C + 31) / 32)), 512, stream,
+    rc = launch_chained(layernorm_reduce_kernel, dim3(static_cast<unsigned>(2 * C / kNormReduceCols)), 512, stream,
                         static_cast<float *>(dweight), static_cast<float *>(dbias), static_cast<const float *>(p.part), blocks,
                         static_cast<int>(C), accumulate);
     if (rc != NB_OK) return rc;

@@ -499,35 +499,34 @@ layernorm_backward_kernel(const NormBackward p)
 }
 
 // dweight[c] (+)= sum over the blocks' sums, dbias likewise, in a fixed order: results do not depend on which block ended
-// first. A block owns 32 columns of [dweight | dbias], a warp every sixteenth part, all of them (ten at most) loaded at once, as is what
+// first. A block owns 16 columns of [dweight | dbias], half a warp every 32nd part, all of them (five at most) loaded at once, as is what
 // the result is added to: one trip to memory.
-constexpr int kNormMaxBlocks = 148;
+constexpr int kNormMaxBlocks = 148, kNormReduceCols = 16;
 __global__ void __launch_bounds__(512)
 layernorm_reduce_kernel(float *dweight, float *dbias, const float *part, int parts, int C, int accumulate)
 {
-    constexpr int N = (kNormMaxBlocks + 15) / 16;
-    __shared__ float s[16][32];
+    constexpr int N = (kNormMaxBlocks + 31) / 32;
+    __shared__ float s[32][kNormReduceCols];
     chained_start();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = blockIdx.x * 32 + lane;
+    const int column = threadIdx.x % kNormReduceCols, group = threadIdx.x / kNormReduceCols;
+    const int c = blockIdx.x * kNormReduceCols + column;  // 2 C is a multiple of 16
     float *dst = c < C ? dweight : dbias;
-    if (dst != nullptr && c < 2 * C) dst += c < C ? c : c - C;
-    else dst = nullptr;
-    const float old = warp == 0 && accumulate && dst != nullptr ? __ldcg(dst) : 0.0f;
+    if (dst != nullptr) dst += c < C ? c : c - C;
+    const float old = group == 0 && accumulate && dst != nullptr ? __ldcg(dst) : 0.0f;
     float v[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int k = warp + 16 * i;
+        const int k = group + 32 * i;
         v[i] = dst != nullptr && k < parts ? __ldcg(part + static_cast<long long>(k) * 2 * C + c) : 0.0f;
     }
     float a = v[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) a += v[i];
-    s[warp][lane] = a;
+    s[group][column] = a;
     __syncthreads();
-    if (warp != 0 || dst == nullptr) return;
+    if (group != 0 || dst == nullptr) return;
 #pragma unroll
-    for (int k = 1; k < 16; ++k) a += s[k][lane];
+    for (int k = 1; k < 32; ++k) a += s[k][column];
     *dst = old + a;
 }
 
