@@ -1802,32 +1802,34 @@ bool any_overlap(Span *v, int64_t n)
 // Threads of a row's team and vectors per thread by the row's length: a warp up to 1024 elements, where its
 // shuffles are all the meeting it needs, four to sixteen warps above.
 struct NormForm {
-    int threads, nv;
+    int threads, nv, teams;  // teams of a block
+    bool direct;             // no team has more than one row
 };
-NormForm norm_form(int64_t C)
+NormForm norm_form(int64_t BT, int64_t C)
 {
     const int nvec = static_cast<int>(C / 8);
-    if (nvec <= 128) return {32, (nvec + 31) / 32};
-    if (nvec <= 256) return {128, 2};
-    return {nvec <= 512 ? 256 : 512, 2};
+    NormForm f{32, (nvec + 31) / 32, 0, false};
+    if (nvec > 512) f = {512, 2, 0, false};
+    else if (nvec > 256) f = {256, 2, 0, false};
+    else if (nvec > 128) f = {128, 2, 0, false};
+    // sixteen warps where there are rows enough for as many teams, else half of them, a row each if that suffices
+    f.teams = kNormMaxThreads / f.threads;
+    if (f.teams > 1 && BT <= f.teams / 2 * kNormMaxBlocks) {
+        f.teams /= 2;
+        f.direct = true;
+    }
+    return f;
 }
-// A block on each of 148 SMs, of sixteen warps where there are rows enough for as many teams. By sizes alone, so that the backward's
-// workspace is known before the device is.
-int norm_teams(int64_t BT, int64_t C)
-{
-    const int most = kNormMaxThreads / norm_form(C).threads;
-    return most > 1 && BT <= most / 2 * kNormMaxBlocks ? most / 2 : most;
-}
+// A block on each of 148 SMs: by sizes alone, so that the backward's workspace is known before the device is.
 int norm_blocks(int64_t BT, int64_t C)
 {
-    const int64_t teams = norm_teams(BT, C), blocks = (BT + teams - 1) / teams;
+    const int64_t teams = norm_form(BT, C).teams, blocks = (BT + teams - 1) / teams;
     return static_cast<int>(blocks < kNormMaxBlocks ? blocks : kNormMaxBlocks);
 }
 
 // Fills in the ring and launches. `sums`: bytes per team that follow the rows in the same memory.
-template <int T, class P>
-int launch_norm(DeviceState &s, void (*kernel)(P), P p, bool direct, int row_bytes, int sums,
-                bool (&attr_set)[kMaxDevices], cudaStream_t stream)
+template <class P>
+int launch_norm(DeviceState &s, void (*kernel)(P), P p, int row_bytes, int sums, bool (&attr_set)[kMaxDevices], cudaStream_t stream)
 {
     constexpr int kMost = 227 * 1024 - 2048;  // of shared memory, beside what the kernel has of its own
     int dev = 0;
@@ -1836,60 +1838,53 @@ int launch_norm(DeviceState &s, void (*kernel)(P), P p, bool direct, int row_byt
         NB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
         attr_set[dev] = true;
     }
-    int teams = norm_teams(p.BT, 8ll * p.nvec);
+    NormForm f = norm_form(p.BT, 8ll * p.nvec);
+    const int blocks = norm_blocks(p.BT, 8ll * p.nvec);
     int rows = 0;
-    if (!direct) {
-        if (teams > 1 && 2 * teams * row_bytes > kMost) teams /= 2;  // two rows of each team at least
-        const int fit = kMost / (teams * row_bytes);
+    if (!f.direct) {
+        if (f.teams > 1 && 2 * f.teams * row_bytes > kMost) f.teams /= 2;  // two rows of each team at least
+        const int fit = kMost / (f.teams * row_bytes);
         p.slots = fit < kNormMaxSlots ? fit : kNormMaxSlots;
-        rows = teams * p.slots * row_bytes;
+        rows = f.teams * p.slots * row_bytes;
     }
-    if (teams == 1) sums = 0;
+    if (f.teams == 1) sums = 0;
     p.status = s.status;
     p.timeout_ns = kDefaultTimeoutNs;
-    return launch_chained_smem(kernel, dim3(static_cast<unsigned>(norm_blocks(p.BT, 8ll * p.nvec))), T * teams,
-                               static_cast<size_t>(rows > teams * sums ? rows : teams * sums), stream, p);
+    return launch_chained_smem(kernel, dim3(static_cast<unsigned>(blocks)), f.threads * f.teams,
+                               static_cast<size_t>(rows > f.teams * sums ? rows : f.teams * sums), stream, p);
 }
-// Whether every team has one row at most, in blocks of half the largest size.
-template <int T>
-bool norm_direct(int64_t BT)
-{
-    return T < kNormMaxThreads && BT <= kNormMaxThreads / 2 / T * kNormMaxBlocks;
-}
-template <bool F32, int T, int NV>
+template <bool F32, int T, int NV, bool DIRECT>
 int launch_norm_forward(DeviceState &s, const NormForward &p, cudaStream_t stream)
 {
-    static bool attr_set[2][kMaxDevices] = {};
-    const int row = norm_forward_row_bytes(F32, p.nvec, p.branch != nullptr);
-    if constexpr (T < kNormMaxThreads)
-        if (norm_direct<T>(p.BT)) return launch_norm<T>(s, layernorm_forward_kernel<F32, T, NV, true>, p, true, row, 0, attr_set[1], stream);
-    return launch_norm<T>(s, layernorm_forward_kernel<F32, T, NV, false>, p, false, row, 0, attr_set[0], stream);
+    static bool attr_set[kMaxDevices] = {};
+    return launch_norm(s, layernorm_forward_kernel<F32, T, NV, DIRECT>, p, norm_forward_row_bytes(F32, p.nvec, p.branch != nullptr), 0,
+                       attr_set, stream);
 }
-template <bool F32, int T, int NV>
+template <bool F32, int T, int NV, bool DIRECT>
 int launch_norm_backward(DeviceState &s, const NormBackward &p, cudaStream_t stream)
 {
-    static bool attr_set[2][kMaxDevices] = {};
-    const int row = norm_row_bytes(F32, p.nvec, p.dres != nullptr), sums = p.part ? p.nvec * 64 : 0;
-    if constexpr (T < kNormMaxThreads)
-        if (norm_direct<T>(p.BT)) return launch_norm<T>(s, layernorm_backward_kernel<F32, T, NV, true>, p, true, row, sums, attr_set[1], stream);
-    return launch_norm<T>(s, layernorm_backward_kernel<F32, T, NV, false>, p, false, row, sums, attr_set[0], stream);
+    static bool attr_set[kMaxDevices] = {};
+    return launch_norm(s, layernorm_backward_kernel<F32, T, NV, DIRECT>, p, norm_row_bytes(F32, p.nvec, p.dres != nullptr),
+                       p.part ? p.nvec * 64 : 0, attr_set, stream);
 }
 
 template <int V>
 using IntC = std::integral_constant<int, V>;
-// fn(threads, vectors) of the form, as constants
-template <class F>
+// fn(threads, vectors, direct) of the form, as constants
+template <bool DIRECT, class F>
 int with_norm_form(const NormForm &f, F &&fn)
 {
+    constexpr std::bool_constant<DIRECT> d{};
     if (f.threads == 32) {
-        switch (f.nv) {
-            case 1: return fn(IntC<32>{}, IntC<1>{});
-            case 2: return fn(IntC<32>{}, IntC<2>{});
-            case 3: return fn(IntC<32>{}, IntC<3>{});
-            default: return fn(IntC<32>{}, IntC<4>{});
-        }
+        if (f.nv == 1) return fn(IntC<32>{}, IntC<1>{}, d);
+        if (f.nv == 2) return fn(IntC<32>{}, IntC<2>{}, d);
+        if (f.nv == 3) return fn(IntC<32>{}, IntC<3>{}, d);
+        return fn(IntC<32>{}, IntC<4>{}, d);
     }
-    return f.threads == 128 ? fn(IntC<128>{}, IntC<2>{}) : f.threads == 256 ? fn(IntC<256>{}, IntC<2>{}) : fn(IntC<512>{}, IntC<2>{});
+    if constexpr (!DIRECT) {
+        if (f.threads == 512) return fn(IntC<512>{}, IntC<2>{}, d);
+    }
+    return f.threads == 128 ? fn(IntC<128>{}, IntC<2>{}, d) : fn(IntC<256>{}, IntC<2>{}, d);
 }
 
 // ----------------------------------------------------------------------------- orthogonalised momentum
@@ -2634,10 +2629,12 @@ int nb_layernorm_forward(void *out, void *sum, void *mean, void *rstd, const voi
     p.inv_c = static_cast<float>(1.0 / static_cast<double>(C));
     p.eps = eps;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    rc = with_norm_form(norm_form(C), [&](auto T, auto NV) {
-        return stream_dtype == NB_DTYPE_F32 ? launch_norm_forward<true, T.value, NV.value>(*s, p, stream)
-                                            : launch_norm_forward<false, T.value, NV.value>(*s, p, stream);
-    });
+    auto launch = [&](auto T, auto NV, auto direct) {
+        return stream_dtype == NB_DTYPE_F32 ? launch_norm_forward<true, T.value, NV.value, direct.value>(*s, p, stream)
+                                            : launch_norm_forward<false, T.value, NV.value, direct.value>(*s, p, stream);
+    };
+    const NormForm form = norm_form(BT, C);
+    rc = form.direct ? with_norm_form<true>(form, launch) : with_norm_form<false>(form, launch);
     if (rc != NB_OK) return rc;
     ++g_launches;
     return NB_OK;
@@ -2694,10 +2691,12 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
     p.nvec = static_cast<int>(C / 8);
     p.inv_c = static_cast<float>(1.0 / static_cast<double>(C));
     const int blocks = norm_blocks(BT, C);
-    rc = with_norm_form(norm_form(C), [&](auto T, auto NV) {
-        return stream_dtype == NB_DTYPE_F32 ? launch_norm_backward<true, T.value, NV.value>(*s, p, stream)
-                                            : launch_norm_backward<false, T.value, NV.value>(*s, p, stream);
-    });
+    auto launch = [&](auto T, auto NV, auto direct) {
+        return stream_dtype == NB_DTYPE_F32 ? launch_norm_backward<true, T.value, NV.value, direct.value>(*s, p, stream)
+                                            : launch_norm_backward<false, T.value, NV.value, direct.value>(*s, p, stream);
+    };
+    const NormForm form = norm_form(BT, C);
+    rc = form.direct ? with_norm_form<true>(form, launch) : with_norm_form<false>(form, launch);
     if (rc != NB_OK) return rc;
     ++g_launches;
     if (!grads) return NB_OK;

@@ -151,7 +151,7 @@ __device__ __forceinline__ float2 team_sum(float2 v, float2 (*slots)[T / 32], in
 }
 
 constexpr int kNormMaxSlots = 4;
-constexpr int kNormMaxThreads = 512;
+constexpr int kNormMaxThreads = 512;  // of a block; half of that in the DIRECT forms
 
 // What the passes share: rows come into shared memory by bulk copies, up to kNormMaxSlots per team under way, whatever registers the
 // arithmetic needs. (By loads into registers, with the next row's ahead, a backward row of 768 took 218 registers and one of
