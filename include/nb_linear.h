@@ -38,6 +38,7 @@
  *    while a stream is being captured into a CUDA graph: size it first with
  *    nb_workspace_reserve (a call that would have to grow it during a capture returns
  *    NB_ERR_UNSUPPORTED and launches nothing).
+ *    nb_layernorm_backward and nb_muon_update take a workspace of the caller's instead.
  */
 #ifndef NB_LINEAR_H
 #define NB_LINEAR_H

@@ -104,6 +104,20 @@ def test_gradients_of_any_size(std):
             assert got.double().abs().max() <= 1e-6 and ref.abs().max() <= 1e-6
 
 
+@pytest.mark.parametrize("R,C", [(256, 512), (768, 520)])
+def test_steeply_falling_singular_values(R, C):
+    """Singular values 1 / j^2. The first rounding to fp16 leaves noise of 2^-11 / sqrt(3) of each value of x, whose norm is one: spread over the
+    matrix its singular values reach 2.8e-4 (1 / sqrt(R) + 1 / sqrt(C)), and five steps multiply small ones by 485. Beside an update whose
+    singular values are of the order of one that is up to 1.5e-2 (256 x 512) of its norm; the later iterates' roundings,
+    multiplied by 140, 41, 12 and 3.4, add less than as much again."""
+    m = min(R, C)
+    u, v = torch.linalg.qr(rand(60, (R, m), dtype=torch.float64))[0], torch.linalg.qr(rand(61, (C, m), dtype=torch.float64))[0]
+    g = (u * torch.arange(1, m + 1, device=DEV, dtype=torch.float64) ** -2 @ v.T).float()
+    got, ref = nb.muon_update([g])[0], newton_schulz(g.double(), 5, COEFFICIENTS, 1e-7)
+    noise = 485 * 2 ** -11 / 3 ** 0.5 * (R ** -0.5 + C ** -0.5)
+    assert ((got.double() - ref).norm() / ref.norm()).item() <= 2 * noise + 2.5e-3
+
+
 def test_matrices_do_not_touch_each_other():
     n, R, C = 4, 264, 136
     grad = gradients(70, n, R, C, 1e-3)
