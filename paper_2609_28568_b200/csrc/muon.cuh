@@ -8,6 +8,7 @@
 
 namespace nb {
 
+constexpr int kMuonCountPitch = 32;  // words between the counts of two matrices: a line of L2 each
 constexpr int kMuonBatch = 32;  // matrices per launch: their addresses are kernel parameters
 
 struct MuonApply {
@@ -183,7 +184,7 @@ muon_momentum_kernel(const __grid_constant__ MuonPrepare p)
     sq = block_sum_256(sq);
     if (threadIdx.x == 0) {
         p.part[static_cast<long long>(blockIdx.y) * p.parts + blockIdx.x] = sq;
-        if (blockIdx.x == 0) p.done[blockIdx.y] = 0;
+        if (blockIdx.x == 0) p.done[blockIdx.y * kMuonCountPitch] = 0;
     }
 }
 

@@ -1911,7 +1911,7 @@ MuonSpace muon_space(int64_t n, int64_t R, int64_t C)
     w.p = w.s + up(n * m * muon_pitch(m) * 2);
     w.part = w.p + up(n * m * muon_pitch(m) * 2);
     w.done = w.part + up(n * muon_parts(R * C / 8) * 8);
-    w.bytes = w.done + up(n * 4);
+    w.bytes = w.done + up(n * 4 * kMuonCountPitch);
     return w;
 }
 

@@ -37,7 +37,7 @@ struct NsParams {
     float gram_alpha, poly_alpha, poly_beta, poly_diag, step_alpha, last_alpha;
     __half *x[2], *s, *p;  // [n, R, ldx], [n, m, lds]
     int ldx, lds;          // of whole 128-byte pieces: rows of 776 as they are straddle the lines that their boxes are read from
-    unsigned *done;        // [n]: CTAs that have stored their part of a tile, over all phases
+    unsigned *done;        // [n], kMuonCountPitch apart: CTAs that have stored their part of a tile, over all phases
     void *out[kMuonBatch];
     int *status;
     unsigned long long timeout_ns;
@@ -55,8 +55,7 @@ struct NsCfg {
     static constexpr int WARP_ROWS = ROWS / 4;
     static constexpr int WARP_COLS = EDGE_ / (EPI_WARPS / 4);
     static constexpr int PIECES = WARP_COLS / 64;
-    static constexpr int COUNT_WARP = 2 + EPI_WARPS;  // counts finished tiles
-    static constexpr int THREADS = (3 + EPI_WARPS) * 32;
+    static constexpr int THREADS = (2 + EPI_WARPS) * 32;
     static constexpr uint32_t BOX_BYTES = WARP_ROWS * 128;  // a piece in staging
     static constexpr uint32_t STG_BYTES = EPI_WARPS * PIECES * BOX_BYTES;
     static constexpr int FIT = static_cast<int>((232448 - 512 - STG_BYTES) / (2 * OP_BYTES));
@@ -114,6 +113,12 @@ __device__ __forceinline__ unsigned ld_acquire_gpu(const unsigned *p)
 __device__ __forceinline__ void red_release_gpu(unsigned *p, unsigned v)
 {
     asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+__device__ __forceinline__ uint32_t atom_add_acq_rel_shared(uint32_t addr, uint32_t v)
+{
+    uint32_t old;
+    asm volatile("atom.acq_rel.cta.shared::cta.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(addr), "r"(v) : "memory");
+    return old;
 }
 // between plain accesses to global memory and those of the TMA unit, in either direction
 __device__ __forceinline__ void fence_proxy_async_global()
@@ -208,6 +213,30 @@ __device__ __forceinline__ bool ns_wait_done(const WaitCtx &w, int status0, cons
     }
 }
 
+// The same for a word in shared memory that another warp of the block raises.
+__device__ __forceinline__ bool ns_wait_word(const WaitCtx &w, uint32_t word, uint32_t need, int where)
+{
+    bool ok = true;
+    if (ptx::ld_shared_u32_volatile(word) < need) {
+        const uint64_t t0 = ptx::globaltimer_ns();
+        for (uint32_t it = 1; ptx::ld_shared_u32_volatile(word) < need; ++it) {
+            if ((it & 63u) != 0) continue;
+            ok = ptx::ld_shared_u32_volatile(w.abort_addr) == 0;
+            if (ok && ptx::globaltimer_ns() - t0 > w.timeout_ns) {
+                ok = false;
+                ptx::st_shared_u32_volatile(w.abort_addr, 1);
+                if (atomicCAS(w.status, 0, kStatusTimeout) == 0) {
+                    w.status[1] = where;
+                    w.status[2] = static_cast<int>(blockIdx.x);
+                }
+            }
+            if (!ok) break;
+        }
+    }
+    __threadfence_block();
+    return ok;
+}
+
 template <class Cfg>
 __global__ void __launch_bounds__(Cfg::THREADS, 1)
 newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_constant__ CUtensorMap tmX1,
@@ -238,9 +267,11 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
     const uint32_t tmem_slot = bar0 + 240;
     const uint32_t abort_addr = bar0 + 244;
     const uint32_t epi_abort_addr = bar0 + 248;
-    // Tile i's stores are out (one arrival per epilogue warp). Four barriers in turn: a warp arrives for tile i + 3 at the earliest
-    // when all have released the accumulator of tile i + 1, and so are done with tile i.
-    auto stored_bar = [&](uint32_t i) { return bar0 + 256u + 8u * (i & 3u); };
+    // Epilogue warps that have stored tile i. Four words in turn: a warp comes to tile i + 3 at the earliest when all have released the
+    // accumulator of tile i + 1, and so are done with tile i.
+    auto stored_word = [&](uint32_t i) { return bar0 + 256u + 4u * (i & 3u); };
+    // Tiles whose predecessors the producer has seen done; it only grows, as the producer may be many short tiles ahead.
+    const uint32_t ready_word = bar0 + 272u;
     static_assert(8 * (2 * STAGES + 4) <= 240, "barrier region");
 
     if (warp == 0) {
@@ -251,7 +282,8 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             ptx::mbar_init(tfull_bar(lane - STAGES), 1);
             ptx::mbar_init(tempty_bar(lane - STAGES), Cfg::EPI_WARPS * CG);
         }
-        if (lane >= 20 && lane < 24) ptx::mbar_init(stored_bar(static_cast<uint32_t>(lane)), Cfg::EPI_WARPS);
+        if (lane < 4) ptx::st_shared_u32_volatile(stored_word(static_cast<uint32_t>(lane)), 0);
+        if (lane == 4) ptx::st_shared_u32_volatile(ready_word, 0);
         if (lane == 31) {
             ptx::st_shared_u32_volatile(abort_addr, 0);
             ptx::st_shared_u32_volatile(epi_abort_addr, 0);
@@ -293,7 +325,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
         // ------------------------------------------------------------ TMA producer (every CTA)
         if (ptx::elect_one()) {
             int stage = 0;
-            uint32_t phase = 0;
+            uint32_t phase = 0, tile = 0;
             bool ok = true;
             for (int u = first_unit; u < p.units && ok; u += unit_stride) {
                 const NsUnit t = ns_unit(p, u);
@@ -305,9 +337,11 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 const int n0 = t.n_blk * Cfg::EDGE + static_cast<int>(rank) * Cfg::ROWS;
                 const int kblocks = t.phase == kNsGram ? p.kb_gram : p.kb_m;
                 const bool same = ns_same_operand(t);
-                ok = ns_wait_done(wctx, status0, p.done + t.z, t.need * CG, 700 + t.phase);
+                ok = ns_wait_done(wctx, status0, p.done + t.z * kMuonCountPitch, t.need * CG, 700 + t.phase);
                 if (!ok) break;
-                fence_proxy_async_global();  // the tiles were stored by plain stores
+                __threadfence_block();
+                ptx::st_shared_u32_volatile(ready_word, ++tile);
+                fence_proxy_async_global();  // the first X was stored by plain stores
                 for (int kb = 0; kb < kblocks; ++kb) {
                     ok = wait_barrier(wctx, empty_bar(stage), phase ^ 1u, 100 + stage);
                     if (!ok) break;
@@ -381,21 +415,6 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 }
             }
         }
-    } else if (warp == Cfg::COUNT_WARP) {
-        // ------------------------------------------------------------ count of finished tiles
-        // A tile part counts once all epilogue warps have seen their copies of it completed. One release per tile, by a warp that has nothing
-        // else to wait for.
-        if (ptx::elect_one()) {
-            const WaitCtx wctx_count{abort_addr, p.status, 3 * p.timeout_ns};
-            uint32_t tile = 0;
-            for (int u = first_unit; u < p.units; u += unit_stride, ++tile) {
-                const NsUnit t = ns_unit(p, u);
-                if (t.phase == kNsStep && t.step == p.steps - 1) break;  // nobody waits for the results themselves
-                if (!wait_barrier(wctx_count, stored_bar(tile), (tile >> 2) & 1u, 800)) break;
-                if (ptx::ld_shared_u32_volatile(epi_abort_addr) != 0) break;
-                red_release_gpu(p.done + t.z, 1);
-            }
-        }
     } else {
         // ------------------------------------------------------------ epilogue, warp by warp
         // A warp's pieces have a staging box each, which it stores by TMA copies of its own.
@@ -424,7 +443,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             bool ok = true;
             auto in_row = [&](int i) { return y0 + rr0 + i * 4 < M; };
             if (poly) {  // b S is added: the tile's part of S comes into staging while the product is formed
-                if (lane == 0) ok = ns_wait_done(wctx_epi, status0, p.done + t.z, t.need * CG, 710);
+                if (lane == 0) ok = ns_wait_word(wctx_epi, ready_word, tile + 1, 710);
                 __syncwarp();
                 // the lane's first 16 bytes; its rows lie 4 lds apart
                 const __half *src = p.s + (static_cast<long long>(t.z) * M + y0 + rr0) * p.lds + x0 + cc * 8;
@@ -530,7 +549,12 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
             }
             ptx::bulk_wait_group<0>();  // in memory; every lane: only the one that issued copies has any to wait for
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(stored_bar(tile));
+            // The warp that is the last to have its part of the tile in memory counts it for the others; nobody waits for the results.
+            if (lane == 0 && atom_add_acq_rel_shared(stored_word(tile), 1) == Cfg::EPI_WARPS - 1) {
+                ptx::st_shared_u32_volatile(stored_word(tile), 0);
+                if (!last && ptx::ld_shared_u32_volatile(epi_abort_addr) == 0) red_release_gpu(p.done + t.z * kMuonCountPitch, 1);
+            }
+            __syncwarp();
             ++tile;
             if (++acc == 2) {
                 acc = 0;

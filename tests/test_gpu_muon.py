@@ -49,8 +49,9 @@ def close(got, ref, name):
 
 
 # (matrices, rows, columns): tiles of 64 (a few matrices), of 128, of 256 (many), wide, tall and square ones, sides that end inside a
-# tile, inside a k-block and inside a piece of a tile; more matrices than one launch takes
-SHAPES = [(24, 776, 520), (18, 520, 776), (3, 520, 200), (2, 72, 776), (1, 8, 8), (1, 64, 64), (2, 16, 264), (2, 264, 16), (3, 136, 72), (1, 128, 256), (2, 256, 128), (1, 776, 1416),
+# tile, inside a k-block and inside a piece of a tile; more matrices than one launch takes; several short tiles of a phase per
+# block, which loads far ahead of what it computes
+SHAPES = [(28, 64, 2304), (28, 2304, 64), (32, 128, 1024), (32, 1024, 72), (32, 8, 4096), (24, 776, 520), (18, 520, 776), (3, 520, 200), (2, 72, 776), (1, 8, 8), (1, 64, 64), (2, 16, 264), (2, 264, 16), (3, 136, 72), (1, 128, 256), (2, 256, 128), (1, 776, 1416),
           (2, 1416, 776), (3, 768, 768), (1, 3072, 768), (33, 72, 136), (1, 2056, 2048), (12, 768, 768), (5, 264, 1000), (28, 520, 264)]
 
 
