@@ -339,7 +339,7 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
  * are accumulated in fp32. Rounding errors grow as small singular values do (485 times in five steps): against 64 bits the update is 1.2e-3 off
  * before its own rounding to bf16 for gradients of full rank (as of training: a few strong directions over noise), 2e-2 where singular values fall off
  * as 1/j^2. Coefficients that would carry singular values from [0, 1] out of the intermediates' range return NB_ERR_UNSUPPORTED.
- * An infinity or a NaN in a matrix makes its update NaN and touches no other matrix. With eps > 0 a zero matrix gives a
+ * An infinity or a NaN in a matrix makes its update NaN (steps > 0) and touches no other matrix. With eps > 0 a zero matrix gives a
  * zero update.
  * nb_muon_workspace returns -1 for sizes that the call would refuse.
  */
