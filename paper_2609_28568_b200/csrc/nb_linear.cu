@@ -2096,15 +2096,17 @@ int check_norm(int64_t BT, int64_t C, int stream_dtype)
     return NB_OK;
 }
 
-// Whether an output overlaps another output or an input, other than the two pairs that may be the same tensor.
-bool norm_overlap(const Span *w, int nw, const Span *r, int nr, const void *a, const void *a_in, const void *b, const void *b_in)
+// Whether an output overlaps another output or an input. The first two outputs may each be one input, the same tensor from its first byte on:
+// a thread reads there what it writes. That input and no other: a third argument at the same address (a weight, or rows of the other type)
+// is read by threads that do not own the element.
+bool norm_overlap(const Span *w, int nw, const Span *r, int nr, int first_may_be, int second_may_be)
 {
     for (int i = 0; i < nw; ++i) {
+        const int may_be = i == 0 ? first_may_be : i == 1 ? second_may_be : -1;
         for (int j = i + 1; j < nw; ++j)
             if (overlap(w[i], w[j])) return true;
         for (int j = 0; j < nr; ++j)
-            if (overlap(w[i], r[j]) && !((w[i].p == a && r[j].p == a_in && a == a_in) || (w[i].p == b && r[j].p == b_in && b == b_in)))
-                return true;
+            if (overlap(w[i], r[j]) && !(j == may_be && w[i].p == r[j].p)) return true;
     }
     return false;
 }
@@ -2610,7 +2612,7 @@ int nb_layernorm_forward(void *out, void *sum, void *mean, void *rstd, const voi
     const int64_t wide = BT * C * (stream_dtype == NB_DTYPE_F32 ? 4 : 2), narrow = BT * C * 2;
     const Span w[] = {{out, narrow, true}, {sum, wide, true}, {mean, 4 * BT, true}, {rstd, 4 * BT, true}},
                r[] = {{inp, wide, false}, {branch, narrow, false}, {weight, 2 * C, false}, {bias, 2 * C, false}};
-    if (norm_overlap(w, 4, r, 4, sum, inp, out, branch))
+    if (norm_overlap(w, 4, r, 4, 1, 0))  // out: branch, sum: inp
         return fail(NB_ERR_INVALID_ARG, "an output overlaps another argument (only sum may be inp, and out may be branch)");
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *s;
@@ -2666,7 +2668,7 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
                       {grads ? workspace : nullptr, nb_layernorm_workspace(BT, C), true}},
                r[] = {{dout, narrow, false}, {dres, wide, false}, {inp, wide, false}, {mean, 4 * BT, false}, {rstd, 4 * BT, false},
                       {weight, 2 * C, false}};
-    if (BT > 0 && norm_overlap(w, 5, r, 6, dinp, dres, dbranch, dout))
+    if (BT > 0 && norm_overlap(w, 5, r, 6, 1, 0))  // dinp: dres, dbranch: dout
         return fail(NB_ERR_INVALID_ARG, "an output overlaps another argument (only dinp may be dres, and dbranch may be dout)");
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *s;
