@@ -281,7 +281,7 @@ int nb_cast_f32_to_bf16(void *dst, const void *src, int64_t n, void *stream);
 /*
  * Layer norm with the residual add in front of it (paper: Figure 1, the two norms of a block and the last one, each in front of
  * a linear layer, behind the add of the layer before; Results/Speed names the add fused into the norm that follows it).
- * Rows of C elements, C a multiple of 8 and at most NB_LAYERNORM_MAX_C; BT is arbitrary.
+ * Rows of C elements, C a multiple of 8 and at most NB_LAYERNORM_MAX_C; BT below 2^31, BT * C at most 2^43.
  *
  * nb_layernorm_forward:
  *     s    = inp + branch, rounded to the stream's type (branch NULL: s = inp)

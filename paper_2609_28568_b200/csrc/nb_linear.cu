@@ -2084,6 +2084,10 @@ bool muon_in_range(int steps, double a, double b, double c)
     return true;
 }
 
+// Rows and elements that the norm takes: row numbers of 31 bits, 2^43 elements (no memory holds them, and offsets in bytes stay far
+// within 64 bits).
+bool norm_size_taken(int64_t BT, int64_t C) { return BT < (1ll << 31) && BT * C <= (1ll << 43); }
+
 int check_norm(int64_t BT, int64_t C, int stream_dtype)
 {
     if (BT < 0 || C <= 0) return fail(NB_ERR_INVALID_ARG, "negative or zero dimension");
@@ -2092,7 +2096,7 @@ int check_norm(int64_t BT, int64_t C, int stream_dtype)
     if (C % 8 != 0 || C > NB_LAYERNORM_MAX_C)
         return fail(NB_ERR_UNSUPPORTED, "C (%lld) must be a multiple of 8 and at most %d", static_cast<long long>(C),
                     NB_LAYERNORM_MAX_C);
-    if (BT >= (1ll << 31) || BT * C >= (1ll << 40)) return fail(NB_ERR_UNSUPPORTED, "dimension too large");
+    if (!norm_size_taken(BT, C)) return fail(NB_ERR_UNSUPPORTED, "dimension too large");
     return NB_OK;
 }
 
@@ -2644,7 +2648,7 @@ int nb_layernorm_forward(void *out, void *sum, void *mean, void *rstd, const voi
 
 int64_t nb_layernorm_workspace(int64_t BT, int64_t C)
 {
-    if (BT < 0 || C <= 0 || C % 8 != 0 || C > NB_LAYERNORM_MAX_C) return -1;
+    if (BT < 0 || C <= 0 || C % 8 != 0 || C > NB_LAYERNORM_MAX_C || !norm_size_taken(BT, C)) return -1;
     return static_cast<int64_t>(norm_blocks(BT, C)) * 2 * C * static_cast<int64_t>(sizeof(float));
 }
 
