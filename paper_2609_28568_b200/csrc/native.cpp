@@ -246,27 +246,32 @@ PyObject *linear_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// n device pointers from a sequence of tensors and addresses. Empty for None.
+// n device pointers from a sequence of tensors and addresses. Empty for None. The tensors are held until the call has been made: those
+// that an iterator makes have no other owner.
 struct Pointers {
     std::vector<void *> p;
-    bool given = false;
-    void **data() { return given ? p.data() : nullptr; }
+    PyObject *seq = nullptr;
+    Pointers() = default;
+    Pointers(const Pointers &) = delete;
+    Pointers &operator=(const Pointers &) = delete;
+    ~Pointers() { Py_XDECREF(seq); }
+    void **data() { return seq ? p.data() : nullptr; }
 };
 bool to_pointers(PyObject *o, Pointers &v, int64_t n, const char *name, CurrentDevice &device)
 {
     if (o == Py_None) return true;
-    PyObject *seq = PySequence_Fast(o, "a sequence of tensors is wanted");
-    if (!seq) return false;
-    bool ok = PySequence_Fast_GET_SIZE(seq) == n;
-    if (!ok) PyErr_Format(PyExc_ValueError, "%s has %zd tensors, not %lld", name, PySequence_Fast_GET_SIZE(seq), static_cast<long long>(n));
-    if (ok) v.p.resize(static_cast<size_t>(n));
-    for (int64_t i = 0; ok && i < n; ++i) {
-        PyObject *t = PySequence_Fast_GET_ITEM(seq, i);
-        ok = to_pointer(t, v.p[static_cast<size_t>(i)]) && device.has(t);
+    v.seq = PySequence_Fast(o, "a sequence of tensors is wanted");
+    if (!v.seq) return false;
+    if (PySequence_Fast_GET_SIZE(v.seq) != n) {
+        PyErr_Format(PyExc_ValueError, "%s has %zd tensors, not %lld", name, PySequence_Fast_GET_SIZE(v.seq), static_cast<long long>(n));
+        return false;
     }
-    Py_DECREF(seq);
-    v.given = ok;
-    return ok;
+    v.p.resize(static_cast<size_t>(n));
+    for (int64_t i = 0; i < n; ++i) {
+        PyObject *t = PySequence_Fast_GET_ITEM(v.seq, i);
+        if (!to_pointer(t, v.p[static_cast<size_t>(i)]) || !device.has(t)) return false;
+    }
+    return true;
 }
 bool to_stream_or_current(PyObject *const *args, Py_ssize_t n, Py_ssize_t at, void *&stream)
 {
