@@ -83,7 +83,7 @@ struct MuonPrepare {
     float *momentum[kMuonBatch];   // or all null
     void *out[kMuonBatch];         // muon_normalise_kernel with no step to follow: bf16 results
     double *part;                  // [n][parts]
-    unsigned *done;                // [n], zeroed for the products' counts
+    unsigned *done;                // [n + 1], zeroed: the products' counts, and the word that says that one of their blocks failed
     __half *x;                     // [n][rows][8 pitch], times `scale`
     long long nvec;                // elements / 8
     int row_vec, pitch;            // vectors of eight in a row, and from one row of x to the next
@@ -185,6 +185,7 @@ muon_momentum_kernel(const __grid_constant__ MuonPrepare p)
     if (threadIdx.x == 0) {
         p.part[static_cast<long long>(blockIdx.y) * p.parts + blockIdx.x] = sq;
         if (blockIdx.x == 0) p.done[blockIdx.y * kMuonCountPitch] = 0;
+        if (blockIdx.x == 0 && blockIdx.y == 0) p.done[gridDim.y * kMuonCountPitch] = 0;
     }
 }
 

@@ -1888,8 +1888,8 @@ int with_norm_form(const NormForm &f, F &&fn)
 }
 
 // ----------------------------------------------------------------------------- orthogonalised momentum
-// The workspace of a group of at most kMuonBatch matrices: two of the iterate, S, P (all fp16), the norms' partial sums
-// and the counts of tiles done.
+// The workspace of a group of at most kMuonBatch matrices: two of the iterate, S, P (all fp16), the norms' partial sums,
+// the counts of tiles done, and the word of failure behind them.
 struct MuonSpace {
     int64_t x[2], s, p, part, done, bytes;
 };
@@ -1911,7 +1911,7 @@ MuonSpace muon_space(int64_t n, int64_t R, int64_t C)
     w.p = w.s + up(n * m * muon_pitch(m) * 2);
     w.part = w.p + up(n * m * muon_pitch(m) * 2);
     w.done = w.part + up(n * muon_parts(R * C / 8) * 8);
-    w.bytes = w.done + up(n * 4 * kMuonCountPitch);
+    w.bytes = w.done + up((n + 1) * 4 * kMuonCountPitch);
     return w;
 }
 
@@ -2038,6 +2038,7 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
     p.s = reinterpret_cast<__half *>(q.workspace + w.s);
     p.p = reinterpret_cast<__half *>(q.workspace + w.p);
     p.done = pr.done;
+    p.failed = pr.done + n * kMuonCountPitch;
     for (int i = 0; i < n; ++i) p.out[i] = q.update[at + i];
     p.status = s.status;
     p.timeout_ns = kDefaultTimeoutNs;

@@ -38,6 +38,7 @@ struct NsParams {
     __half *x[2], *s, *p;  // [n, R, ldx], [n, m, lds]
     int ldx, lds;          // of whole 128-byte pieces: rows of 776 as they are straddle the lines that their boxes are read from
     unsigned *done;        // [n], kMuonCountPitch apart: CTAs that have stored their part of a tile, over all phases
+    unsigned *failed;      // raised by a block that gives up: what the others wait for will not come
     void *out[kMuonBatch];
     int *status;
     unsigned long long timeout_ns;
@@ -187,17 +188,16 @@ __device__ __forceinline__ bool ns_same_operand(const NsUnit &t)
     return t.phase != kNsStep && t.m_blk == t.n_blk;
 }
 
-// Waits, for a limited time, until `need` tile parts of a matrix are stored.
-// status0: the status word as the launch found it.
-__device__ __forceinline__ bool ns_wait_done(const WaitCtx &w, int status0, const unsigned *done, unsigned need, int where)
+// Waits, for a limited time, until `need` tile parts of a matrix are stored. Another block's failure ends this one too. It is told by a
+// word of this launch: the device's status word is written by other launches, and cleared by the host, while this one runs.
+__device__ __forceinline__ bool ns_wait_done(const WaitCtx &w, const unsigned *failed, const unsigned *done, unsigned need, int where)
 {
     if (ld_acquire_gpu(done) >= need) return true;
     const uint64_t t0 = ptx::globaltimer_ns();
     for (uint32_t it = 1;; ++it) {
         if (ld_acquire_gpu(done) >= need) return true;
         if ((it & 15u) == 0) {
-            // another block's failure ends this one too: what it waits for will not come
-            if (ptx::ld_shared_u32_volatile(w.abort_addr) != 0 || *reinterpret_cast<volatile int *>(w.status) != status0) {
+            if (ptx::ld_shared_u32_volatile(w.abort_addr) != 0 || ld_acquire_gpu(failed) != 0) {
                 ptx::st_shared_u32_volatile(w.abort_addr, 1);
                 return false;
             }
@@ -312,7 +312,6 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
     const uint32_t tmem_base = ptx::ld_shared_u32_volatile(tmem_slot);
     const WaitCtx wctx{abort_addr, p.status, p.timeout_ns};
     const WaitCtx wctx_epi{abort_addr, p.status, 2 * p.timeout_ns};
-    const int status0 = *reinterpret_cast<volatile int *>(p.status);
 
     auto load = [&](uint32_t dst, const CUtensorMap *m, uint32_t bar, int x, int y, int z) {
         if (CG == 2) tma_load_3d_pair(dst, m, bar, x, y, z);
@@ -337,7 +336,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 const int n0 = t.n_blk * Cfg::EDGE + static_cast<int>(rank) * Cfg::ROWS;
                 const int kblocks = t.phase == kNsGram ? p.kb_gram : p.kb_m;
                 const bool same = ns_same_operand(t);
-                ok = ns_wait_done(wctx, status0, p.done + t.z * kMuonCountPitch, t.need * CG, 700 + t.phase);
+                ok = ns_wait_done(wctx, p.failed, p.done + t.z * kMuonCountPitch, t.need * CG, 700 + t.phase);
                 if (!ok) break;
                 __threadfence_block();
                 ptx::st_shared_u32_volatile(ready_word, ++tile);
@@ -565,6 +564,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
 
     // ---------------------------------------------------------------- common exit
     if (ptx::ld_shared_u32_volatile(abort_addr) != 0 || ptx::ld_shared_u32_volatile(epi_abort_addr) != 0) {
+        if (lane == 0) atomicExch(p.failed, 1u);
         const uint64_t t0 = ptx::globaltimer_ns();  // copies and MMAs in flight land first
         while (ptx::globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     }
