@@ -503,6 +503,15 @@ int nb_debug_wait_timeout(int64_t limit_us);
  */
 int nb_debug_gemm_timeout(void *out, const void *inp, const void *weight, int64_t limit_us);
 
+/*
+ * The same for the layer norm's rows that come by copies: a pass over [5000, 64] bf16 (forward: inp to out; backward: inp as both
+ * dout and the normed sum, out as dinp) whose rows wait for 16 bytes more than their copies bring. Every team's bounded wait runs out after
+ * `limit_us` microseconds (100 .. 1000000); nothing is stored, and the blocks leave when copies have had time to land.
+ * nb_check_status() reports NB_ERR_TIMEOUT naming wait 811 (backward: 810). stats: [5000] fp32, read as mean and rstd in the backward pass.
+ */
+int nb_debug_layernorm_timeout(void *out, const void *inp, const void *weight, const void *stats, int backward,
+                               int64_t limit_us);
+
 #ifdef __cplusplus
 }
 #endif

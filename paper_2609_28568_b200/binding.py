@@ -30,7 +30,7 @@ EXPORTS = (
     "nb_lora_linear_forward", "nb_lora_linear_backward", "nb_debug_layer_bwd_plan", "nb_debug_gemm_timeout",
     "nb_lora_down_stacked", "nb_lora_linear_forward_stacked", "nb_lora_linear_backward_stacked",
     "nb_lora_da_stacked", "nb_debug_route", "nb_layernorm_forward", "nb_layernorm_workspace", "nb_layernorm_backward",
-    "nb_muon_workspace", "nb_muon_update", "nb_muon_apply",
+    "nb_muon_workspace", "nb_muon_update", "nb_muon_apply", "nb_debug_layernorm_timeout",
 )
 
 CALL_FORWARD, CALL_BACKWARD, CALL_LORA_FORWARD, CALL_LORA_BACKWARD = range(4)
@@ -90,6 +90,7 @@ def lib() -> ctypes.CDLL:
         L.nb_muon_apply.argtypes = [ctypes.POINTER(_vp)] * 3 + [_i64] * 2 + [ctypes.c_float] * 2 + [_vp]
         L.nb_debug_split_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int)]
         L.nb_debug_gemm_timeout.argtypes = [_vp, _vp, _vp, _i64]
+        L.nb_debug_layernorm_timeout.argtypes = [_vp, _vp, _vp, _vp, _int, _i64]
         L.nb_debug_layer_bwd_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int), _i64]
         L.nb_debug_route.argtypes = [_int] + [_i64] * 4 + [_int] * 3 + [ctypes.POINTER(_int)]
         _lib = L
@@ -346,6 +347,12 @@ def nb_debug_gemm_timeout(out, inp, weight, limit_us: int) -> None:
     """One-tile forward GEMM whose producer stops half way: exercises the kernel's time-out exit."""
     lib().nb_set_stream(_stream())
     _check(lib().nb_debug_gemm_timeout(_ptr(out), _ptr(inp), _ptr(weight), limit_us))
+
+
+def nb_debug_layernorm_timeout(out, inp, weight, stats, backward: bool, limit_us: int) -> None:
+    """A layer norm of [5000, 64] whose rows never come whole: exercises the kernels' time-out exit."""
+    lib().nb_set_stream(_stream())
+    _check(lib().nb_debug_layernorm_timeout(_ptr(out), _ptr(inp), _ptr(weight), _ptr(stats), int(backward), limit_us))
 
 
 def nb_debug_wait_timeout(limit_us: int) -> None:

@@ -1849,7 +1849,7 @@ int launch_norm(DeviceState &s, void (*kernel)(P), P p, int row_bytes, int sums,
     }
     if (f.teams == 1) sums = 0;
     p.status = s.status;
-    p.timeout_ns = kDefaultTimeoutNs;
+    if (p.timeout_ns == 0) p.timeout_ns = kDefaultTimeoutNs;
     return launch_chained_smem(kernel, dim3(static_cast<unsigned>(blocks)), f.threads * f.teams,
                                static_cast<size_t>(rows > f.teams * sums ? rows : f.teams * sums), stream, p);
 }
@@ -2989,6 +2989,44 @@ int nb_debug_gemm_timeout(void *out, const void *inp, const void *weight, int64_
     a.debug_stop_kb = 2;  // the first two k-blocks are loaded, the third never is
     a.debug_timeout_ns = static_cast<unsigned long long>(limit_us) * 1000ull;
     return launch_gemm<FwdStore1>(*s, a, g_stream);
+}
+
+int nb_debug_layernorm_timeout(void *out, const void *inp, const void *weight, const void *stats, int backward, int64_t limit_us)
+{
+    if (!out || !inp || !weight || !stats) return fail(NB_ERR_INVALID_ARG, "out, inp, weight and stats must not be NULL");
+    if (!aligned16(out) || !aligned16(inp) || !aligned16(weight) || !aligned16(stats))
+        return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+    if (limit_us < 100 || limit_us > 1000000)
+        return fail(NB_ERR_INVALID_ARG, "limit_us must be within [100, 1000000]");
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    int rc = get_state(&s);
+    if (rc != NB_OK) return rc;
+    const int64_t BT = 5000, C = 64;  // two or three rows for each of 2368 teams
+    auto launch = [&](auto p, auto run) {
+        p.inp = inp;
+        p.weight = weight;
+        p.BT = BT;
+        p.nvec = static_cast<int>(C / 8);
+        p.inv_c = 1.0f / static_cast<float>(C);
+        p.withhold = 16;
+        p.timeout_ns = static_cast<unsigned long long>(limit_us) * 1000ull;
+        return run(p);
+    };
+    if (backward) {
+        NormBackward p{};
+        p.dinp = out;
+        p.dout = inp;
+        p.mean = p.rstd = static_cast<const float *>(stats);
+        rc = launch(p, [&](const NormBackward &q) { return launch_norm_backward<false, 32, 1, false>(*s, q, g_stream); });
+    } else {
+        NormForward p{};
+        p.out = out;
+        rc = launch(p, [&](const NormForward &q) { return launch_norm_forward<false, 32, 1, false>(*s, q, g_stream); });
+    }
+    if (rc != NB_OK) return rc;
+    ++g_launches;
+    return NB_OK;
 }
 
 int nb_debug_wait_timeout(int64_t limit_us)

@@ -180,6 +180,13 @@ __device__ __forceinline__ Raw8<F32> shared8(uint32_t base, int vec)
     return r;
 }
 
+// Where a wait ran out: copies that are still under way write the block's shared memory, so it stays until they have landed.
+__device__ __forceinline__ void norm_leave()
+{
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (ptx::globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+}
+
 struct NormForward {
     void *out;           // bf16
     void *sum;           // stream's type, or null where there is no branch
@@ -192,8 +199,9 @@ struct NormForward {
     int nvec;            // C / 8
     int slots;           // rows that a team has in shared memory
     float inv_c, eps;
+    int withhold;        // nb_debug_layernorm_timeout only: bytes that every row waits for and that never come; else 0
     int *status;
-    unsigned long long timeout_ns;
+    unsigned long long timeout_ns;  // 0: the usual limit
 };
 // Shared memory of a row of the forward pass: inp, branch (if there is one).
 __host__ __device__ constexpr int norm_forward_row_bytes(bool f32, int nvec, bool has_branch) { return nvec * ((f32 ? 32 : 16) + (has_branch ? 16 : 0)); }
@@ -227,7 +235,7 @@ layernorm_forward_kernel(const NormForward p)
     const long long first = static_cast<long long>(blockIdx.x) * teams + team;
     auto fetch = [&](long long row, int slot) {  // one thread of the team
         const uint32_t dst = ring.at + static_cast<uint32_t>(slot) * row_bytes, b = ring.bar + 8u * slot;
-        ptx::mbar_expect_tx(b, row_bytes);
+        ptx::mbar_expect_tx(b, row_bytes + static_cast<uint32_t>(p.withhold));
         bulk_load(dst, static_cast<const uint8_t *>(p.inp) + row * x_bytes, x_bytes, b);
         if (has_branch) bulk_load(dst + x_bytes, static_cast<const uint8_t *>(p.branch) + row * branch_bytes, branch_bytes, b);
     };
@@ -254,9 +262,11 @@ layernorm_forward_kernel(const NormForward p)
         }
     }
     int turn = 0;
+    bool ok = true;  // a thread that gave up goes on with its team, which meets at barriers, but waits, fetches and stores no more
     for (long long row = first; row < p.BT; row += stride) {
-        bool ok = true;
-        if constexpr (!DIRECT) ok = wait_barrier(wctx, ring.full(), ring.phase, 811);
+        if constexpr (!DIRECT) {
+            if (!ptx::mbar_try_wait(ring.full(), ring.phase)) ok = ok && wait_barrier(wctx, ring.full(), ring.phase, 811);
+        }
         Pairs v[NV];
         ptx::f2 sum = both(0.0f);
 #pragma unroll
@@ -311,6 +321,9 @@ layernorm_forward_kernel(const NormForward p)
             p.rstd[row] = rstd;
         }
     }
+    if constexpr (!DIRECT) {
+        if (!ok) norm_leave();
+    }
 }
 
 struct NormBackward {
@@ -326,6 +339,7 @@ struct NormBackward {
     int nvec;
     int slots;            // rows that a team has in shared memory
     float inv_c;
+    int withhold;         // as in the forward pass
     int *status;
     unsigned long long timeout_ns;
 };
@@ -363,7 +377,7 @@ layernorm_backward_kernel(const NormBackward p)
     const long long first = static_cast<long long>(blockIdx.x) * teams + team;
     auto fetch = [&](long long row, int slot) {  // one thread of the team
         const uint32_t dst = ring.at + static_cast<uint32_t>(slot) * row_bytes, b = ring.bar + 8u * slot;
-        ptx::mbar_expect_tx(b, row_bytes);
+        ptx::mbar_expect_tx(b, row_bytes + static_cast<uint32_t>(p.withhold));
         bulk_load(dst, static_cast<const uint8_t *>(p.dout) + row * dout_bytes, dout_bytes, b);
         bulk_load(dst + dout_bytes, static_cast<const uint8_t *>(p.inp) + row * x_bytes, x_bytes, b);
         if (has_res) bulk_load(dst + dout_bytes + x_bytes, static_cast<const uint8_t *>(p.dres) + row * x_bytes, x_bytes, b);
@@ -397,14 +411,16 @@ layernorm_backward_kernel(const NormBackward p)
         rstd = __ldcg(p.rstd + first);
     }
     int turn = 0;
+    bool ok = true;  // a thread that gave up goes on with its team, which meets at barriers, but waits, fetches and stores no more
     for (long long row = first; row < p.BT; row += stride) {
         const float mu = mean, rs = rstd;
         if (row + stride < p.BT) {
             mean = __ldcg(p.mean + row + stride);
             rstd = __ldcg(p.rstd + row + stride);
         }
-        bool ok = true;
-        if constexpr (!DIRECT) ok = wait_barrier(wctx, ring.full(), ring.phase, 810);
+        if constexpr (!DIRECT) {
+            if (!ptx::mbar_try_wait(ring.full(), ring.phase)) ok = ok && wait_barrier(wctx, ring.full(), ring.phase, 810);
+        }
         const uint32_t src = ring.row();
         auto get_dout = [&](int i) {
             if constexpr (DIRECT) return dd[i];
@@ -465,6 +481,9 @@ layernorm_backward_kernel(const NormBackward p)
         team_sync<T>(team);  // the slot has been read
         if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, ring.slot);
         ring.next();
+    }
+    if constexpr (!DIRECT) {
+        if (!ok) norm_leave();
     }
     if (p.part == nullptr) return;
     __syncthreads();  // every row has been read: the same memory holds the sums now
