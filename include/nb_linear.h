@@ -512,6 +512,15 @@ int nb_debug_gemm_timeout(void *out, const void *inp, const void *weight, int64_
 int nb_debug_layernorm_timeout(void *out, const void *inp, const void *weight, const void *stats, int backward,
                                int64_t limit_us);
 
+/*
+ * The same for the blocks of an update, which wait for one another's tiles: two steps for one fp32 matrix [128, 128] without
+ * momentum, in which every tile of P waits for one tile of S more than there are. Blocks stop issuing work, tell the others, let what is
+ * under way land, free tensor memory and leave. `update` is left unwritten; nb_check_status() reports NB_ERR_TIMEOUT naming wait 701 (for P) or 702
+ * (for X, whose tiles wait for those of P).
+ * workspace: nb_muon_workspace(1, 128, 128) bytes, 128-byte aligned.
+ */
+int nb_debug_muon_timeout(void *update, const void *grad, void *workspace, int64_t workspace_bytes, int64_t limit_us);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,6 +31,7 @@ EXPORTS = (
     "nb_lora_down_stacked", "nb_lora_linear_forward_stacked", "nb_lora_linear_backward_stacked",
     "nb_lora_da_stacked", "nb_debug_route", "nb_layernorm_forward", "nb_layernorm_workspace", "nb_layernorm_backward",
     "nb_muon_workspace", "nb_muon_update", "nb_muon_apply", "nb_debug_layernorm_timeout",
+    "nb_debug_muon_timeout",
 )
 
 CALL_FORWARD, CALL_BACKWARD, CALL_LORA_FORWARD, CALL_LORA_BACKWARD = range(4)
@@ -91,6 +92,7 @@ def lib() -> ctypes.CDLL:
         L.nb_debug_split_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int)]
         L.nb_debug_gemm_timeout.argtypes = [_vp, _vp, _vp, _i64]
         L.nb_debug_layernorm_timeout.argtypes = [_vp, _vp, _vp, _vp, _int, _i64]
+        L.nb_debug_muon_timeout.argtypes = [_vp, _vp, _vp, _i64, _i64]
         L.nb_debug_layer_bwd_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int), _i64]
         L.nb_debug_route.argtypes = [_int] + [_i64] * 4 + [_int] * 3 + [ctypes.POINTER(_int)]
         _lib = L
@@ -353,6 +355,12 @@ def nb_debug_layernorm_timeout(out, inp, weight, stats, backward: bool, limit_us
     """A layer norm of [5000, 64] whose rows never come whole: exercises the kernels' time-out exit."""
     lib().nb_set_stream(_stream())
     _check(lib().nb_debug_layernorm_timeout(_ptr(out), _ptr(inp), _ptr(weight), _ptr(stats), int(backward), limit_us))
+
+
+def nb_debug_muon_timeout(update, grad, workspace, workspace_bytes: int, limit_us: int) -> None:
+    """An update of one matrix [128, 128] whose tiles never come whole: exercises the time-out exit of blocks that wait for one another."""
+    lib().nb_set_stream(_stream())
+    _check(lib().nb_debug_muon_timeout(_ptr(update), _ptr(grad), _ptr(workspace), workspace_bytes, limit_us))
 
 
 def nb_debug_wait_timeout(limit_us: int) -> None:

@@ -1977,6 +1977,8 @@ struct MuonCall {
     float a, b, c, eps;
     bool grad_f32;
     unsigned char *workspace;
+    int debug_withhold;                   // nb_debug_muon_timeout only: see NsParams
+    unsigned long long debug_timeout_ns;  // 0: the usual limit
 };
 
 // A group of n <= kMuonBatch matrices, from the at-th on.
@@ -2040,8 +2042,9 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
     p.done = pr.done;
     p.failed = pr.done + n * kMuonCountPitch;
     for (int i = 0; i < n; ++i) p.out[i] = q.update[at + i];
+    p.withhold = q.debug_withhold;
     p.status = s.status;
-    p.timeout_ns = kDefaultTimeoutNs;
+    p.timeout_ns = q.debug_timeout_ns ? q.debug_timeout_ns : kDefaultTimeoutNs;
     // Pairs of CTAs on 256 x 256 tiles where X has two of them for every pair. Below that the chain of a phase counts, which is shorter with
     // CTAs on 128 x 128 tiles (at twice the reads), and shorter yet on 64 x 64 (at four times) where these are two per SM at most. Measured, us (64,
     // 128, 256): 768 x 768 (144 tiles of 64) 86, 97, 130; 12 x 128 x 512 (192) 62, 68, 91; 2 x 768 x 768 (288) 97, 99, 132; 28 x 256 x 256 (448)
@@ -2762,7 +2765,7 @@ int nb_muon_update(void *const *update, void *const *momentum, const void *const
     int rc = get_state(&s);
     if (rc != NB_OK) return rc;
     const MuonCall q{update, momentum, grad, R, C, mu, nesterov, steps, a, b, c, eps, grad_dtype == NB_DTYPE_F32,
-                     static_cast<unsigned char *>(workspace)};
+                     static_cast<unsigned char *>(workspace), 0, 0};
     for (int64_t at = 0; at < n; at += kMuonBatch)
         if ((rc = run_muon(*s, q, at, static_cast<int>(n - at < kMuonBatch ? n - at : kMuonBatch), static_cast<cudaStream_t>(stream_))) != NB_OK)
             return rc;
@@ -3027,6 +3030,25 @@ int nb_debug_layernorm_timeout(void *out, const void *inp, const void *weight, c
     if (rc != NB_OK) return rc;
     ++g_launches;
     return NB_OK;
+}
+
+int nb_debug_muon_timeout(void *update, const void *grad, void *workspace, int64_t workspace_bytes, int64_t limit_us)
+{
+    const int64_t n = 128;
+    if (!update || !grad || !workspace) return fail(NB_ERR_INVALID_ARG, "update, grad and workspace must not be NULL");
+    if (!aligned16(update) || !aligned16(grad) || (reinterpret_cast<uintptr_t>(workspace) & 127u))
+        return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, the workspace 128-byte aligned");
+    if (workspace_bytes < muon_space(1, n, n).bytes)
+        return fail(NB_ERR_INVALID_ARG, "a workspace of %lld bytes is needed", static_cast<long long>(muon_space(1, n, n).bytes));
+    if (limit_us < 100 || limit_us > 1000000)
+        return fail(NB_ERR_INVALID_ARG, "limit_us must be within [100, 1000000]");
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    int rc = get_state(&s);
+    if (rc != NB_OK) return rc;
+    const MuonCall q{&update, nullptr, &grad, n, n, 0.0f, 0, 2, 1.5f, -0.5f, 0.0f, 1e-7f, true, static_cast<unsigned char *>(workspace),
+                     1, static_cast<unsigned long long>(limit_us) * 1000ull};
+    return run_muon(*s, q, 0, 1, g_stream);
 }
 
 int nb_debug_wait_timeout(int64_t limit_us)

@@ -40,6 +40,7 @@ struct NsParams {
     unsigned *done;        // [n], kMuonCountPitch apart: CTAs that have stored their part of a tile, over all phases
     unsigned *failed;      // raised by a block that gives up: what the others wait for will not come
     void *out[kMuonBatch];
+    int withhold;          // nb_debug_muon_timeout only: tiles that P's tiles wait for beside those that come; else 0
     int *status;
     unsigned long long timeout_ns;
 };
@@ -145,7 +146,7 @@ __device__ __forceinline__ NsUnit ns_unit(const NsParams &p, int u)
         t.phase = r < sym ? kNsGram : kNsPoly;
         if (t.phase == kNsPoly) {
             r -= sym;
-            t.need += p.sym_tiles;
+            t.need += p.sym_tiles + p.withhold;
         }
         t.z = r / p.sym_tiles;
         const int k = r - t.z * p.sym_tiles;  // through the lower triangle row by row
@@ -310,8 +311,10 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
     else __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem_base = ptx::ld_shared_u32_volatile(tmem_slot);
+    // the wait nearest the cause of a stall is the one that runs out: the producer's for other blocks, then the issuer's, then the epilogue's
     const WaitCtx wctx{abort_addr, p.status, p.timeout_ns};
-    const WaitCtx wctx_epi{abort_addr, p.status, 2 * p.timeout_ns};
+    const WaitCtx wctx_mma{abort_addr, p.status, 2 * p.timeout_ns};
+    const WaitCtx wctx_epi{abort_addr, p.status, 3 * p.timeout_ns};
 
     auto load = [&](uint32_t dst, const CUtensorMap *m, uint32_t bar, int x, int y, int z) {
         if (CG == 2) tma_load_3d_pair(dst, m, bar, x, y, z);
@@ -378,12 +381,12 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
                 const NsUnit t = ns_unit(p, u);
                 const int kblocks = t.phase == kNsGram ? p.kb_gram : p.kb_m;
                 const bool same = ns_same_operand(t);
-                ok = wait_barrier(wctx, tempty_bar(acc), acc_phase ^ 1u, 200 + acc);
+                ok = wait_barrier(wctx_mma, tempty_bar(acc), acc_phase ^ 1u, 200 + acc);
                 if (!ok) break;
                 ptx::tc_fence_after();
                 const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * Cfg::EDGE);
                 for (int kb = 0; kb < kblocks; ++kb) {
-                    ok = wait_barrier(wctx, full_bar(stage), phase, 300 + stage);
+                    ok = wait_barrier(wctx_mma, full_bar(stage), phase, 300 + stage);
                     if (!ok) break;
                     ptx::tc_fence_after();
                     const uint32_t sa = smem + stage * Cfg::OP_BYTES;
