@@ -76,8 +76,8 @@ muon_apply_kernel(const __grid_constant__ MuonApply p)
 }
 
 // What comes ahead of the products: m <- mu m + g (fp32, in place; without momentum the gradient itself is taken), v = g + mu m (nesterov)
-// or m, and |v|^2 per matrix. Squares are summed in 64 bits, which hold those of every fp32 value: a gradient of
-// 1e-30 or 1e30 is normalised like any other. In a fixed order: one partial sum per block, added up by whoever needs the norm.
+// or m, and |v|^2 per matrix. Squares are summed in 64 bits, which hold those of every fp32 value: the norm of a gradient of 1e-30 or
+// 1e30 is as exact as any other's. In a fixed order: one partial sum per block, added up by whoever needs the norm.
 struct MuonPrepare {
     const void *grad[kMuonBatch];  // fp32 or bf16
     float *momentum[kMuonBatch];   // or all null
@@ -190,7 +190,8 @@ muon_momentum_kernel(const __grid_constant__ MuonPrepare p)
 }
 
 // x = fp16(scale v / (|v| + eps)); v from the momentum as the launch before left it. The division is by a 64-bit factor, so that it neither
-// overflows nor vanishes for gradients at either end of fp32.
+// overflows nor vanishes for gradients at either end of fp32. The scale is fixed: where eps exceeds |v| by so much that the values of x come below
+// 2^-14 / scale, fp16 holds them to 2^-25 / scale and no closer.
 template <bool G32, bool LAST>
 __global__ void __launch_bounds__(256)
 muon_normalise_kernel(const __grid_constant__ MuonPrepare p)
