@@ -296,7 +296,8 @@ int nb_cast_f32_to_bf16(void *dst, const void *src, int64_t n, void *stream);
  *   stream_dtype NB_DTYPE_BF16 or NB_DTYPE_F32
  * Statistics, deviations and products are held in fp32; s and out are rounded once each. sum may be inp, and out may be branch.
  * Any other overlap of an output with another argument is refused.
- * A row with an infinity or a NaN gives NaN in that row alone. BT == 0 does nothing.
+ * A row with an infinity or a NaN gives NaN in that row alone, as does one whose sum leaves fp32's range. One whose squared deviations
+ * add up past it (deviations of about 1e18 and more) is not normalised: rstd is 0 and out the bias. BT == 0 does nothing.
  *
  * nb_layernorm_backward, with s, mean and rstd of the forward pass, xh = (s - mean) * rstd and g = dout * weight:
  *     dinp    = dres + rstd * (g - mean_j(g) - xh * mean_j(g * xh))
