@@ -180,6 +180,14 @@ __device__ __forceinline__ Raw8<F32> shared8(uint32_t base, int vec)
     return r;
 }
 
+// Waits for a row's copy; not again once a thread of the block gave up. A team that gave up goes on through its rows, since its threads
+// meet at barriers, but no slot is filled again: its barrier may not have come to the end of its phase. (The failure held in a
+// variable over the rows instead: 29.6 us against 29.0 for 4096 x 4096 bf16 backward, 47.1 against 43.9 for 4096 x 8192 forward.)
+__device__ __forceinline__ bool norm_wait(const WaitCtx &w, const NormRing &ring, int where)
+{
+    return ptx::mbar_try_wait(ring.full(), ring.phase) ||
+           (ptx::ld_shared_u32_volatile(w.abort_addr) == 0 && wait_barrier(w, ring.full(), ring.phase, where));
+}
 // Where a wait ran out: copies that are still under way write the block's shared memory, so it stays until they have landed.
 __device__ __forceinline__ void norm_leave()
 {
@@ -231,6 +239,7 @@ layernorm_forward_kernel(const NormForward p)
     }
     chained_start();
     const WaitCtx wctx{ptx::smem_u32(&abort_flag), p.status, p.timeout_ns};
+    auto gave_up = [&] { return ptx::ld_shared_u32_volatile(wctx.abort_addr) != 0; };
     const long long stride = static_cast<long long>(gridDim.x) * teams;
     const long long first = static_cast<long long>(blockIdx.x) * teams + team;
     auto fetch = [&](long long row, int slot) {  // one thread of the team
@@ -262,11 +271,9 @@ layernorm_forward_kernel(const NormForward p)
         }
     }
     int turn = 0;
-    bool ok = true;  // a thread that gave up goes on with its team, which meets at barriers, but waits, fetches and stores no more
     for (long long row = first; row < p.BT; row += stride) {
-        if constexpr (!DIRECT) {
-            if (!ptx::mbar_try_wait(ring.full(), ring.phase)) ok = ok && wait_barrier(wctx, ring.full(), ring.phase, 811);
-        }
+        bool ok = true;
+        if constexpr (!DIRECT) ok = norm_wait(wctx, ring, 811);
         Pairs v[NV];
         ptx::f2 sum = both(0.0f);
 #pragma unroll
@@ -289,7 +296,7 @@ layernorm_forward_kernel(const NormForward p)
         if constexpr (!DIRECT) {
             if (T == 32) __syncwarp();
             // the whole team has read the slot
-            if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, ring.slot);
+            if (t == 0 && row + p.slots * stride < p.BT && ok && !gave_up()) fetch(row + p.slots * stride, ring.slot);
             ring.next();
         }
         const ptx::f2 minus = both(-mean);
@@ -322,7 +329,7 @@ layernorm_forward_kernel(const NormForward p)
         }
     }
     if constexpr (!DIRECT) {
-        if (!ok) norm_leave();
+        if (gave_up()) norm_leave();
     }
 }
 
@@ -371,6 +378,7 @@ layernorm_backward_kernel(const NormBackward p)
     }
     chained_start();
     const WaitCtx wctx{ptx::smem_u32(&abort_flag), p.status, p.timeout_ns};
+    auto gave_up = [&] { return ptx::ld_shared_u32_volatile(wctx.abort_addr) != 0; };
     const uint32_t dout_bytes = static_cast<uint32_t>(p.nvec) * 16u, x_bytes = dout_bytes * (F32 ? 2u : 1u);
 
     const long long stride = static_cast<long long>(gridDim.x) * teams;
@@ -411,16 +419,14 @@ layernorm_backward_kernel(const NormBackward p)
         rstd = __ldcg(p.rstd + first);
     }
     int turn = 0;
-    bool ok = true;  // a thread that gave up goes on with its team, which meets at barriers, but waits, fetches and stores no more
     for (long long row = first; row < p.BT; row += stride) {
+        bool ok = true;
         const float mu = mean, rs = rstd;
         if (row + stride < p.BT) {
             mean = __ldcg(p.mean + row + stride);
             rstd = __ldcg(p.rstd + row + stride);
         }
-        if constexpr (!DIRECT) {
-            if (!ptx::mbar_try_wait(ring.full(), ring.phase)) ok = ok && wait_barrier(wctx, ring.full(), ring.phase, 810);
-        }
+        if constexpr (!DIRECT) ok = norm_wait(wctx, ring, 810);
         const uint32_t src = ring.row();
         auto get_dout = [&](int i) {
             if constexpr (DIRECT) return dd[i];
@@ -479,11 +485,11 @@ layernorm_backward_kernel(const NormBackward p)
         }
         if constexpr (DIRECT) break;
         team_sync<T>(team);  // the slot has been read
-        if (t == 0 && row + p.slots * stride < p.BT && ok) fetch(row + p.slots * stride, ring.slot);
+        if (t == 0 && row + p.slots * stride < p.BT && ok && !gave_up()) fetch(row + p.slots * stride, ring.slot);
         ring.next();
     }
     if constexpr (!DIRECT) {
-        if (!ok) norm_leave();
+        if (gave_up()) norm_leave();
     }
     if (p.part == nullptr) return;
     __syncthreads();  // every row has been read: the same memory holds the sums now
