@@ -341,7 +341,7 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
  * before its own rounding to bf16 for gradients of full rank (as of training: a few strong directions over noise), 2e-2 where singular values fall off
  * as 1/j^2. Beside that a value is off by up to 2^-37 times what the steps multiply small ones by, 5e-9 in five steps: nothing next to an
  * orthogonal update, but more than 1e-3 of one that is itself below 2e-6 per element, as eps leaves it where |v| is a few millionths of eps or
- * less, and all of one where the values of v / eps are below 2^-38. Coefficients that would carry singular values from [0, 1] out of the intermediates' range return NB_ERR_UNSUPPORTED.
+ * less, and all of one where the values of v / eps are below 2^-37. Coefficients that would carry singular values from [0, 1] out of the intermediates' range return NB_ERR_UNSUPPORTED.
  * An infinity or a NaN in a matrix makes its update NaN (steps > 0) and touches no other matrix. With eps > 0 a zero matrix gives a
  * zero update.
  * nb_muon_workspace returns -1 for sizes that the call would refuse.

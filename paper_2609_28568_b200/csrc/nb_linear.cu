@@ -2045,11 +2045,14 @@ int run_muon(DeviceState &s, const MuonCall &q, int64_t at, int n, cudaStream_t 
     p.withhold = q.debug_withhold;
     p.status = s.status;
     p.timeout_ns = q.debug_timeout_ns ? q.debug_timeout_ns : kDefaultTimeoutNs;
-    // Pairs of CTAs on 256 x 256 tiles where X has two of them for every pair. Below that the chain of a phase counts, which is shorter with
-    // CTAs on 128 x 128 tiles (at twice the reads), and shorter yet on 64 x 64 (at four times) where these are two per SM at most. Measured, us (64,
-    // 128, 256): 768 x 768 (144 tiles of 64) 86, 97, 130; 12 x 128 x 512 (192) 62, 68, 91; 2 x 768 x 768 (288) 97, 99, 132; 28 x 256 x 256 (448)
-    // 77, 75, 97; 4 x 768 x 768 (576) 150, 106, 135; (128, 256): 4 x 3072 x 768 (144 tiles of 256) 206, 216; 16 x 768 x 768 (144) 199, 177;
-    // 6 x 2304 x 768 (162) 205, 206; 6 x 3072 x 768 (216) 251, 239; 28 x 1024 x 1024 (448) 775, 610.
+    // By the number of X's tiles. Pairs of CTAs on 256 x 256 tiles where X has two of them for every pair. Below that the chain of a phase
+    // counts, which is shorter with CTAs on 128 x 128 tiles (at twice the reads), and shorter yet on 64 x 64 (at four times) where these are two per
+    // SM at most. Measured, us (64, 128, 256; in brackets X's tiles of the size that decides): 64: 768 x 768 (144) 83, 95, 128; 12 x 128 x 512 (192)
+    // 60, 67, 89; 2 x 768 x 768 (288) 95, 97, 129. 128: 28 x 256 x 256 (448) 76, 73, 95; 4 x 768 x 768 (576) 144, 101, 134; 12 x 768 x 768 (108 of 256)
+    // 423, 153, 158; 4 x 3072 x 768 (144) 453, 205, 215. Pairs: 20 x 768 x 768 (180) 743, 250, 213; 28 x 1024 x 1024 (448) 2122, 830, 616;
+    // 6 x 3072 x 768 (216) 673, 249, 257. What the rule does not look at costs: the tiles of S and P (16 x 768 x 768, 144 tiles of 256: 128 x 128, 201
+    // against 188), and how much of its tiles a thin matrix fills, for which pairs are taken where CTAs on 128 x 128 are faster
+    // (28 x 2304 x 64: 143 against 101; 32 x 8 x 4096: 215, 143; 20 x 72 x 2000: 132, 93; 28 x 128 x 2304: 165, 118).
     auto tiles = [&](int edge) { return static_cast<long long>(n) * ((R + edge - 1) / edge) * ((C + edge - 1) / edge); };
     if (tiles(256) >= s.num_sms) return launch_ns<NsCfg<2, 256>>(s, p, stream);
     if (tiles(64) <= 2 * s.num_sms) return launch_ns<NsCfg<1, 64>>(s, p, stream);
