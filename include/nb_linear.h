@@ -338,8 +338,9 @@ int nb_layernorm_backward(void *dinp, void *dbranch, void *dweight, void *dbias,
  * An update or a momentum that overlaps another tensor or the workspace is refused. R and C are multiples of 8 and at most NB_MUON_MAX_DIM, n at most NB_MUON_MAX_N, steps at most 32.
  * m, v and the norm are held in fp32 and more; x, y and the polynomial between the products in fp16 at fixed powers of two, products
  * are accumulated in fp32. Rounding errors grow as small singular values do (485 times in five steps): against 64 bits the update is 1.2e-3 off
- * before its own rounding to bf16 for gradients of full rank (as of training: a few strong directions over noise), 2e-2 where singular values fall off
- * as 1/j^2. Beside that a value is off by up to 2^-37 times what the steps multiply small ones by, 5e-9 in five steps: nothing next to an
+ * before its own rounding to bf16 for gradients of full rank (as of training: a few strong directions over noise), up to 4e-3 where
+ * most singular values are alike (thin matrices, of 24 to 48 rows or columns before all: a step multiplies relative errors by up to five), 2e-2
+ * where they fall off as 1/j^2. Beside that a value is off by up to 2^-37 times what the steps multiply small ones by, 5e-9 in five steps: nothing next to an
  * orthogonal update, but more than 1e-3 of one that is itself below 2e-6 per element, as eps leaves it where |v| is a few millionths of eps or
  * less, and all of one where the values of v / eps are below 2^-37. Coefficients that would carry singular values from [0, 1] out of the intermediates' range return NB_ERR_UNSUPPORTED.
  * An infinity or a NaN in a matrix makes its update NaN (steps > 0) and touches no other matrix. With eps > 0 a zero matrix gives a
