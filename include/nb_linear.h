@@ -367,6 +367,36 @@ int nb_muon_apply(void *const *master, void *const *weight, const void *const *u
                   int64_t count, float decay, float step, void *stream);
 
 /*
+ * Attention over packed sequences (the step between the qkv linear and attn_proj; paper: Figure 1, the attention box of a block).
+ *
+ * Rows are tokens, T of them. Head h of a tensor is its columns [h D, (h + 1) D); rows lie ld elements apart, so that queries, keys and values may be
+ * columns of the one activation that a qkv linear wrote. Sequence i is the rows [cu_seqlens[i], cu_seqlens[i + 1]). Queries' head h reads head
+ * h / (heads / kv_heads) of keys and values. Per sequence and head, for a query i and the keys j of its sequence (causal: j <= i):
+ *
+ *     s_ij = scale q_i . k_j     lse_i = log sum_j exp(s_ij)     out_i = sum_j exp(s_ij - lse_i) v_j
+ *
+ *   out         [out] [T, heads, D] bf16
+ *   lse         [out] [heads, T] fp32, or NULL where no backward pass follows
+ *   q           [in]  [T, heads, D] bf16;  k, v [in] [T, kv_heads, D] bf16
+ *   cu_seqlens  [in]  [n + 1] int32 on the device, rising (equal neighbours: an empty sequence) within [0, T]; or NULL: n sequences of T / n rows.
+ *                     Rows in no sequence are neither used nor written. Bounds that fall or lie outside [0, T] are cut (nothing outside
+ *                     the tensors is touched, results are undefined) and nb_check_status reports NB_ERR_INVALID_ARG.
+ *   scale       positive and finite
+ * D a multiple of 8, at most NB_HEAD_MAX_D; heads a multiple of kv_heads, at most NB_HEAD_MAX_HEADS; ld_* multiples of 8, at least the row's width. Pointers 16-byte aligned (lse and cu_seqlens: 4).
+ * An output that overlaps another argument is refused (columns of one buffer with one ld do not overlap).
+ * Scores, their maximum and sum, and the output's sums are fp32; probabilities are rounded to bf16 for the product with v. T == 0 and n == 0 do nothing.
+ * What is not finite in one sequence, or in rows that belong to none, reaches no other sequence. Within a sequence an infinity or a NaN
+ * in v may reach the rows of the 128 before it too, which do not see it.
+ */
+#define NB_HEAD_MAX_D 128
+#define NB_HEAD_MAX_HEADS 1024
+#define NB_HEAD_MAX_T 2147483000ll
+#define NB_HEAD_MAX_LD (1ll << 32)
+int nb_attention_forward(void *out, void *lse, const void *q, const void *k, const void *v, const void *cu_seqlens, int64_t T, int64_t n,
+                         int64_t heads, int64_t kv_heads, int64_t D, int64_t ld_out, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                         float scale, int causal, void *stream);
+
+/*
  * Bias gradient of a GELU layer without any allocation (the paper has no counterpart; this
  * exists for callers that must not allocate device memory):
  *

@@ -31,7 +31,7 @@ EXPORTS = (
     "nb_lora_down_stacked", "nb_lora_linear_forward_stacked", "nb_lora_linear_backward_stacked",
     "nb_lora_da_stacked", "nb_debug_route", "nb_layernorm_forward", "nb_layernorm_workspace", "nb_layernorm_backward",
     "nb_muon_workspace", "nb_muon_update", "nb_muon_apply", "nb_debug_layernorm_timeout",
-    "nb_debug_muon_timeout",
+    "nb_debug_muon_timeout", "nb_attention_forward",
 )
 
 CALL_FORWARD, CALL_BACKWARD, CALL_LORA_FORWARD, CALL_LORA_BACKWARD = range(4)
@@ -89,6 +89,7 @@ def lib() -> ctypes.CDLL:
         L.nb_muon_update.argtypes = ([ctypes.POINTER(_vp)] * 3 + [_i64] * 3 + [ctypes.c_float, _int, _int] + [ctypes.c_float] * 4 +
                                      [_int, _vp, _i64, _vp])
         L.nb_muon_apply.argtypes = [ctypes.POINTER(_vp)] * 3 + [_i64] * 2 + [ctypes.c_float] * 2 + [_vp]
+        L.nb_attention_forward.argtypes = [_vp] * 6 + [_i64] * 9 + [ctypes.c_float, _int, _vp]
         L.nb_debug_split_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int)]
         L.nb_debug_gemm_timeout.argtypes = [_vp, _vp, _vp, _i64]
         L.nb_debug_layernorm_timeout.argtypes = [_vp, _vp, _vp, _vp, _int, _i64]
@@ -302,6 +303,14 @@ def nb_muon_update(update, momentum, grad, n, R, C, mu, nesterov, steps, a, b, c
 def nb_muon_apply(master, weight, update, n, count, decay, step, stream=None) -> None:
     """master <- decay * master - step * update, weight <- bf16(master), for n tensors of count elements given as sequences."""
     (_native or _load_native()).nb_muon_apply(master, weight, update, n, count, decay, step, stream)
+
+
+def nb_attention_forward(out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, ld_out, ld_q, ld_k, ld_v, scale, causal,
+                         stream=None) -> None:
+    """out = attention of q over k and v, per sequence and head; lse for the backward pass, or None. The tensors of heads may be columns
+    of wider ones, with rows ld elements apart."""
+    (_native or _load_native()).nb_attention_forward(out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, ld_out, ld_q, ld_k, ld_v,
+                                                     scale, int(causal), stream)
 
 
 def nb_debug_split_plan(M: int, N: int, K: int, slots: int, tile_m: int):

@@ -5,6 +5,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sysconfig
+import tempfile
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
@@ -14,8 +15,9 @@ NATIVE_PATH = os.path.join(_PKG, "_native.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared",
+    "-Xcompiler", "-fPIC",
 ]
+UNITS = ("nb_linear.cu", "attention.cu")
 
 
 def sources() -> list[str]:
@@ -34,15 +36,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Build ``libnb_linear.so`` and ``_native.so`` next to the package if they are missing or older than
     their sources."""
     if force or is_stale():
-        nvcc = os.environ.get("NVCC", "nvcc")
-        cmd = [nvcc, *NVCC_FLAGS, "-I", os.path.join(_ROOT, "include"), "-I", _CSRC,
-               "-o", LIB_PATH, os.path.join(_CSRC, "nb_linear.cu")]
-        if verbose:
-            cmd.insert(1, "-Xptxas")
-            cmd.insert(2, "-v")
-        subprocess.run(cmd, check=True)
+        _build_library(verbose)
         _build_native()
     return LIB_PATH
+
+
+def _build_library(verbose: bool) -> None:
+    """The translation units are compiled at the same time, then linked."""
+    nvcc = os.environ.get("NVCC", "nvcc")
+    flags = [*(["-Xptxas", "-v"] if verbose else []), *NVCC_FLAGS, "-I", os.path.join(_ROOT, "include"), "-I", _CSRC]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, u + ".o") for u in UNITS]
+        jobs = [subprocess.Popen([nvcc, *flags, "-c", "-o", o, os.path.join(_CSRC, u)]) for u, o in zip(UNITS, objects)]
+        codes = [j.wait() for j in jobs]
+        if any(codes):
+            raise subprocess.CalledProcessError(max(codes, key=abs), nvcc)
+        subprocess.run([nvcc, *NVCC_FLAGS, "-shared", "-o", LIB_PATH, *objects], check=True)
 
 
 def _build_native() -> None:

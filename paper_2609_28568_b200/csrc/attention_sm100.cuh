@@ -1,0 +1,103 @@
+// Attention over packed sequences for sm_100a: what its kernels share. Parameters, the work of a block, tiles.
+//
+//   S = scale Q K^T (a query sees the keys of its sequence, if causal up to its own row)   P = softmax(S)   O = P V
+//
+// Rows are tokens, T of them; head h of a tensor is D columns from column h D on, rows are ld elements apart. Sequence i is
+// the rows [cu[i], cu[i+1]) (or T / n rows each), queries' heads h = 0..heads-1 read the keys of head h / (heads / kv_heads).
+// Tiles are 128 rows of a sequence by 64 or 128 columns (D rounded up: what lies beyond D reads as zero), fetched by TMA in
+// boxes of 128 rows x 64 columns of one head with the 128-byte swizzle. A sequence's last tile ends inside a box: the
+// rows after it are another sequence's or nobody's, and where they would enter a sum as 0 x value they are overwritten with zeros
+// in shared memory (they may hold infinities or NaN).
+#pragma once
+#include "attention.h"
+#include "gemm_sm100.cuh"
+
+namespace nb {
+
+constexpr uint32_t kAttnBox = 128 * 128;  // bytes of a box
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttnSpan {
+    int start, len;  // rows of the sequence
+    int block;       // block of `rows` rows of it, or -1: nothing to do
+};
+
+// The sequence and block that a slot stands for, found by one warp. Sequence i has the slots from cu[i] / rows + i on, at least as many as it
+// has blocks of `rows` rows, so that no sums over the sequences before it are needed; it uses the last ones first (with a
+// causal mask they have the most work). Bounds outside [0, T] or falling ones are cut to an empty or shorter sequence and reported.
+__device__ __forceinline__ AttnSpan attn_span(const AttnParams &p, int slot, int rows, bool descending)
+{
+    const int lane = static_cast<int>(threadIdx.x & 31);
+    AttnSpan s;
+    int local;
+    if (p.cu == nullptr) {
+        const int len = p.T / p.n, per = (len + rows - 1) / rows;
+        const int i = slot / per;
+        s.start = i * len;
+        s.len = i < p.n ? len : 0;
+        local = slot - i * per;
+    } else {
+        int lo = 0, hi = p.n;  // the last i with cu[i] / rows + i <= slot lies in [lo, hi)
+        int at = 0;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) / 32;
+            const int i = lo + lane * step;
+            const int c = i < hi ? p.cu[i] : 0;
+            const unsigned before = __ballot_sync(0xffffffffu, i < hi && max(c, 0) / rows + i <= slot);
+            const int last = before ? 31 - __clz(before) : 0;
+            lo += last * step;
+            hi = min(hi, lo + step);
+        }
+        const int a = p.cu[lo], b = p.cu[lo + 1];
+        const int start = min(max(a, 0), p.T), end = min(max(b, start), p.T);
+        if ((start != a || end != b) && lane == 0 && atomicCAS(p.status, 0, kStatusBadSequences) == 0) p.status[1] = lo;
+        at = max(a, 0) / rows + lo;
+        s.start = start;
+        s.len = end - start;
+        local = slot - at;
+    }
+    const int blocks = (s.len + rows - 1) / rows;
+    s.block = local < 0 || local >= blocks ? -1 : descending ? blocks - 1 - local : local;
+    return s;
+}
+
+__device__ __forceinline__ bool warp_wait(const WaitCtx &w, uint32_t bar, uint32_t parity, int where)
+{
+    return __all_sync(0xffffffffu, wait_barrier(w, bar, parity, where));
+}
+
+// A tile of 128 rows, in boxes of 64 columns, from row `row` on.
+template <int D>
+__device__ __forceinline__ void attn_load(uint32_t dst, const CUtensorMap *m, uint32_t bar, int head, int row)
+{
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) ptx::tma_load_3d(dst + c * kAttnBox, m, bar, c * 64, head, row);
+}
+// Rows [from, to) of a tile in shared memory are set to zero by one warp.
+template <int D>
+__device__ __forceinline__ void attn_zero_rows(uint32_t tile, int from, int to)
+{
+    const int lane = static_cast<int>(threadIdx.x & 31);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+        for (int i = lane; i < (to - from) * 8; i += 32) ptx::st_shared_v4(tile + c * kAttnBox + from * 128 + i * 16, 0, 0, 0, 0);
+}
+
+// D[128, 128] = A B^T over `steps` pieces of 16 columns, tiles A and B with the summed index contiguous (boxes of 64 columns).
+__device__ __forceinline__ void attn_mma_kk(uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t idesc, int steps)
+{
+    const uint64_t ad = make_smem_desc(a, 16, 1024), bd = make_smem_desc(b, 16, 1024);
+    for (int k = 0; k < steps; ++k) {
+        const uint64_t off = static_cast<uint64_t>((k >> 2) * (kAttnBox >> 4) + (k & 3) * (32 >> 4));
+        ptx::umma_bf16<1>(d_tmem, ad + off, bd + off, idesc, k > 0 ? 1u : 0u);
+    }
+}
+// D[128, N] (+)= A B, A [128, 16 steps] in tensor memory, B's rows the summed index (a tile of 128 rows).
+__device__ __forceinline__ void attn_mma_tn(uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, bool accumulate)
+{
+    const uint64_t bd = make_smem_desc(b, kAttnBox, 1024);
+    for (int k = 0; k < steps; ++k)
+        ptx::umma_bf16_ts(d_tmem, a_tmem + k * 8, bd + static_cast<uint64_t>(k * (2048 >> 4)), idesc, accumulate || k > 0 ? 1u : 0u);
+}
+
+}  // namespace nb

@@ -15,6 +15,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <iterator>
 #include <tuple>
 #include <type_traits>
 #include <utility>
@@ -146,6 +147,51 @@ PyObject *call(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, std::index_
     if (rc != NB_OK) return raise(rc);
     Py_RETURN_NONE;
 }
+
+// Tensors whose rows may lie inside wider ones: {position of the tensor, position of its ld} in a call's arguments.
+template <class... A, size_t... I>
+PyObject *call_rows(int (*fn)(A...), const int (*pairs)[2], int npairs, PyObject *const *args, Py_ssize_t n, std::index_sequence<I...>)
+{
+    constexpr Py_ssize_t N = sizeof...(A);
+    if (n != N && n != N - 1) return PyErr_Format(PyExc_TypeError, "%zd or %zd arguments are wanted, not %zd", N - 1, N, n);
+    PyObject *address[N] = {};  // of a tensor with rows apart: its address in place of the tensor
+    bool ok = true;
+    CurrentDevice device;
+    for (int i = 0; i < npairs && ok; ++i) {
+        PyObject *o = args[pairs[i][0]];
+        if (!THPVariable_Check(o)) continue;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        int64_t ld = 0, dense = 1;
+        if (!(ok = device.has(o) && convert(args[pairs[i][1]], ld))) break;
+        ok = t.is_cuda() && t.dim() >= 2;
+        for (int64_t d = t.dim() - 1; d >= 1 && ok; dense *= t.size(d--)) ok = t.size(d) == 1 || t.stride(d) == dense;
+        if (!(ok = ok && (t.size(0) <= 1 || t.stride(0) == ld)))
+            PyErr_Format(PyExc_AssertionError, "argument %d: a CUDA tensor of dense rows, ld elements apart, is wanted", pairs[i][0]);
+        else
+            ok = (address[pairs[i][0]] = PyLong_FromVoidPtr(t.data_ptr())) != nullptr;
+    }
+    PyObject *result = nullptr;
+    if (ok) {
+        PyObject *given[N];
+        for (Py_ssize_t i = 0; i < n; ++i) given[i] = address[i] ? address[i] : args[i];
+        result = call<true>(fn, given, n, std::index_sequence<I...>{});
+    }
+    for (PyObject *a : address) Py_XDECREF(a);
+    return result;
+}
+
+template <auto fn, class ROWS>
+PyObject *entry_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    return [&]<class... A>(int (*f)(A...)) {
+        return call_rows(f, ROWS::pairs, static_cast<int>(std::size(ROWS::pairs)), args, n, std::index_sequence_for<A...>{});
+    }(fn);
+    END_HANDLE_TH_ERRORS
+}
+struct AttentionForwardRows {
+    static constexpr int pairs[][2] = {{0, 11}, {2, 12}, {3, 13}, {4, 14}};
+};
 
 template <auto fn, bool DEVICE_CHECKED = false>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -343,6 +389,8 @@ PyObject *set_python(PyObject *, PyObject *const *args, Py_ssize_t n)
 #define NB_ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&entry<name>)), METH_FASTCALL, nullptr}
 #define NB_ENTRY_CHECKED(name) \
     {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&entry<name, true>)), METH_FASTCALL, nullptr}
+#define NB_ENTRY_ROWS(name, rows) \
+    {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&entry_rows<name, rows>)), METH_FASTCALL, nullptr}
 #define NB_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     NB_ENTRY(nb_linear_forward_ex),
@@ -359,6 +407,7 @@ PyMethodDef g_methods[] = {
     NB_ENTRY(nb_cast_f32_to_bf16),
     NB_ENTRY_CHECKED(nb_layernorm_forward),
     NB_ENTRY_CHECKED(nb_layernorm_backward),
+    NB_ENTRY_ROWS(nb_attention_forward, AttentionForwardRows),
     {"nb_muon_update", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&muon_update)), METH_FASTCALL, nullptr},
     {"nb_muon_apply", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&muon_apply)), METH_FASTCALL, nullptr},
     NB_FAST(linear_forward),

@@ -17,6 +17,7 @@
 #include <type_traits>
 #include <unordered_map>
 
+#include "attention.h"
 #include "elementwise.cuh"
 #include "gemm_sm100.cuh"
 #include "layer_bwd_sm100.cuh"
@@ -217,6 +218,35 @@ int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n
     if (r != CUDA_SUCCESS)
         return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) for %llu x [%llu, %llu] at %p", static_cast<int>(r),
                     static_cast<unsigned long long>(n), static_cast<unsigned long long>(rows),
+                    static_cast<unsigned long long>(cols), ptr);
+    if (s.tmaps.size() > 8192) s.tmaps.clear();
+    s.tmaps.emplace(key, m);
+    *out = m;
+    return NB_OK;
+}
+
+// `heads` bf16 matrices [rows, cols] side by side, cols elements from one to the next and ld from row to row, in boxes of 128 rows x 64 columns
+// of one of them with the 128-byte swizzle. What lies outside a matrix reads as zero.
+int get_heads_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t rows, uint64_t cols, uint64_t heads, uint64_t ld)
+{
+    TmapKey key{ptr, rows, cols, ld, 64, 128, 3, heads};
+    auto it = s.tmaps.find(key);
+    if (it != s.tmaps.end()) {
+        *out = it->second;
+        return NB_OK;
+    }
+    cuuint64_t dims[3] = {cols, heads, rows};
+    cuuint64_t strides[2] = {cols * 2, ld * 2};
+    cuuint32_t box[3] = {64, 1, 128};
+    cuuint32_t estr[3] = {1, 1, 1};
+    alignas(64) CUtensorMap m;
+    memset(&m, 0, sizeof(m));
+    CUresult r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) for [%llu, %llu, %llu] at %p", static_cast<int>(r),
+                    static_cast<unsigned long long>(rows), static_cast<unsigned long long>(heads),
                     static_cast<unsigned long long>(cols), ptr);
     if (s.tmaps.size() > 8192) s.tmaps.clear();
     s.tmaps.emplace(key, m);
@@ -2124,6 +2154,92 @@ bool norm_overlap(const Span *w, int nw, const Span *r, int nr, int first_may_be
 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
+// ----------------------------------------------------------------------------- heads of queries, keys and values
+// A tensor of rows that may lie inside wider ones.
+struct Rows {
+    const void *p;
+    int64_t ld, width, rows;  // ld and width in bytes
+    bool written;
+};
+bool overlap(const Rows &a, const Rows &b)
+{
+    if (!a.p || !b.p || a.rows == 0 || b.rows == 0) return false;
+    const Span x{a.p, (a.rows - 1) * a.ld + a.width, true}, y{b.p, (b.rows - 1) * b.ld + b.width, true};
+    if (!overlap(x, y)) return false;
+    if (a.ld != b.ld) return true;
+    // columns of one buffer: apart if neither reaches into the other within a row
+    const int64_t d = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % a.ld, off = d < 0 ? d + a.ld : d;
+    return off < a.width || a.ld - off < b.width;
+}
+bool any_overlap(const Rows *v, int n)
+{
+    for (int i = 0; i < n; ++i)
+        for (int j = i + 1; j < n; ++j)
+            if ((v[i].written || v[j].written) && overlap(v[i], v[j])) return true;
+    return false;
+}
+
+int check_heads(int64_t T, int64_t n, int64_t heads, int64_t kv_heads, int64_t D, const void *cu)
+{
+    if (T < 0 || n < 0 || heads <= 0 || kv_heads <= 0 || D <= 0) return fail(NB_ERR_INVALID_ARG, "negative or zero dimension");
+    if (heads % kv_heads != 0)
+        return fail(NB_ERR_INVALID_ARG, "heads (%lld) must be a multiple of kv_heads (%lld)", static_cast<long long>(heads),
+                    static_cast<long long>(kv_heads));
+    if (D % 8 != 0 || D > NB_HEAD_MAX_D)
+        return fail(NB_ERR_UNSUPPORTED, "D (%lld) must be a multiple of 8 and at most %d", static_cast<long long>(D), NB_HEAD_MAX_D);
+    if (T > NB_HEAD_MAX_T || n > NB_HEAD_MAX_T || heads > NB_HEAD_MAX_HEADS)
+        return fail(NB_ERR_UNSUPPORTED, "too many rows, sequences or heads");
+    if (!cu && n > 0 && T % n != 0)
+        return fail(NB_ERR_INVALID_ARG, "without cu_seqlens the sequences are of one length: T (%lld) must be a multiple of n (%lld)",
+                    static_cast<long long>(T), static_cast<long long>(n));
+    return NB_OK;
+}
+int check_ld(const char *name, int64_t ld, int64_t width)
+{
+    if (ld < width) return fail(NB_ERR_INVALID_ARG, "ld_%s (%lld) is less than a row's %lld elements", name, static_cast<long long>(ld), static_cast<long long>(width));
+    if (ld % 8 != 0 || ld > NB_HEAD_MAX_LD)
+        return fail(NB_ERR_UNSUPPORTED, "ld_%s (%lld) must be a multiple of 8 and at most %lld", name, static_cast<long long>(ld),
+                    static_cast<long long>(NB_HEAD_MAX_LD));
+    return NB_OK;
+}
+
+// Launches an attention kernel on `slots` blocks of a sequence for each of `heads` heads.
+template <int MAPS>
+int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtensorMap (&maps)[MAPS], AttnParams &p, int64_t slots, int64_t heads,
+                     cudaStream_t stream)
+{
+    int dev = 0;
+    NB_CUDA(cudaGetDevice(&dev));
+    if (!attr_set[dev]) {
+        NB_CUDA(cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem)));
+        attr_set[dev] = true;
+    }
+    if (slots * heads >= (1ll << 31)) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(slots * heads));
+    cfg.blockDim = dim3(kAttnThreads);
+    cfg.dynamicSmemBytes = k.smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = dependent_launch_allowed(stream) ? 1 : 0;
+    void *args[MAPS + 1];
+    for (int i = 0; i < MAPS; ++i) args[i] = &maps[i];
+    args[MAPS] = &p;
+    NB_CUDA(cudaLaunchKernelExC(&cfg, k.fn, args));
+    ++g_launches;
+    return NB_OK;
+}
+// Slots for blocks of `rows` rows (attn_span).
+int64_t attn_slots(const AttnParams &p, int rows)
+{
+    if (p.cu) return p.T / rows + p.n;
+    const int64_t len = p.T / p.n;
+    return p.n * ((len + rows - 1) / rows);
+}
+
 }  // namespace
 
 // ================================================================================ C ABI
@@ -2821,6 +2937,50 @@ int nb_muon_apply(void *const *master, void *const *weight, const void *const *u
     return NB_OK;
 }
 
+// ----------------------------------------------------------------------------- attention
+int nb_attention_forward(void *out, void *lse, const void *q, const void *k, const void *v, const void *cu_seqlens, int64_t T, int64_t n,
+                         int64_t heads, int64_t kv_heads, int64_t D, int64_t ld_out, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                         float scale, int causal, void *stream_)
+{
+    int rc = check_heads(T, n, heads, kv_heads, D, cu_seqlens);
+    if (rc != NB_OK) return rc;
+    if ((rc = check_ld("out", ld_out, heads * D)) != NB_OK || (rc = check_ld("q", ld_q, heads * D)) != NB_OK ||
+        (rc = check_ld("k", ld_k, kv_heads * D)) != NB_OK || (rc = check_ld("v", ld_v, kv_heads * D)) != NB_OK)
+        return rc;
+    if (!(scale > 0.0f) || scale > 3.0e38f) return fail(NB_ERR_INVALID_ARG, "scale must be positive and finite");
+    if (T == 0 || n == 0) return NB_OK;  // tensors without elements have no address
+    if (!out || !q || !k || !v) return fail(NB_ERR_INVALID_ARG, "out, q, k and v must not be NULL");
+    if (!aligned16(out) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned4(lse) || !aligned4(cu_seqlens))
+        return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, lse and cu_seqlens 4-byte aligned");
+    const Rows r[] = {{out, ld_out * 2, heads * D * 2, T, true}, {lse, heads * T * 4, heads * T * 4, 1, true},
+                      {q, ld_q * 2, heads * D * 2, T, false}, {k, ld_k * 2, kv_heads * D * 2, T, false},
+                      {v, ld_v * 2, kv_heads * D * 2, T, false}, {cu_seqlens, (n + 1) * 4, (n + 1) * 4, 1, false}};
+    if (any_overlap(r, 6)) return fail(NB_ERR_INVALID_ARG, "out or lse overlaps another argument");
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    if ((rc = get_state(&s)) != NB_OK) return rc;
+    AttnParams p{};
+    p.T = static_cast<int>(T);
+    p.n = static_cast<int>(n);
+    p.heads = static_cast<int>(heads);
+    p.group = static_cast<int>(heads / kv_heads);
+    p.D = static_cast<int>(D);
+    p.causal = causal != 0;
+    p.cu = static_cast<const int *>(cu_seqlens);
+    p.scale = scale;
+    p.ld_out = ld_out;
+    p.out = out;
+    p.lse = static_cast<float *>(lse);
+    p.status = s->status;
+    p.timeout_ns = kDefaultTimeoutNs;
+    CUtensorMap maps[3];
+    if ((rc = get_heads_tmap(*s, &maps[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &maps[1], k, T, D, kv_heads, ld_k)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &maps[2], v, T, D, kv_heads, ld_v)) != NB_OK)
+        return rc;
+    static bool attr_set[2][kMaxDevices] = {};
+    return launch_attention(attn_forward(p.D), attr_set[D > 64], maps, p, attn_slots(p, 256), heads, static_cast<cudaStream_t>(stream_));
+}
+
 int nb_workspace_reserve(int64_t bytes)
 {
     if (bytes < 0) return fail(NB_ERR_INVALID_ARG, "negative size");
@@ -2860,6 +3020,8 @@ int nb_check_status(void)
     if (host[0] == kStatusTimeout)
         return fail(NB_ERR_TIMEOUT, "a bounded device wait expired (wait id %d, block %d)", host[1],
                     host[2]);
+    if (host[0] == kStatusBadSequences)
+        return fail(NB_ERR_INVALID_ARG, "cu_seqlens does not rise from 0 to T at most (sequence %d)", host[1]);
     return fail(NB_ERR_CUDA, "kernel reported internal error %d (block %d)", host[0], host[2]);
 }
 

@@ -72,13 +72,6 @@ struct NsCfg {
 };
 
 // 3-D forms of the tile load: z is the matrix of the batch.
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *m, uint32_t bar, int x, int y, int z)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z)
-        : "memory");
-}
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *m, uint32_t bar, int x, int y, int z)
 {
     asm volatile(
@@ -318,7 +311,7 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap tmX0, const __grid_cons
 
     auto load = [&](uint32_t dst, const CUtensorMap *m, uint32_t bar, int x, int y, int z) {
         if (CG == 2) tma_load_3d_pair(dst, m, bar, x, y, z);
-        else tma_load_3d(dst, m, bar, x, y, z);
+        else ptx::tma_load_3d(dst, m, bar, x, y, z);
     };
 
     if (!smem_ok) {
