@@ -397,6 +397,27 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
                          float scale, int causal, void *stream);
 
 /*
+ * Its backward pass, with out and lse of the forward pass. With p_ij = exp(s_ij - lse_i) and delta_i = sum over a row of dout out:
+ *
+ *     dv_j = sum_i p_ij dout_i     ds_ij = p_ij (dout_i . v_j - delta_i)     dq_i = scale sum_j ds_ij k_j     dk_j = scale sum_i ds_ij q_i
+ *
+ * dk and dv are sums over the queries' heads that share a head of keys.
+ *   dq         [out] [T, heads, D] bf16;  dk, dv [out] [T, kv_heads, D] bf16 (all three may be columns of one buffer, as the qkv linear's
+ *                    backward pass takes it)
+ *   dout, out  [in]  [T, heads, D] bf16;  lse [in] [heads, T] fp32;  the rest as in the forward pass
+ *   workspace  device memory of nb_attention_workspace(T, heads) bytes, 16-byte aligned, the caller's: calls that may run at the same time (on two streams,
+ *              or captured into two graphs) need one each
+ * Sums are fp32 and in a fixed order: the same inputs give the same bits. p and ds are rounded to bf16 for the tensor cores, gradients once at the end.
+ * Rows in no sequence are not written. What is not finite in one sequence reaches no other.
+ * nb_attention_workspace returns -1 for sizes that the call would refuse.
+ */
+int64_t nb_attention_workspace(int64_t T, int64_t heads);
+int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const void *out, const void *lse, const void *q, const void *k,
+                          const void *v, const void *cu_seqlens, int64_t T, int64_t n, int64_t heads, int64_t kv_heads, int64_t D,
+                          int64_t ld_dq, int64_t ld_dk, int64_t ld_dv, int64_t ld_dout, int64_t ld_out, int64_t ld_q, int64_t ld_k,
+                          int64_t ld_v, float scale, int causal, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * Bias gradient of a GELU layer without any allocation (the paper has no counterpart; this
  * exists for callers that must not allocate device memory):
  *

@@ -31,7 +31,7 @@ EXPORTS = (
     "nb_lora_down_stacked", "nb_lora_linear_forward_stacked", "nb_lora_linear_backward_stacked",
     "nb_lora_da_stacked", "nb_debug_route", "nb_layernorm_forward", "nb_layernorm_workspace", "nb_layernorm_backward",
     "nb_muon_workspace", "nb_muon_update", "nb_muon_apply", "nb_debug_layernorm_timeout",
-    "nb_debug_muon_timeout", "nb_attention_forward",
+    "nb_debug_muon_timeout", "nb_attention_forward", "nb_attention_workspace", "nb_attention_backward",
 )
 
 CALL_FORWARD, CALL_BACKWARD, CALL_LORA_FORWARD, CALL_LORA_BACKWARD = range(4)
@@ -90,6 +90,9 @@ def lib() -> ctypes.CDLL:
                                      [_int, _vp, _i64, _vp])
         L.nb_muon_apply.argtypes = [ctypes.POINTER(_vp)] * 3 + [_i64] * 2 + [ctypes.c_float] * 2 + [_vp]
         L.nb_attention_forward.argtypes = [_vp] * 6 + [_i64] * 9 + [ctypes.c_float, _int, _vp]
+        L.nb_attention_workspace.argtypes = [_i64] * 2
+        L.nb_attention_workspace.restype = _i64
+        L.nb_attention_backward.argtypes = [_vp] * 10 + [_i64] * 13 + [ctypes.c_float, _int, _vp, _i64, _vp]
         L.nb_debug_split_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int)]
         L.nb_debug_gemm_timeout.argtypes = [_vp, _vp, _vp, _i64]
         L.nb_debug_layernorm_timeout.argtypes = [_vp, _vp, _vp, _vp, _int, _i64]
@@ -311,6 +314,19 @@ def nb_attention_forward(out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D
     of wider ones, with rows ld elements apart."""
     (_native or _load_native()).nb_attention_forward(out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, ld_out, ld_q, ld_k, ld_v,
                                                      scale, int(causal), stream)
+
+
+def nb_attention_workspace(T: int, heads: int) -> int:
+    """Bytes of workspace that nb_attention_backward needs."""
+    return _size(lib().nb_attention_workspace(T, heads), f"attention of {heads} heads over {T} rows")
+
+
+def nb_attention_backward(dq, dk, dv, dout, out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, ld_dq, ld_dk, ld_dv, ld_dout, ld_out, ld_q,
+                          ld_k, ld_v, scale, causal, workspace, workspace_bytes, stream=None) -> None:
+    """Gradients of attention with out and lse of the forward pass."""
+    (_native or _load_native()).nb_attention_backward(dq, dk, dv, dout, out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, ld_dq, ld_dk,
+                                                      ld_dv, ld_dout, ld_out, ld_q, ld_k, ld_v, scale, int(causal), workspace, workspace_bytes,
+                                                      stream)
 
 
 def nb_debug_split_plan(M: int, N: int, K: int, slots: int, tile_m: int):

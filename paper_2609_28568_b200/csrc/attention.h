@@ -21,11 +21,21 @@ struct AttnParams {
     unsigned long long timeout_ns;
 };
 
-// A kernel for heads of D columns and its dynamic shared memory. Parameters: its tensor maps, then AttnParams.
+struct AttnBackward {
+    AttnParams a;            // a.out: the forward pass's output, a.ld_out its ld; a.lse: read
+    float *delta;            // [heads, T]: sum over a row of dout out, written by the pass of dq, read by that of dk and dv
+    const void *dout;
+    void *dq, *dk, *dv;
+    long long ld_dout, ld_dq, ld_dk, ld_dv;
+};
+
+// A kernel for heads of D columns and its dynamic shared memory. Parameters: its tensor maps (forward: q, k, v), then AttnParams or AttnBackward.
 struct AttnKernel {
     const void *fn;
     uint32_t smem;
 };
 AttnKernel attn_forward(int D);
+AttnKernel attn_backward_q(int D);   // maps: q, dout, k, v
+AttnKernel attn_backward_kv(int D);  // the same
 
 }  // namespace nb

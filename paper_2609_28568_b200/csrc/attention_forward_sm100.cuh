@@ -285,35 +285,10 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         if (ok && nt > 0) ok = warp_wait(wctx2, o_bar(t), 0, 420 + t);
         if (ok && nt > 0) {
             ptx::tc_fence_after();
-            // The rows leave through shared memory (where this warp's queries were: all products that read them are done), so that
-            // neighbouring threads store neighbouring pieces of 16 bytes.
-            const float inv = 1.0f / total;
-            constexpr int CH = D / 8;  // pieces of a row
-            const uint32_t stg = smem + Cfg::OFF_Q + t * Cfg::TILE + (warp & 3) * 32 * D * 2;
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                ptx::tmem_ld_32x32_wait(o_tm + c * 32, o);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        w[i] = ptx::pack_bf16x2(__uint_as_float(o[k * 8 + 2 * i]) * inv, __uint_as_float(o[k * 8 + 2 * i + 1]) * inv);
-                    ptx::st_shared_v4(stg + lane * D * 2 + (((c * 4 + k) ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
-                }
-            }
-            __syncwarp();
+            // through where this warp's queries were: all products that read them are done
             const int first = row - lane;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                const int r = i * (32 / CH) + lane / CH, k = lane % CH;
-                uint32_t w[4];
-                ptx::ld_shared_v4(stg + r * D * 2 + ((k ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
-                if (first + r < len && k * 8 < p.D)
-                    *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + (start + first + r) * p.ld_out + head * p.D + k * 8) =
-                        make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            attn_store_rows<D>(o_tm, 1.0f / total, smem + Cfg::OFF_Q + t * Cfg::TILE + (warp & 3) * 32 * D * 2,
+                               static_cast<__nv_bfloat16 *>(p.out) + (start + first) * p.ld_out + head * p.D, p.ld_out, len - first, p.D);
             if (p.lse && row < len) p.lse[static_cast<long long>(head) * p.T + start + row] = top * p.scale + logf(total);
         }
         ptx::tc_fence_before();

@@ -92,12 +92,46 @@ __device__ __forceinline__ void attn_mma_kk(uint32_t d_tmem, uint32_t a, uint32_
         ptx::umma_bf16<1>(d_tmem, ad + off, bd + off, idesc, k > 0 ? 1u : 0u);
     }
 }
-// D[128, N] (+)= A B, A [128, 16 steps] in tensor memory, B's rows the summed index (a tile of 128 rows).
+// D[128, N] (+)= A B, A [128, 16 steps] in tensor memory (piece k of 16 columns at a_tmem + 8 k, or, SPLIT, the second 64 columns of A
+// 64 columns of tensor memory after the first), B's rows the summed index (a tile of 128 rows).
+template <bool SPLIT = false>
 __device__ __forceinline__ void attn_mma_tn(uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, bool accumulate)
 {
     const uint64_t bd = make_smem_desc(b, kAttnBox, 1024);
     for (int k = 0; k < steps; ++k)
-        ptx::umma_bf16_ts(d_tmem, a_tmem + k * 8, bd + static_cast<uint64_t>(k * (2048 >> 4)), idesc, accumulate || k > 0 ? 1u : 0u);
+        ptx::umma_bf16_ts(d_tmem, a_tmem + (SPLIT ? (k >> 2) * 64 + (k & 3) * 8 : k * 8), bd + static_cast<uint64_t>(k * (2048 >> 4)), idesc,
+                          accumulate || k > 0 ? 1u : 0u);
+}
+
+// 32 rows of W columns, a row per lane, from the fp32 accumulator at `acc` to bf16 rows in global memory, by way of shared memory (32 W 2 bytes
+// at `stg`, this warp's own), so that neighbouring threads store neighbouring pieces of 16 bytes. Rows and pieces beyond the bounds are left out.
+template <int W>
+__device__ __forceinline__ void attn_store_rows(uint32_t acc, float factor, uint32_t stg, void *dst, long long ld, int rows, int cols)
+{
+    constexpr int CH = W / 8;  // pieces of a row
+    const int lane = static_cast<int>(threadIdx.x & 31);
+#pragma unroll
+    for (int c = 0; c < W / 32; ++c) {
+        uint32_t o[32];
+        ptx::tmem_ld_32x32_wait(acc + c * 32, o);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = ptx::pack_bf16x2(__uint_as_float(o[k * 8 + 2 * i]) * factor, __uint_as_float(o[k * 8 + 2 * i + 1]) * factor);
+            ptx::st_shared_v4(stg + lane * W * 2 + (((c * 4 + k) ^ (lane & (CH < 8 ? CH - 1 : 7))) << 4), w[0], w[1], w[2], w[3]);
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int r = i * (32 / CH) + lane / CH, k = lane % CH;
+        uint32_t w[4];
+        ptx::ld_shared_v4(stg + r * W * 2 + ((k ^ (r & (CH < 8 ? CH - 1 : 7))) << 4), w[0], w[1], w[2], w[3]);
+        if (r < rows && k * 8 < cols)
+            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(dst) + r * ld + k * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
 }
 
 }  // namespace nb

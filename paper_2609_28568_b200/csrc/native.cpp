@@ -193,6 +193,10 @@ struct AttentionForwardRows {
     static constexpr int pairs[][2] = {{0, 11}, {2, 12}, {3, 13}, {4, 14}};
 };
 
+struct AttentionBackwardRows {
+    static constexpr int pairs[][2] = {{0, 15}, {1, 16}, {2, 17}, {3, 18}, {4, 19}, {6, 20}, {7, 21}, {8, 22}};
+};
+
 template <auto fn, bool DEVICE_CHECKED = false>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -408,6 +412,7 @@ PyMethodDef g_methods[] = {
     NB_ENTRY_CHECKED(nb_layernorm_forward),
     NB_ENTRY_CHECKED(nb_layernorm_backward),
     NB_ENTRY_ROWS(nb_attention_forward, AttentionForwardRows),
+    NB_ENTRY_ROWS(nb_attention_backward, AttentionBackwardRows),
     {"nb_muon_update", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&muon_update)), METH_FASTCALL, nullptr},
     {"nb_muon_apply", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&muon_apply)), METH_FASTCALL, nullptr},
     NB_FAST(linear_forward),

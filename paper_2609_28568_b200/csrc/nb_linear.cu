@@ -2203,9 +2203,25 @@ int check_ld(const char *name, int64_t ld, int64_t width)
     return NB_OK;
 }
 
+AttnParams attn_params(const DeviceState &s, int64_t T, int64_t n, int64_t heads, int64_t kv_heads, int64_t D, const void *cu, float scale, int causal)
+{
+    AttnParams p{};
+    p.T = static_cast<int>(T);
+    p.n = static_cast<int>(n);
+    p.heads = static_cast<int>(heads);
+    p.group = static_cast<int>(heads / kv_heads);
+    p.D = static_cast<int>(D);
+    p.causal = causal != 0;
+    p.cu = static_cast<const int *>(cu);
+    p.scale = scale;
+    p.status = s.status;
+    p.timeout_ns = kDefaultTimeoutNs;
+    return p;
+}
+
 // Launches an attention kernel on `slots` blocks of a sequence for each of `heads` heads.
-template <int MAPS>
-int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtensorMap (&maps)[MAPS], AttnParams &p, int64_t slots, int64_t heads,
+template <int MAPS, class P>
+int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtensorMap (&maps)[MAPS], P &p, int64_t slots, int64_t heads,
                      cudaStream_t stream)
 {
     int dev = 0;
@@ -2959,26 +2975,77 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *s;
     if ((rc = get_state(&s)) != NB_OK) return rc;
-    AttnParams p{};
-    p.T = static_cast<int>(T);
-    p.n = static_cast<int>(n);
-    p.heads = static_cast<int>(heads);
-    p.group = static_cast<int>(heads / kv_heads);
-    p.D = static_cast<int>(D);
-    p.causal = causal != 0;
-    p.cu = static_cast<const int *>(cu_seqlens);
-    p.scale = scale;
+    AttnParams p = attn_params(*s, T, n, heads, kv_heads, D, cu_seqlens, scale, causal);
     p.ld_out = ld_out;
     p.out = out;
     p.lse = static_cast<float *>(lse);
-    p.status = s->status;
-    p.timeout_ns = kDefaultTimeoutNs;
     CUtensorMap maps[3];
     if ((rc = get_heads_tmap(*s, &maps[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &maps[1], k, T, D, kv_heads, ld_k)) != NB_OK ||
         (rc = get_heads_tmap(*s, &maps[2], v, T, D, kv_heads, ld_v)) != NB_OK)
         return rc;
     static bool attr_set[2][kMaxDevices] = {};
     return launch_attention(attn_forward(p.D), attr_set[D > 64], maps, p, attn_slots(p, 256), heads, static_cast<cudaStream_t>(stream_));
+}
+
+int64_t nb_attention_workspace(int64_t T, int64_t heads)
+{
+    if (T < 0 || heads <= 0 || T > NB_HEAD_MAX_T || heads > NB_HEAD_MAX_HEADS) return -1;
+    return T * heads * static_cast<int64_t>(sizeof(float));
+}
+
+int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const void *out, const void *lse, const void *q, const void *k,
+                          const void *v, const void *cu_seqlens, int64_t T, int64_t n, int64_t heads, int64_t kv_heads, int64_t D,
+                          int64_t ld_dq, int64_t ld_dk, int64_t ld_dv, int64_t ld_dout, int64_t ld_out, int64_t ld_q, int64_t ld_k,
+                          int64_t ld_v, float scale, int causal, void *workspace, int64_t workspace_bytes, void *stream_)
+{
+    int rc = check_heads(T, n, heads, kv_heads, D, cu_seqlens);
+    if (rc != NB_OK) return rc;
+    const int64_t wide = heads * D, narrow = kv_heads * D;
+    if ((rc = check_ld("dq", ld_dq, wide)) != NB_OK || (rc = check_ld("dk", ld_dk, narrow)) != NB_OK || (rc = check_ld("dv", ld_dv, narrow)) != NB_OK ||
+        (rc = check_ld("dout", ld_dout, wide)) != NB_OK || (rc = check_ld("out", ld_out, wide)) != NB_OK || (rc = check_ld("q", ld_q, wide)) != NB_OK ||
+        (rc = check_ld("k", ld_k, narrow)) != NB_OK || (rc = check_ld("v", ld_v, narrow)) != NB_OK)
+        return rc;
+    if (!(scale > 0.0f) || scale > 3.0e38f) return fail(NB_ERR_INVALID_ARG, "scale must be positive and finite");
+    if (T == 0 || n == 0) return NB_OK;  // tensors without elements have no address
+    if (!dq || !dk || !dv || !dout || !out || !lse || !q || !k || !v)
+        return fail(NB_ERR_INVALID_ARG, "dq, dk, dv, dout, out, lse, q, k and v must not be NULL");
+    if (!aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dout) || !aligned16(out) || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
+        !aligned16(workspace) || !aligned4(lse) || !aligned4(cu_seqlens))
+        return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, lse and cu_seqlens 4-byte aligned");
+    const int64_t need = nb_attention_workspace(T, heads);
+    if (!workspace || workspace_bytes < need)
+        return fail(NB_ERR_INVALID_ARG, "a workspace of %lld bytes is needed (nb_attention_workspace)", static_cast<long long>(need));
+    const Rows r[] = {{dq, ld_dq * 2, wide * 2, T, true}, {dk, ld_dk * 2, narrow * 2, T, true}, {dv, ld_dv * 2, narrow * 2, T, true},
+                      {workspace, need, need, 1, true}, {dout, ld_dout * 2, wide * 2, T, false}, {out, ld_out * 2, wide * 2, T, false},
+                      {lse, need, need, 1, false}, {q, ld_q * 2, wide * 2, T, false}, {k, ld_k * 2, narrow * 2, T, false},
+                      {v, ld_v * 2, narrow * 2, T, false}, {cu_seqlens, (n + 1) * 4, (n + 1) * 4, 1, false}};
+    if (any_overlap(r, 11)) return fail(NB_ERR_INVALID_ARG, "a gradient or the workspace overlaps another argument");
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    if ((rc = get_state(&s)) != NB_OK) return rc;
+    AttnBackward b{};
+    b.a = attn_params(*s, T, n, heads, kv_heads, D, cu_seqlens, scale, causal);
+    b.a.ld_out = ld_out;
+    b.a.out = const_cast<void *>(out);
+    b.a.lse = const_cast<float *>(static_cast<const float *>(lse));
+    b.delta = static_cast<float *>(workspace);
+    b.dout = dout;
+    b.dq = dq;
+    b.dk = dk;
+    b.dv = dv;
+    b.ld_dout = ld_dout;
+    b.ld_dq = ld_dq;
+    b.ld_dk = ld_dk;
+    b.ld_dv = ld_dv;
+    CUtensorMap maps[4];
+    if ((rc = get_heads_tmap(*s, &maps[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &maps[1], dout, T, D, heads, ld_dout)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &maps[2], k, T, D, kv_heads, ld_k)) != NB_OK || (rc = get_heads_tmap(*s, &maps[3], v, T, D, kv_heads, ld_v)) != NB_OK)
+        return rc;
+    static bool attr_set[4][kMaxDevices] = {};
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int64_t slots = attn_slots(b.a, 128);
+    if ((rc = launch_attention(attn_backward_q(b.a.D), attr_set[D > 64], maps, b, slots, heads, stream)) != NB_OK) return rc;
+    return launch_attention(attn_backward_kv(b.a.D), attr_set[2 + (D > 64)], maps, b, slots, kv_heads, stream);
 }
 
 int nb_workspace_reserve(int64_t bytes)
