@@ -367,6 +367,34 @@ int nb_muon_apply(void *const *master, void *const *weight, const void *const *u
                   int64_t count, float decay, float step, void *stream);
 
 /*
+ * Rotary positions of queries and keys (between the q and k projections of an adapter-stage layer and its attention). The first R of a head's D columns
+ * are pairs (a, b), pair j of a token at position t turned by the angle t freq[j]; the columns after them are copied:
+ *
+ *     a' = scale (a cos - b sin)     b' = scale (b cos + a sin)
+ *
+ * Tensors of heads, their ld and cu_seqlens as in nb_attention_forward below.
+ *   out_q, q    [out], [in] [T, heads, D] bf16; may be the same tensor
+ *   out_k, k    [out], [in] [T, kv_heads, D] bf16; may be the same tensor; both NULL: queries alone
+ *   freq        [in]  [R / 2] fp64 on the device, radians per position, 8-byte aligned (nb_rotary_frequencies)
+ *   positions   [in]  [T] int32 on the device, or NULL: a row's place in its sequence
+ *   layout      NB_ROTARY_HALF: pairs (j, j + R / 2), R a multiple of 16; NB_ROTARY_NEIGHBOURS: (2 j, 2 j + 1), R a multiple of 8
+ *   scale       finite; of cosine and sine (1, or the factor by which queries and keys grow in a scaled context)
+ *   inverse     turns back: the gradients of q and k are those of the outputs, turned back with the same scale
+ * Angles are formed in 64 bits and reduced to a part of a turn before they are rounded; results are rounded once. An output that overlaps another
+ * argument is refused.
+ *
+ * nb_rotary_frequencies writes to host memory, freq[j] = base^(-2 j / R), for j < R / 2. Scaled contexts: with original == 0 all
+ * of them divided by factor; with original > 0 by parts: those that turn more than `high` times over `original` positions stay, those that turn
+ * less than `low` times are divided by factor, with a straight line (of freq over the turns) between.
+ */
+#define NB_ROTARY_HALF 0
+#define NB_ROTARY_NEIGHBOURS 1
+int nb_rotary_frequencies(double *freq, int64_t R, double base, double factor, double low, double high, int64_t original);
+int nb_rotary(void *out_q, void *out_k, const void *q, const void *k, const void *freq, const void *positions, const void *cu_seqlens, int64_t T,
+              int64_t n, int64_t heads, int64_t kv_heads, int64_t D, int64_t R, int64_t ld_out_q, int64_t ld_out_k, int64_t ld_q, int64_t ld_k,
+              float scale, int layout, int inverse, void *stream);
+
+/*
  * Attention over packed sequences (the step between the qkv linear and attn_proj; paper: Figure 1, the attention box of a block).
  *
  * Rows are tokens, T of them. Head h of a tensor is its columns [h D, (h + 1) D); rows lie ld elements apart, so that queries, keys and values may be

@@ -20,6 +20,7 @@ from .build import LIB_PATH, NATIVE_PATH
 NB_OK, NB_ERR_INVALID_ARG, NB_ERR_UNSUPPORTED, NB_ERR_CUDA, NB_ERR_TIMEOUT = 0, 1, 2, 3, 4
 ACT_NONE, ACT_GELU, ACT_SWIGLU = 0, 1, 2
 DTYPE_F32, DTYPE_BF16 = 0, 1
+ROTARY_HALF, ROTARY_NEIGHBOURS = 0, 1
 
 EXPORTS = (
     "nb_version", "nb_last_error", "nb_set_stream", "nb_get_stream", "nb_linear_out_elems",
@@ -31,7 +32,7 @@ EXPORTS = (
     "nb_lora_down_stacked", "nb_lora_linear_forward_stacked", "nb_lora_linear_backward_stacked",
     "nb_lora_da_stacked", "nb_debug_route", "nb_layernorm_forward", "nb_layernorm_workspace", "nb_layernorm_backward",
     "nb_muon_workspace", "nb_muon_update", "nb_muon_apply", "nb_debug_layernorm_timeout",
-    "nb_debug_muon_timeout", "nb_attention_forward", "nb_attention_workspace", "nb_attention_backward",
+    "nb_debug_muon_timeout", "nb_rotary_frequencies", "nb_rotary", "nb_attention_forward", "nb_attention_workspace", "nb_attention_backward",
 )
 
 CALL_FORWARD, CALL_BACKWARD, CALL_LORA_FORWARD, CALL_LORA_BACKWARD = range(4)
@@ -89,6 +90,8 @@ def lib() -> ctypes.CDLL:
         L.nb_muon_update.argtypes = ([ctypes.POINTER(_vp)] * 3 + [_i64] * 3 + [ctypes.c_float, _int, _int] + [ctypes.c_float] * 4 +
                                      [_int, _vp, _i64, _vp])
         L.nb_muon_apply.argtypes = [ctypes.POINTER(_vp)] * 3 + [_i64] * 2 + [ctypes.c_float] * 2 + [_vp]
+        L.nb_rotary_frequencies.argtypes = [ctypes.POINTER(ctypes.c_double), _i64] + [ctypes.c_double] * 4 + [_i64]
+        L.nb_rotary.argtypes = [_vp] * 7 + [_i64] * 10 + [ctypes.c_float, _int, _int, _vp]
         L.nb_attention_forward.argtypes = [_vp] * 6 + [_i64] * 9 + [ctypes.c_float, _int, _vp]
         L.nb_attention_workspace.argtypes = [_i64] * 2
         L.nb_attention_workspace.restype = _i64
@@ -306,6 +309,21 @@ def nb_muon_update(update, momentum, grad, n, R, C, mu, nesterov, steps, a, b, c
 def nb_muon_apply(master, weight, update, n, count, decay, step, stream=None) -> None:
     """master <- decay * master - step * update, weight <- bf16(master), for n tensors of count elements given as sequences."""
     (_native or _load_native()).nb_muon_apply(master, weight, update, n, count, decay, step, stream)
+
+
+def nb_rotary_frequencies(R: int, base: float = 10000.0, factor: float = 1.0, low: float = 1.0, high: float = 32.0, original: int = 0):
+    """Radians per position of R / 2 pairs, a list. factor: of a longer context; by parts where original is its positions before (see the header)."""
+    freq = (ctypes.c_double * max(R // 2, 1))()
+    _check(lib().nb_rotary_frequencies(freq, R, base, factor, low, high, original))
+    return list(freq[:R // 2])
+
+
+def nb_rotary(out_q, out_k, q, k, freq, positions, cu_seqlens, T, n, heads, kv_heads, D, R, ld_out_q, ld_out_k, ld_q, ld_k, scale, layout,
+              inverse, stream=None) -> None:
+    """Queries and keys turned by their positions (inverse: back). The tensors of heads may be columns of wider ones, with rows ld elements
+    apart; an output may be its input."""
+    (_native or _load_native()).nb_rotary(out_q, out_k, q, k, freq, positions, cu_seqlens, T, n, heads, kv_heads, D, R, ld_out_q, ld_out_k,
+                                          ld_q, ld_k, scale, layout, int(inverse), stream)
 
 
 def nb_attention_forward(out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, ld_out, ld_q, ld_k, ld_v, scale, causal,

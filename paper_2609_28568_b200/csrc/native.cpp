@@ -193,6 +193,9 @@ struct AttentionForwardRows {
     static constexpr int pairs[][2] = {{0, 11}, {2, 12}, {3, 13}, {4, 14}};
 };
 
+struct RotaryRows {
+    static constexpr int pairs[][2] = {{0, 13}, {1, 14}, {2, 15}, {3, 16}};
+};
 struct AttentionBackwardRows {
     static constexpr int pairs[][2] = {{0, 15}, {1, 16}, {2, 17}, {3, 18}, {4, 19}, {6, 20}, {7, 21}, {8, 22}};
 };
@@ -411,6 +414,7 @@ PyMethodDef g_methods[] = {
     NB_ENTRY(nb_cast_f32_to_bf16),
     NB_ENTRY_CHECKED(nb_layernorm_forward),
     NB_ENTRY_CHECKED(nb_layernorm_backward),
+    NB_ENTRY_ROWS(nb_rotary, RotaryRows),
     NB_ENTRY_ROWS(nb_attention_forward, AttentionForwardRows),
     NB_ENTRY_ROWS(nb_attention_backward, AttentionBackwardRows),
     {"nb_muon_update", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&muon_update)), METH_FASTCALL, nullptr},

@@ -25,6 +25,7 @@
 #include "muon.cuh"
 #include "newton_schulz_sm100.cuh"
 #include "norm.cuh"
+#include "rotary.cuh"
 #include "rows_sm100.cuh"
 #include "tile_sm100.cuh"
 
@@ -2950,6 +2951,90 @@ int nb_muon_apply(void *const *master, void *const *weight, const void *const *u
         if (rc != NB_OK) return rc;
         ++g_launches;
     }
+    return NB_OK;
+}
+
+// ----------------------------------------------------------------------------- rotary positions
+int nb_rotary_frequencies(double *freq, int64_t R, double base, double factor, double low, double high, int64_t original)
+{
+    if (R <= 0 || original < 0) return fail(NB_ERR_INVALID_ARG, "negative or zero dimension");
+    if (R % 2 != 0 || R > NB_HEAD_MAX_D) return fail(NB_ERR_UNSUPPORTED, "R (%lld) must be even and at most %d", static_cast<long long>(R), NB_HEAD_MAX_D);
+    if (!freq) return fail(NB_ERR_INVALID_ARG, "freq must not be NULL");
+    if (!(base > 0.0) || !std::isfinite(base) || !(factor > 0.0) || !std::isfinite(factor))
+        return fail(NB_ERR_INVALID_ARG, "base and factor must be positive and finite");
+    if (original > 0 && (!std::isfinite(low) || !std::isfinite(high) || !(low < high)))
+        return fail(NB_ERR_INVALID_ARG, "low and high must be finite, low less than high");
+    for (int64_t j = 0; j < R / 2; ++j) {
+        const double f = std::pow(base, -2.0 * static_cast<double>(j) / static_cast<double>(R));
+        double keep = 0.0;
+        if (original > 0) {
+            const double turns = static_cast<double>(original) * f / 6.283185307179586;
+            keep = std::fmin(std::fmax((turns - low) / (high - low), 0.0), 1.0);
+        }
+        freq[j] = f * (keep + (1.0 - keep) / factor);
+    }
+    return NB_OK;
+}
+
+int nb_rotary(void *out_q, void *out_k, const void *q, const void *k, const void *freq, const void *positions, const void *cu_seqlens, int64_t T,
+              int64_t n, int64_t heads, int64_t kv_heads, int64_t D, int64_t R, int64_t ld_out_q, int64_t ld_out_k, int64_t ld_q, int64_t ld_k,
+              float scale, int layout, int inverse, void *stream_)
+{
+    int rc = check_heads(T, n, heads, kv_heads, D, cu_seqlens);
+    if (rc != NB_OK) return rc;
+    if (layout != NB_ROTARY_HALF && layout != NB_ROTARY_NEIGHBOURS) return fail(NB_ERR_INVALID_ARG, "unknown layout %d", layout);
+    const int unit = layout == NB_ROTARY_HALF ? 16 : 8;
+    if (R <= 0 || R > D) return fail(NB_ERR_INVALID_ARG, "R must be within [1, D]");
+    if (R % unit != 0) return fail(NB_ERR_UNSUPPORTED, "R (%lld) must be a multiple of %d in this layout", static_cast<long long>(R), unit);
+    if ((rc = check_ld("out_q", ld_out_q, heads * D)) != NB_OK || (rc = check_ld("q", ld_q, heads * D)) != NB_OK) return rc;
+    if ((k || out_k) && ((rc = check_ld("out_k", ld_out_k, kv_heads * D)) != NB_OK || (rc = check_ld("k", ld_k, kv_heads * D)) != NB_OK)) return rc;
+    if (!std::isfinite(scale)) return fail(NB_ERR_INVALID_ARG, "scale must be finite");
+    if (T == 0 || n == 0) return NB_OK;  // tensors without elements have no address
+    if (!out_q || !q || !freq) return fail(NB_ERR_INVALID_ARG, "out_q, q and freq must not be NULL");
+    if (!k != !out_k) return fail(NB_ERR_INVALID_ARG, "k and out_k are given together or not at all");
+    if (!aligned16(out_q) || !aligned16(q) || !aligned16(out_k) || !aligned16(k) || (reinterpret_cast<uintptr_t>(freq) & 7u) || !aligned4(positions) ||
+        !aligned4(cu_seqlens))
+        return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, freq 8-byte, positions and cu_seqlens 4-byte aligned");
+    const Rows oq{out_q, ld_out_q * 2, heads * D * 2, T, true}, ok{out_k, ld_out_k * 2, kv_heads * D * 2, T, true},
+               iq{q, ld_q * 2, heads * D * 2, T, false}, ik{k, ld_k * 2, kv_heads * D * 2, T, false},
+               rest[] = {{freq, R * 4, R * 4, 1, false}, {positions, T * 4, T * 4, 1, false}, {cu_seqlens, (n + 1) * 4, (n + 1) * 4, 1, false}};
+    bool clash = overlap(oq, ok) || overlap(oq, ik) || overlap(ok, iq) || (overlap(oq, iq) && !(out_q == q && ld_out_q == ld_q)) ||
+                 (overlap(ok, ik) && !(out_k == k && ld_out_k == ld_k));
+    for (const Rows &r : rest) clash = clash || overlap(oq, r) || overlap(ok, r);
+    if (clash) return fail(NB_ERR_INVALID_ARG, "an output overlaps another argument (only out_q may be q, and out_k may be k)");
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    if ((rc = get_state(&s)) != NB_OK) return rc;
+    RotaryParams p{};
+    p.in[0] = q;
+    p.in[1] = k;
+    p.out[0] = out_q;
+    p.out[1] = out_k;
+    p.ld_in[0] = ld_q;
+    p.ld_in[1] = ld_k;
+    p.ld_out[0] = ld_out_q;
+    p.ld_out[1] = ld_out_k;
+    p.heads[0] = static_cast<int>(heads);
+    p.heads[1] = k ? static_cast<int>(kv_heads) : 0;
+    p.T = static_cast<int>(T);
+    p.n = static_cast<int>(n);
+    p.D = static_cast<int>(D);
+    p.R = static_cast<int>(R);
+    p.scale = scale;
+    p.sign = inverse ? -1.0f : 1.0f;
+    p.freq = static_cast<const double *>(freq);
+    p.positions = static_cast<const int *>(positions);
+    p.cu = static_cast<const int *>(cu_seqlens);
+    p.status = s->status;
+    // tokens of a block: one while that fills the device no more than four times
+    const int64_t want = T / (4 * s->num_sms) + 1;
+    const int tokens = static_cast<int>(want < kRotaryTokens ? want : kRotaryTokens);
+    const dim3 grid(static_cast<unsigned>((T + tokens - 1) / tokens));
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    rc = layout == NB_ROTARY_HALF ? launch_chained(rotary_kernel<true>, grid, kRotaryThreads, stream, p, tokens)
+                                  : launch_chained(rotary_kernel<false>, grid, kRotaryThreads, stream, p, tokens);
+    if (rc != NB_OK) return rc;
+    ++g_launches;
     return NB_OK;
 }
 
