@@ -604,6 +604,13 @@ int nb_debug_layernorm_timeout(void *out, const void *inp, const void *weight, c
  */
 int nb_debug_muon_timeout(void *update, const void *grad, void *workspace, int64_t workspace_bytes, int64_t limit_us);
 
+/*
+ * The same for the attention kernels (pass 0: forward, 1: dq, 2: dk and dv) over one sequence of 256 rows and one head of 64, whose streamed tiles wait for
+ * 16 bytes more than their copies bring. The products' bounded wait for the first of them runs out; nothing of the pass's results is written but, in pass 1, the workspace.
+ * nb_check_status() reports NB_ERR_TIMEOUT naming wait 300. tensors: q, k, v, out, lse, dout, dq, dk, dv, workspace.
+ */
+int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,7 @@ EXPORTS = (
     "nb_lora_da_stacked", "nb_debug_route", "nb_layernorm_forward", "nb_layernorm_workspace", "nb_layernorm_backward",
     "nb_muon_workspace", "nb_muon_update", "nb_muon_apply", "nb_debug_layernorm_timeout",
     "nb_debug_muon_timeout", "nb_rotary_frequencies", "nb_rotary", "nb_attention_forward", "nb_attention_workspace", "nb_attention_backward",
+    "nb_debug_attention_timeout",
 )
 
 CALL_FORWARD, CALL_BACKWARD, CALL_LORA_FORWARD, CALL_LORA_BACKWARD = range(4)
@@ -100,6 +101,7 @@ def lib() -> ctypes.CDLL:
         L.nb_debug_gemm_timeout.argtypes = [_vp, _vp, _vp, _i64]
         L.nb_debug_layernorm_timeout.argtypes = [_vp, _vp, _vp, _vp, _int, _i64]
         L.nb_debug_muon_timeout.argtypes = [_vp, _vp, _vp, _i64, _i64]
+        L.nb_debug_attention_timeout.argtypes = [ctypes.POINTER(_vp), _int, _i64]
         L.nb_debug_layer_bwd_plan.argtypes = [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_int), _i64]
         L.nb_debug_route.argtypes = [_int] + [_i64] * 4 + [_int] * 3 + [ctypes.POINTER(_int)]
         _lib = L
@@ -406,6 +408,12 @@ def nb_debug_muon_timeout(update, grad, workspace, workspace_bytes: int, limit_u
     _check(lib().nb_debug_muon_timeout(_ptr(update), _ptr(grad), _ptr(workspace), workspace_bytes, limit_us))
 
 
+def nb_debug_attention_timeout(tensors, which: int, limit_us: int) -> None:
+    """A pass of attention over 256 rows whose streamed tiles never come whole: exercises the kernels' time-out exit."""
+    lib().nb_set_stream(_stream())
+    _check(lib().nb_debug_attention_timeout((_vp * len(tensors))(*(_ptr(t) for t in tensors)), which, limit_us))
+
+
 def nb_debug_wait_timeout(limit_us: int) -> None:
     lib().nb_set_stream(_stream())
     _check(lib().nb_debug_wait_timeout(limit_us))
@@ -496,3 +504,89 @@ def muon_update(grad, momentum=None, mu=0.95, nesterov=True, steps=5, coefficien
     nb_muon_update(update, momentum, grad, len(grad), R, C, mu, int(nesterov), steps, *coefficients, eps, _stream_dtype(grad[0]), ws,
                    ws.numel())
     return update
+
+
+def rotary_frequencies(R, base=10000.0, factor=1.0, low=1.0, high=32.0, original=0, device="cuda"):
+    """The frequencies of nb_rotary_frequencies on the device, as nb_rotary takes them."""
+    return torch.tensor(nb_rotary_frequencies(R, base, factor, low, high, original), dtype=torch.float64, device=device)
+
+
+def _heads(t, name: str):
+    """(heads, D, ld) of a tensor [T, heads, D], whose rows may lie inside wider ones."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3:
+        raise ValueError(f"{name}: {torch.bfloat16} [T, heads, D] is wanted, not {t.dtype} {tuple(t.shape)}")
+    T, heads, D = t.shape
+    # of one row no stride is told: any will do
+    return heads, D, t.stride(0) if T > 1 else heads * D
+
+
+def _sequences(cu_seqlens, n: int, T: int, **others) -> int:
+    for name, t in others.items():
+        if t is not None and t.shape[0] != T:
+            raise ValueError(f"{name}: {t.shape[0]} rows, not {T}")
+    if cu_seqlens is None:
+        return n
+    if cu_seqlens.dtype != torch.int32 or cu_seqlens.dim() != 1 or len(cu_seqlens) < 1:
+        raise ValueError(f"cu_seqlens: {torch.int32} [n + 1] is wanted, not {cu_seqlens.dtype} {tuple(cu_seqlens.shape)}")
+    return len(cu_seqlens) - 1
+
+
+def _like(t, cu_seqlens, shape=None, dtype=torch.bfloat16):
+    """A dense tensor of t's shape; of zeros where there may be rows in no sequence, which a call does not write."""
+    make = torch.empty if cu_seqlens is None else torch.zeros
+    return make(t.shape if shape is None else shape, dtype=dtype, device=t.device)
+
+
+def rotary(q, k, freq, positions=None, cu_seqlens=None, n=1, scale=1.0, layout=ROTARY_HALF, inverse=False, in_place=False):
+    """nb_rotary of q [T, heads, D] and k [T, kv_heads, D] (or None); freq has R / 2 frequencies. Returns (q, k), new ones unless in_place."""
+    T = q.shape[0]
+    heads, D, ld_q = _heads(q, "q")
+    kv_heads, Dk, ld_k = _heads(k, "k") if k is not None else (1, D, D)
+    if Dk != D:
+        raise ValueError(f"k: heads of {Dk} columns, not {D}")
+    _want(freq, torch.float64, (freq.numel(),), "freq")
+    _want(positions, torch.int32, (T,), "positions")
+    n = _sequences(cu_seqlens, n, T, k=k)
+    out_q = q if in_place else _like(q, cu_seqlens)
+    out_k = k if in_place or k is None else _like(k, cu_seqlens)
+    nb_rotary(out_q, out_k, q, k, freq, positions, cu_seqlens, T, n, heads, kv_heads, D, 2 * freq.numel(), ld_q if in_place else heads * D,
+              ld_k if in_place else kv_heads * D, ld_q, ld_k, scale, layout, int(inverse))
+    return out_q, out_k
+
+
+def _attention_sizes(q, k, v):
+    (heads, D, ld_q), (kv_heads, Dk, ld_k), (kv2, Dv, ld_v) = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    if Dk != D or Dv != D or kv2 != kv_heads:
+        raise ValueError(f"k and v: heads of {D} columns are wanted, as many of both, not {tuple(k.shape)} and {tuple(v.shape)}")
+    return heads, kv_heads, D, ld_q, ld_k, ld_v
+
+
+def attention_forward(q, k, v, cu_seqlens=None, n=1, scale=None, causal=True, train=True):
+    """Allocate the outputs and call nb_attention_forward. q [T, heads, D], k and v [T, kv_heads, D]: dense, or columns of wider tensors.
+    Sequences by cu_seqlens (int32), or n of one length. scale: 1 / sqrt(D) where it is None. Returns (out, lse or None); rows in no sequence are zeros."""
+    T = q.shape[0]
+    heads, kv_heads, D, ld_q, ld_k, ld_v = _attention_sizes(q, k, v)
+    n = _sequences(cu_seqlens, n, T, k=k, v=v)
+    out = _like(q, cu_seqlens)
+    lse = _like(q, cu_seqlens, (heads, T), torch.float32) if train else None
+    nb_attention_forward(out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, heads * D, ld_q, ld_k, ld_v, D ** -0.5 if scale is None else scale,
+                         int(causal))
+    return out, lse
+
+
+def attention_backward(dout, out, lse, q, k, v, cu_seqlens=None, n=1, scale=None, causal=True, grads=None):
+    """Allocate the workspace and missing gradients and call nb_attention_backward. grads: (dq, dk, dv) to be written, columns of one
+    buffer for example; rows in no sequence are left as they are (zeros where they are allocated here). Returns (dq, dk, dv)."""
+    T = q.shape[0]
+    heads, kv_heads, D, ld_q, ld_k, ld_v = _attention_sizes(q, k, v)
+    n = _sequences(cu_seqlens, n, T, k=k, v=v)
+    for t, name in ((dout, "dout"), (out, "out")):
+        _want(t, torch.bfloat16, q.shape, name)
+    _want(lse, torch.float32, (heads, T), "lse")
+    dq, dk, dv = grads if grads is not None else (_like(t, cu_seqlens) for t in (q, k, v))
+    for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        _want(t, torch.bfloat16, like.shape, name)
+    ws = torch.empty(nb_attention_workspace(T, heads), dtype=torch.uint8, device=q.device)
+    nb_attention_backward(dq, dk, dv, dout, out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, *(_heads(t, "")[2] for t in (dq, dk, dv, dout, out)),
+                          ld_q, ld_k, ld_v, D ** -0.5 if scale is None else scale, int(causal), ws, ws.numel())
+    return dq, dk, dv

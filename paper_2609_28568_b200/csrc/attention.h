@@ -19,6 +19,7 @@ struct AttnParams {
     float *lse;              // [heads, T]; forward: or null
     int *status;
     unsigned long long timeout_ns;
+    int withhold;            // nb_debug_attention_timeout only: bytes that a tile of the ring waits for beyond what its copies bring
 };
 
 struct AttnBackward {

@@ -84,6 +84,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             ptx::st_shared_u32(span_addr + 8, static_cast<uint32_t>(s.block));
         }
     }
+    if (warp == 11 && blockIdx.x == 0 && p.cu) attn_report_bounds(p.cu, p.n, p.T, p.status);
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
@@ -121,7 +122,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                 const bool part = valid < 128 && valid < up;
                 if (ptx::elect_one()) {
                     const uint32_t bar = part ? part_bar : full_bar(stage);
-                    ptx::mbar_expect_tx(bar, Cfg::TILE);
+                    ptx::mbar_expect_tx(bar, Cfg::TILE + p.withhold);
                     attn_load<D>(dst, (i & 1) ? &tmV : &tmK, bar, kv_head, start + j * 128);
                 }
                 __syncwarp();
@@ -336,6 +337,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             ptx::st_shared_u32(span_addr + 8, static_cast<uint32_t>(s.block));
         }
     }
+    if (warp == 11 && blockIdx.x == 0 && p.cu) attn_report_bounds(p.cu, p.n, p.T, p.status);
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
@@ -373,7 +375,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 const bool part = valid < 128 && valid < up;
                 if (ptx::elect_one()) {
                     const uint32_t bar = part ? part_bar : full_bar(stage);
-                    ptx::mbar_expect_tx(bar, Cfg::TILE);
+                    ptx::mbar_expect_tx(bar, Cfg::TILE + p.withhold);
                     attn_load<D>(dst, (i & 1) ? &tmDO : &tmQ, bar, kv_head * p.group + g, start + t * 128);
                 }
                 __syncwarp();

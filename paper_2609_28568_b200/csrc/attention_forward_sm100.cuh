@@ -80,6 +80,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             ptx::st_shared_u32(span_addr + 8, static_cast<uint32_t>(s.block));
         }
     }
+    if (warp == 11 && blockIdx.x == 0 && p.cu) attn_report_bounds(p.cu, p.n, p.T, p.status);
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
@@ -125,7 +126,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const bool part = (i & 1) && valid < 128 && valid < up;
                 if (ptx::elect_one()) {
                     const uint32_t bar = part ? part_bar : full_bar(stage);
-                    ptx::mbar_expect_tx(bar, Cfg::TILE);
+                    ptx::mbar_expect_tx(bar, Cfg::TILE + p.withhold);
                     attn_load<D>(dst, (i & 1) ? &tmV : &tmK, bar, kv_head, start + j * 128);
                 }
                 __syncwarp();
@@ -244,9 +245,11 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             if (j == 0) {
                 top = now;
             } else if (__any_sync(0xffffffffu, (now - top) * sl > 8.0f)) {
-                const float to = fmaxf(top, now), f = ptx::ex2_approx((top - to) * sl);
+                // only rows that grew that much: a row's bits do not depend on its neighbours
+                const bool grown = (now - top) * sl > 8.0f;
+                const float f = grown ? ptx::ex2_approx((top - now) * sl) : 1.0f;
                 total *= f;
-                top = to;
+                if (grown) top = now;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];

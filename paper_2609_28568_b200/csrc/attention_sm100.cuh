@@ -24,7 +24,8 @@ struct AttnSpan {
 
 // The sequence and block that a slot stands for, found by one warp. Sequence i has the slots from cu[i] / rows + i on, at least as many as it
 // has blocks of `rows` rows, so that no sums over the sequences before it are needed; it uses the last ones first (with a
-// causal mask they have the most work). Bounds outside [0, T] or falling ones are cut to an empty or shorter sequence and reported.
+// causal mask they have the most work). Bounds outside [0, T] or falling ones
+// are cut to an empty or shorter sequence (and reported by attn_report_bounds).
 __device__ __forceinline__ AttnSpan attn_span(const AttnParams &p, int slot, int rows, bool descending)
 {
     const int lane = static_cast<int>(threadIdx.x & 31);
@@ -50,7 +51,6 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnParams &p, int slot, int
         }
         const int a = p.cu[lo], b = p.cu[lo + 1];
         const int start = min(max(a, 0), p.T), end = min(max(b, start), p.T);
-        if ((start != a || end != b) && lane == 0 && atomicCAS(p.status, 0, kStatusBadSequences) == 0) p.status[1] = lo;
         at = max(a, 0) / rows + lo;
         s.start = start;
         s.len = end - start;
@@ -59,6 +59,14 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnParams &p, int slot, int
     const int blocks = (s.len + rows - 1) / rows;
     s.block = local < 0 || local >= blocks ? -1 : descending ? blocks - 1 - local : local;
     return s;
+}
+
+// Reports bounds that fall or leave [0, T]; by one warp of a launch.
+__device__ __forceinline__ void attn_report_bounds(const int *cu, int n, int T, int *status)
+{
+    for (int i = static_cast<int>(threadIdx.x & 31); i <= n; i += 32)
+        if (cu[i] < (i ? cu[i - 1] : 0) || cu[i] > T)
+            if (atomicCAS(status, 0, kStatusBadSequences) == 0) status[1] = i;
 }
 
 __device__ __forceinline__ bool warp_wait(const WaitCtx &w, uint32_t bar, uint32_t parity, int where)

@@ -3349,6 +3349,45 @@ int nb_debug_layernorm_timeout(void *out, const void *inp, const void *weight, c
     return NB_OK;
 }
 
+int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us)
+{
+    if (!tensors) return fail(NB_ERR_INVALID_ARG, "tensors must not be NULL");
+    for (int i = 0; i < 10; ++i) {
+        if (!tensors[i]) return fail(NB_ERR_INVALID_ARG, "tensor %d has a NULL pointer", i);
+        if (!aligned16(tensors[i])) return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+    }
+    if (pass < 0 || pass > 2) return fail(NB_ERR_INVALID_ARG, "unknown pass %d", pass);
+    if (limit_us < 100 || limit_us > 1000000) return fail(NB_ERR_INVALID_ARG, "limit_us must be within [100, 1000000]");
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *s;
+    int rc = get_state(&s);
+    if (rc != NB_OK) return rc;
+    const int64_t T = 256, D = 64;  // one head, two tiles
+    AttnBackward b{};
+    b.a = attn_params(*s, T, 1, 1, 1, D, nullptr, 0.125f, 1);
+    b.a.timeout_ns = static_cast<unsigned long long>(limit_us) * 1000ull;
+    b.a.withhold = 16;
+    b.a.out = tensors[3];
+    b.a.lse = static_cast<float *>(tensors[4]);
+    b.a.ld_out = b.ld_dout = b.ld_dq = b.ld_dk = b.ld_dv = D;
+    b.dout = tensors[5];
+    b.dq = tensors[6];
+    b.dk = tensors[7];
+    b.dv = tensors[8];
+    b.delta = static_cast<float *>(tensors[9]);
+    CUtensorMap q, k, v, dout;
+    if ((rc = get_heads_tmap(*s, &q, tensors[0], T, D, 1, D)) != NB_OK || (rc = get_heads_tmap(*s, &k, tensors[1], T, D, 1, D)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &v, tensors[2], T, D, 1, D)) != NB_OK || (rc = get_heads_tmap(*s, &dout, tensors[5], T, D, 1, D)) != NB_OK)
+        return rc;
+    static bool attr_set[3][kMaxDevices] = {};
+    if (pass == 0) {
+        CUtensorMap maps[3] = {q, k, v};
+        return launch_attention(attn_forward(D), attr_set[0], maps, b.a, attn_slots(b.a, 256), 1, g_stream);
+    }
+    CUtensorMap maps[4] = {q, dout, k, v};
+    return launch_attention(pass == 1 ? attn_backward_q(D) : attn_backward_kv(D), attr_set[pass], maps, b, attn_slots(b.a, 128), 1, g_stream);
+}
+
 int nb_debug_muon_timeout(void *update, const void *grad, void *workspace, int64_t workspace_bytes, int64_t limit_us)
 {
     const int64_t n = 128;

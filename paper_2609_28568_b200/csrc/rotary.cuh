@@ -82,8 +82,8 @@ rotary_kernel(const RotaryParams p, int tokens)
     auto load = [&](RotaryItem &x) {
         const int t = h < p.heads[0] ? 0 : 1, hh = t ? h - p.heads[0] : h;
         const long long row = row0 + tok;
-        x.in = static_cast<const __nv_bfloat16 *>(p.in[t]) + row * p.ld_in[t] + hh * p.D + col;
-        x.out = static_cast<__nv_bfloat16 *>(p.out[t]) + row * p.ld_out[t] + hh * p.D + col;
+        x.in = static_cast<const __nv_bfloat16 *>(t ? p.in[1] : p.in[0]) + row * (t ? p.ld_in[1] : p.ld_in[0]) + hh * p.D + col;
+        x.out = static_cast<__nv_bfloat16 *>(t ? p.out[1] : p.out[0]) + row * (t ? p.ld_out[1] : p.ld_out[0]) + hh * p.D + col;
         x.a = ptx::ld_global_v4(x.in);
         if (HALF && turns) x.b = ptx::ld_global_v4(x.in + pairs);
     };
