@@ -6,21 +6,21 @@
 
 namespace nb {
 
-AttnKernel attn_forward(int D)
+template <class Cfg>
+static AttnKernel forward_kernel()
 {
-    if (D <= 64) return {reinterpret_cast<const void *>(&attn_forward_kernel<64>), AttnFwdCfg<64>::SMEM};
-    return {reinterpret_cast<const void *>(&attn_forward_kernel<128>), AttnFwdCfg<128>::SMEM};
+    return {reinterpret_cast<const void *>(&attn_forward_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM, 128, Cfg::KEYS};
 }
-
+AttnKernel attn_forward(int D) { return D <= 64 ? forward_kernel<AttnFwdCfg<64>>() : forward_kernel<AttnFwdCfg<128>>(); }
 AttnKernel attn_backward_q(int D)
 {
-    if (D <= 64) return {reinterpret_cast<const void *>(&attn_backward_q_kernel<64>), AttnBwdCfg<64>::SMEM_Q};
-    return {reinterpret_cast<const void *>(&attn_backward_q_kernel<128>), AttnBwdCfg<128>::SMEM_Q};
+    if (D <= 64) return {reinterpret_cast<const void *>(&attn_backward_q_kernel<64>), kAttnThreads, AttnBwdCfg<64>::SMEM_Q, 128, 128};
+    return {reinterpret_cast<const void *>(&attn_backward_q_kernel<128>), kAttnThreads, AttnBwdCfg<128>::SMEM_Q, 128, 128};
 }
 AttnKernel attn_backward_kv(int D)
 {
-    if (D <= 64) return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<64>), AttnBwdCfg<64>::SMEM_KV};
-    return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<128>), AttnBwdCfg<128>::SMEM_KV};
+    if (D <= 64) return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<64>), kAttnThreads, AttnBwdCfg<64>::SMEM_KV, 128, 128};
+    return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<128>), kAttnThreads, AttnBwdCfg<128>::SMEM_KV, 128, 128};
 }
 
 }  // namespace nb

@@ -5,7 +5,7 @@
 namespace nb {
 
 constexpr int kAttnTile = 128;
-constexpr int kAttnThreads = 384;  // two warpgroups on scores, warp 8: loads, warp 9: products
+constexpr int kAttnThreads = 384;  // backward: two warpgroups on scores, warp 8: loads, warp 9: products
 constexpr int kStatusBadSequences = 6;
 
 struct AttnParams {
@@ -30,10 +30,12 @@ struct AttnBackward {
     long long ld_dout, ld_dq, ld_dk, ld_dv;
 };
 
-// A kernel for heads of D columns and its dynamic shared memory. Parameters: its tensor maps (forward: q, k, v), then AttnParams or AttnBackward.
+// A kernel for heads of D columns, its threads, its dynamic shared memory, the rows of a block and those of the tiles that it walks over. Parameters: its tensor maps (forward: q, k, v), then AttnParams or AttnBackward.
 struct AttnKernel {
     const void *fn;
+    int threads;
     uint32_t smem;
+    int rows, streamed;
 };
 AttnKernel attn_forward(int D);
 AttnKernel attn_backward_q(int D);   // maps: q, dout, k, v

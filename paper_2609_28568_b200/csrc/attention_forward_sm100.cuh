@@ -1,13 +1,21 @@
-// Attention forward: one block per 256 rows of a sequence and head.
+// Attention forward, on items of 128 rows of a sequence and head, two blocks to an SM.
 //
-// Two tiles of 128 queries share the keys and values that stream through shared memory. A thread of a warpgroup owns a row of its
-// tile: scores come from tensor memory, the running maximum and sum stay in registers, probabilities go back to tensor
-// memory as bf16 (over the scores) and are the A operand of the product with V. While one warpgroup works on its scores,
-// the tensor core works for the other.
+// A thread of a warpgroup owns a query: scores come from tensor memory, 64 keys at a time, the running maximum and sum stay in
+// registers, probabilities go back to tensor memory as bf16, over the scores, and are the A operand of the product with V. With two tiles of
+// scores the next one is formed while the exponentials of this one run.
+//
+// What bounds it are the exponentials (16 a clock and SM) and the latencies of a step (scores, maximum, exponentials, the way back); the two
+// blocks of an SM fill each other's gaps. Two tiles of queries in one block that share keys and values took as long on one long sequence and a fifth longer
+// on packed ones; 128 keys at a time took the same, and more registers. A quarter of the exponentials formed by a polynomial, on the multipliers, saved
+// nothing: those instructions wait in the same line.
+//
+// Items differ in work by the length of their sequence and their place in it, and are short beside what a block costs to start (first loads, first
+// products: 2 to 3 us). So a block that is done with its item takes another off the grid (the hardware hands out blocks that have not
+// started), asks for it an item ahead, and its loads and first scores come while the last output is still being stored.
 //
 // The output accumulator in tensor memory is rescaled only when a row's maximum has grown by more than 2^8 since the last
 // rescaling: until then probabilities up to 2^8 are summed against the old maximum, which changes no bit of their relative precision.
-// Probabilities are rounded to bf16 for the tensor core (half an ulp, 2^-9 of each); their sum takes them unrounded.
+// Probabilities are rounded to bf16 for the tensor core (half an ulp, 2^-8 of each at most); their sum takes them unrounded.
 #pragma once
 #include "attention_sm100.cuh"
 
@@ -15,22 +23,28 @@ namespace nb {
 
 template <int D_>
 struct AttnFwdCfg {
-    static constexpr int D = D_;
-    static constexpr uint32_t TILE = 128 * D_ * 2;
-    static constexpr int STAGES = D_ == 64 ? 8 : 4;  // keys and values in turn
+    static constexpr int D = D_, KEYS = 64;  // keys of a tile
+    static constexpr int THREADS = 256, BLOCKS = 2;
+    static constexpr uint32_t TMEM = 256, TM_O = 2 * KEYS;  // scores from 0 on
+    static constexpr uint32_t Q_BYTES = 128 * D_ * 2, TILE = KEYS * D_ * 2;
+    static constexpr uint32_t MOST = 113 * 1024;  // of shared memory: 228 KB of an SM less 1 KB a block
+    static constexpr int STAGES = (MOST - Q_BYTES - 512) / TILE < 8 ? (MOST - Q_BYTES - 512) / TILE : 8;  // keys and values in turn
     static constexpr uint32_t OFF_Q = 0;
-    static constexpr uint32_t OFF_KV = 2 * TILE;
+    static constexpr uint32_t OFF_KV = Q_BYTES;
     static constexpr uint32_t OFF_BAR = OFF_KV + STAGES * TILE;
-    static constexpr uint32_t SMEM = OFF_BAR + 256;
-    static_assert(SMEM <= 232448, "shared memory");
+    static constexpr uint32_t SMEM = OFF_BAR + 512;
+    // registers of a thread after they have been divided anew: within the 128 that the block is launched with
+    static constexpr int REGS_ROWS = 192, REGS_OTHER = 64;
+    static_assert(REGS_ROWS + REGS_OTHER <= 2 * 128, "registers");
+    static_assert(TMEM >= TM_O + D_ && STAGES >= 4 && SMEM <= MOST, "memory");
 };
 
-template <int D>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+template <class Cfg>
+__global__ void __launch_bounds__(Cfg::THREADS, Cfg::BLOCKS)
 attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                     const AttnParams p)
 {
-    using Cfg = AttnFwdCfg<D>;
+    constexpr int D = Cfg::D, KEYS = Cfg::KEYS, STAGES = Cfg::STAGES, LOAD = 4, MMA = 5;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem = ptx::smem_u32(smem_raw);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
@@ -40,22 +54,49 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 
     const uint32_t bar0 = smem + Cfg::OFF_BAR;
     auto full_bar = [&](int s) { return bar0 + 8u * s; };
-    auto empty_bar = [&](int s) { return bar0 + 8u * (Cfg::STAGES + s); };
-    auto named = [&](int i) { return bar0 + 8u * (2 * Cfg::STAGES + i); };
-    auto q_bar = [&](int t) { return named(t); };
-    auto s_bar = [&](int t) { return named(2 + t); };  // scores are there (and the product before them is done)
-    auto p_bar = [&](int t) { return named(4 + t); };  // probabilities are there
-    auto o_bar = [&](int t) { return named(6 + t); };  // the output is complete
-    const uint32_t part_bar = named(8);                // values of a sequence's last tile have landed
-    const uint32_t tmem_slot = bar0 + 232, abort_addr = bar0 + 236, span_addr = bar0 + 240;
-    static_assert(8 * (2 * Cfg::STAGES + 9) <= 232, "barriers");
+    auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
+    auto named = [&](int i) { return bar0 + 8u * (2 * STAGES + i); };
+    const uint32_t q_bar = named(0), qfree_bar = named(1);    // queries are there, and have been used
+    // of even and odd tiles, since a warpgroup may be two of them ahead of the products
+    auto s_bar = [&](uint32_t r) { return named(2 + (r & 1)); };  // scores are there
+    auto p_bar = [&](uint32_t r) { return named(4 + (r & 1)); };  // probabilities are there
+    auto o_bar = [&](uint32_t r) { return named(6 + (r & 1)); };  // their product with V is done
+    auto half = [](uint32_t r) { return (r >> 1) & 1u; };         // parity of the r-th tile in them
+    auto item_bar = [&](int i) { return named(8 + i); };          // an item has been put down
+    auto ifree_bar = [&](int i) { return named(10 + i); };        // and been read by all
+    const uint32_t part_bar = named(12), next_bar = named(13);    // values of a sequence's last tile, the next item have come
+    const uint32_t answer = bar0 + 400, item0 = bar0 + 416;   // 16 bytes; two of 16
+    const uint32_t tmem_slot = bar0 + 480, abort_addr = bar0 + 484;
+    static_assert(8 * (2 * STAGES + 14) <= 400, "barriers");
 
-    if (warp == 8) {
-        if (lane < Cfg::STAGES) {
+    const WaitCtx wctx{abort_addr, p.status, p.timeout_ns};
+    // The waits for a whole round of work have twice the limit, so that the wait closest to the cause of a stall is reported.
+    const WaitCtx wctx2{abort_addr, p.status, 2 * p.timeout_ns};
+    struct Item {
+        int start, len, block, head;
+    };
+    auto tiles_of = [&](const Item &m) {  // tiles of keys that an item's queries see
+        const int tiles = (m.len + KEYS - 1) / KEYS;
+        return p.causal ? min(tiles, (m.block + 1) * (128 / KEYS)) : tiles;
+    };
+    // the k-th item, by one thread of a warp for all; no more: block < 0
+    auto take = [&](int k, Item &m, bool all) {
+        const uint32_t par = static_cast<uint32_t>(k >> 1) & 1u, at = item0 + (k & 1) * 16;
+        if (!(all ? warp_wait(wctx2, item_bar(k & 1), par, 500) : wait_barrier(wctx2, item_bar(k & 1), par, 500))) return false;
+        uint32_t v[4];
+        ptx::ld_shared_v4(at, v[0], v[1], v[2], v[3]);
+        m = {static_cast<int>(v[0]), static_cast<int>(v[1]), static_cast<int>(v[2]), static_cast<int>(v[3])};
+        if (all) __syncwarp();
+        if (!all || lane == 0) ptx::mbar_arrive(ifree_bar(k & 1));
+        return m.block >= 0;
+    };
+
+    if (warp == LOAD) {
+        if (lane < STAGES) {
             ptx::mbar_init(full_bar(lane), 1);
             ptx::mbar_init(empty_bar(lane), 1);
         }
-        if (lane < 9) ptx::mbar_init(named(lane), lane == 4 || lane == 5 ? 4 : 1);
+        if (lane < 14) ptx::mbar_init(named(lane), lane == 4 || lane == 5 ? 4 : lane == 10 || lane == 11 ? 5 : 1);
         if (lane == 31) ptx::st_shared_u32_volatile(abort_addr, 0);
         ptx::fence_barrier_init();
         if (lane == 30) {
@@ -65,234 +106,231 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
         __syncwarp();
     }
-    if (warp == 9) {
-        ptx::tmem_alloc<1>(tmem_slot, 512);
+    if (warp == MMA) {
+        ptx::tmem_alloc<1>(tmem_slot, Cfg::TMEM);
         ptx::tmem_relinquish<1>();
     }
-    ptx::grid_launch_dependents();
-    ptx::grid_dependency_wait();
-    const int head = static_cast<int>(blockIdx.x) % p.heads;
-    if (warp == 0) {
-        const AttnSpan s = attn_span(p, static_cast<int>(blockIdx.x) / p.heads, 256, true);
-        if (lane == 0) {
-            ptx::st_shared_u32(span_addr, static_cast<uint32_t>(s.start));
-            ptx::st_shared_u32(span_addr + 4, static_cast<uint32_t>(s.len));
-            ptx::st_shared_u32(span_addr + 8, static_cast<uint32_t>(s.block));
-        }
-    }
-    if (warp == 11 && blockIdx.x == 0 && p.cu) attn_report_bounds(p.cu, p.n, p.T, p.status);
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem = ptx::ld_shared_u32_volatile(tmem_slot);
-    const int start = static_cast<int>(ptx::ld_shared_u32_volatile(span_addr)), len = static_cast<int>(ptx::ld_shared_u32_volatile(span_addr + 4)),
-              block = static_cast<int>(ptx::ld_shared_u32_volatile(span_addr + 8));
-    const WaitCtx wctx{abort_addr, p.status, p.timeout_ns};
-    // The waits for a whole round of work have twice the limit, so that the wait closest to the cause of a stall is reported.
-    const WaitCtx wctx2{abort_addr, p.status, 2 * p.timeout_ns};
+    ptx::grid_launch_dependents();
+    ptx::grid_dependency_wait();
 
-    const int q0 = block * 256;
-    const int kv_tiles = (len + 127) / 128;
-    auto tiles_of = [&](int t) {  // tiles of keys that queries' tile t sees
-        const int row = q0 + t * 128;
-        return row >= len ? 0 : p.causal ? min(kv_tiles, row / 128 + 1) : kv_tiles;
-    };
-    const int n0 = tiles_of(0), n1 = tiles_of(1), nkv = max(n0, n1);
-
-    if (!smem_ok || block < 0) {
+    if (!smem_ok) {
         // nothing to do
-    } else if (warp >= 8) {
-        ptx::setmaxnreg_dec<64>();
-        if (warp == 8) {
-            // ------------------------------------------------------------ loads
-            const int kv_head = head / p.group;
-            if (ptx::elect_one()) {
-                ptx::mbar_expect_tx(q_bar(0), Cfg::TILE);
-                attn_load<D>(smem + Cfg::OFF_Q, &tmQ, q_bar(0), head, start + q0);
-                if (n1 > 0) {
-                    ptx::mbar_expect_tx(q_bar(1), Cfg::TILE);
-                    attn_load<D>(smem + Cfg::OFF_Q + Cfg::TILE, &tmQ, q_bar(1), head, start + q0 + 128);
-                }
-            }
+    } else if (warp >= LOAD) {
+        ptx::setmaxnreg_dec<Cfg::REGS_OTHER>();
+        if (warp == LOAD) {
+            // ------------------------------------------------------------ items, and their loads: keys of a tile, its values
             bool ok = true;
             int stage = 0;
-            uint32_t phase = 0;
-            for (int i = 0; i < 2 * nkv && ok; ++i) {
-                const int j = i >> 1;
-                ok = warp_wait(wctx2, empty_bar(stage), phase ^ 1u, 100 + stage);
-                if (!ok) break;
-                const uint32_t dst = smem + Cfg::OFF_KV + stage * Cfg::TILE;
-                const int valid = len - j * 128, up = (valid + 15) & ~15;
-                const bool part = (i & 1) && valid < 128 && valid < up;
-                if (ptx::elect_one()) {
-                    const uint32_t bar = part ? part_bar : full_bar(stage);
-                    ptx::mbar_expect_tx(bar, Cfg::TILE + p.withhold);
-                    attn_load<D>(dst, (i & 1) ? &tmV : &tmK, bar, kv_head, start + j * 128);
-                }
-                __syncwarp();
-                if (part) {
-                    ok = warp_wait(wctx, part_bar, 0, 150);
-                    if (!ok) break;
-                    attn_zero_rows<D>(dst, valid, up);
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(full_bar(stage));
-                }
-                if (++stage == Cfg::STAGES) {
-                    stage = 0;
-                    phase ^= 1u;
-                }
-            }
-        } else if (warp == 9) {
-            // ------------------------------------------------------------ products
-            const uint32_t idesc_s = make_idesc(128, 128, false, false);
-            const int nd = (p.D + 15) & ~15, dsteps = nd / 16;
-            const uint32_t idesc_o = make_idesc(128, nd, false, true);
-            const uint32_t q_s[2] = {smem + Cfg::OFF_Q, smem + Cfg::OFF_Q + Cfg::TILE};
-            if (ptx::elect_one()) {
-                int stage = 0;
-                uint32_t phase = 0;
-                auto next = [&] {
-                    if (++stage == Cfg::STAGES) {
-                        stage = 0;
-                        phase ^= 1u;
+            uint32_t phase = 0, parts = 0, asked = 0, used = 0;
+            for (int k = 0, at = static_cast<int>(blockIdx.x); ok;) {
+                if (at >= 0) {
+                    if (ptx::elect_one()) {  // the one after
+                        ptx::mbar_expect_tx(next_bar, 16);
+                        ptx::launch_cancel(answer, next_bar);
                     }
-                };
-                auto tile = [&](int s) { return smem + Cfg::OFF_KV + s * Cfg::TILE; };
-                const int nt[2] = {n0, n1};
-                bool ok = wait_barrier(wctx, full_bar(0), 0, 300);
-                for (int t = 0; t < 2 && ok; ++t) {
-                    if (nt[t] == 0) continue;
-                    ok = wait_barrier(wctx, q_bar(t), 0, 330 + t);
-                    if (!ok) break;
-                    ptx::tc_fence_after();
-                    attn_mma_kk(tmem + t * 128, q_s[t], tile(0), idesc_s, dsteps);
-                    ptx::umma_commit<1>(s_bar(t));
+                    __syncwarp();
                 }
-                if (ok) ptx::umma_commit<1>(empty_bar(0));
-                next();
-                for (int j = 0; j < nkv && ok; ++j) {
-                    const int vs = stage;
-                    ok = wait_barrier(wctx, full_bar(vs), phase, 300 + vs);
+                Item m{0, 0, -1, 0};
+                if (at >= 0) {
+                    const AttnSpan s = attn_span(p, at / p.heads, 128, true);
+                    m = {s.start, s.len, s.block, at % p.heads};
+                }
+                if (at < 0 || m.block >= 0) {  // slots without a block are passed over
+                    ok = warp_wait(wctx2, ifree_bar(k & 1), (static_cast<uint32_t>(k >> 1) & 1u) ^ 1u, 510);
                     if (!ok) break;
-                    next();
-                    const int ks = stage;
-                    const uint32_t kphase = phase;
-                    if (j + 1 < nkv) next();
-                    const int steps = (min(128, len - j * 128) + 15) / 16;
-                    for (int t = 0; t < 2 && ok; ++t) {
-                        if (j >= nt[t]) continue;
-                        ok = wait_barrier(wctx2, p_bar(t), static_cast<uint32_t>(j) & 1u, 350 + t);
+                    if (lane == 0) {
+                        ptx::st_shared_v4(item0 + (k & 1) * 16, static_cast<uint32_t>(m.start), static_cast<uint32_t>(m.len),
+                                          static_cast<uint32_t>(m.block), static_cast<uint32_t>(m.head));
+                        ptx::mbar_arrive(item_bar(k & 1));
+                    }
+                    __syncwarp();
+                    ++k;
+                    if (at < 0) break;
+                    const int n = tiles_of(m), kv_head = m.head / p.group;
+                    for (int i = 0; i < 2 * n && ok; ++i) {
+                        const int j = i >> 1;
+                        ok = warp_wait(wctx2, empty_bar(stage), phase ^ 1u, 100 + stage);
                         if (!ok) break;
-                        ptx::tc_fence_after();
-                        attn_mma_tn(tmem + 256 + t * D, tmem + t * 128, tile(vs), idesc_o, steps, j > 0);
-                        if (j + 1 < nt[t]) {
-                            ok = wait_barrier(wctx, full_bar(ks), kphase, 300 + ks);
+                        const uint32_t dst = smem + Cfg::OFF_KV + stage * Cfg::TILE;
+                        const int valid = m.len - j * KEYS, up = (valid + 15) & ~15;
+                        const bool part = (i & 1) && valid < KEYS && valid < up;
+                        if (ptx::elect_one()) {
+                            const uint32_t bar = part ? part_bar : full_bar(stage);
+                            ptx::mbar_expect_tx(bar, Cfg::TILE + p.withhold);
+                            attn_load<D, KEYS>(dst, (i & 1) ? &tmV : &tmK, bar, kv_head, m.start + j * KEYS);
+                        }
+                        __syncwarp();
+                        if (part) {
+                            ok = warp_wait(wctx, part_bar, parts++ & 1u, 150);
                             if (!ok) break;
-                            ptx::tc_fence_after();
-                            attn_mma_kk(tmem + t * 128, q_s[t], tile(ks), idesc_s, dsteps);
-                            ptx::umma_commit<1>(s_bar(t));
-                        } else {
-                            ptx::umma_commit<1>(o_bar(t));
+                            attn_zero_rows<D, KEYS>(dst, valid, up);
+                            ptx::fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) ptx::mbar_arrive(full_bar(stage));
+                        }
+                        if (++stage == STAGES) {
+                            stage = 0;
+                            phase ^= 1u;
+                        }
+                        if (i == 0) {  // the queries after the first keys: these may be waiting for the item before
+                            ok = warp_wait(wctx2, qfree_bar, (used++ & 1u) ^ 1u, 130);
+                            if (ok && ptx::elect_one()) {
+                                ptx::mbar_expect_tx(q_bar, Cfg::Q_BYTES);
+                                attn_load<D>(smem + Cfg::OFF_Q, &tmQ, q_bar, m.head, m.start + m.block * 128);
+                            }
+                            __syncwarp();
                         }
                     }
                     if (!ok) break;
-                    ptx::umma_commit<1>(empty_bar(vs));
-                    if (j + 1 < nkv) ptx::umma_commit<1>(empty_bar(ks));
+                }
+                ok = warp_wait(wctx2, next_bar, asked++ & 1u, 520);
+                if (!ok) break;
+                at = ptx::launch_cancelled(answer);
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+            }
+        } else if (warp == MMA) {
+            // ------------------------------------------------------------ products
+            const uint32_t idesc_s = make_idesc(128, KEYS, false, false);
+            const int nd = (p.D + 15) & ~15, dsteps = nd / 16;
+            const uint32_t idesc_o = make_idesc(128, nd, false, true);
+            if (ptx::elect_one()) {
+                uint32_t done = 0;  // tiles before this item: 2 done of the ring
+                auto stage = [&](uint32_t i) { return static_cast<int>((2 * done + i) % STAGES); };
+                auto tile = [&](uint32_t i) { return smem + Cfg::OFF_KV + stage(i) * Cfg::TILE; };
+                auto ready = [&](uint32_t i) { return wait_barrier(wctx, full_bar(stage(i)), ((2 * done + i) / STAGES) & 1u, 300 + stage(i)); };
+                Item m;
+                for (int k = 0; take(k, m, false); ++k) {
+                    const int n = tiles_of(m);
+                    auto scores = [&](int j) {
+                        if (!ready(2 * j)) return false;
+                        ptx::tc_fence_after();
+                        attn_mma_kk<KEYS>(tmem + ((done + j) & 1) * KEYS, smem + Cfg::OFF_Q, tile(2 * j), idesc_s, dsteps);
+                        ptx::umma_commit<1>(s_bar(done + j));
+                        ptx::umma_commit<1>(empty_bar(stage(2 * j)));
+                        if (j + 1 == n) ptx::umma_commit<1>(qfree_bar);
+                        return true;
+                    };
+                    bool ok = wait_barrier(wctx, q_bar, static_cast<uint32_t>(k) & 1u, 330) && scores(0);
+                    for (int j = 0; j < n && ok; ++j) {
+                        if (j + 1 < n) ok = scores(j + 1);
+                        ok = ok && ready(2 * j + 1) && wait_barrier(wctx2, p_bar(done + j), half(done + j), 350);
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+                        attn_mma_tn<false, KEYS>(tmem + Cfg::TM_O, tmem + ((done + j) & 1) * KEYS, tile(2 * j + 1), idesc_o,
+                                                 (min(KEYS, m.len - j * KEYS) + 15) / 16, j > 0);
+                        ptx::umma_commit<1>(o_bar(done + j));
+                        ptx::umma_commit<1>(empty_bar(stage(2 * j + 1)));
+                    }
+                    if (!ok) break;
+                    done += n;
                 }
             }
             __syncwarp();
+        } else if (warp == MMA + 1 && blockIdx.x == 0 && p.cu) {
+            attn_report_bounds(p.cu, p.n, p.T, p.status);
         }
     } else {
         // ------------------------------------------------------------ scores: a row per thread
-        ptx::setmaxnreg_inc<216>();
-        const int t = warp >> 2, nt = t == 0 ? n0 : n1;
-        const int row = q0 + t * 128 + (warp & 3) * 32 + lane;  // of the sequence
-        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t s_tm = tmem + lanes + t * 128, o_tm = tmem + lanes + 256 + t * D;
+        ptx::setmaxnreg_inc<Cfg::REGS_ROWS>();
+        const uint32_t tm = tmem + (static_cast<uint32_t>(warp * 32) << 16), o_tm = tm + Cfg::TM_O;
         const float sl = p.scale * kLog2e;
         const ptx::f2 sl2 = ptx::make_f2(sl, sl);
-        float top = 0.0f, total = 0.0f;  // the maximum that the sums refer to (of unscaled scores), the sum
-        bool ok = true;
-        for (int j = 0; j < nt; ++j) {
-            ok = warp_wait(wctx2, s_bar(t), static_cast<uint32_t>(j) & 1u, 400 + t);
-            if (!ok) break;
-            ptx::tc_fence_after();
-            uint32_t s[4][32];
+        const bool wide = attn_wide(p.out, p.ld_out, p.D);
+        uint32_t done = 0;  // tiles before this item
+        Item m;
+        for (int k = 0; take(k, m, true); ++k) {
+            const int n = tiles_of(m);
+            const int first = m.block * 128 + warp * 32, row = first + lane;  // of the sequence
+            // keys that some row of the warp sees, all of them, this one
+            const int seen_by_one = min(m.len, p.causal ? first + 32 : m.len), seen_by_all = min(m.len, p.causal ? first + 1 : m.len),
+                      seen = min(m.len, p.causal ? row + 1 : m.len);
+            float top = 0.0f, total = 0.0f;  // the maximum that the sums refer to (of unscaled scores), the sum
+            bool ok = true;
+            for (int j = 0; j < n; ++j) {
+                const uint32_t r = done + j, s_tm = tm + (r & 1) * KEYS;
+                ok = warp_wait(wctx2, s_bar(r), half(r), 400);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                uint32_t s[2][32];
+                ptx::tmem_ld_32x32_x2_wait(s_tm, s_tm + 32, s[0], s[1]);
+                const int one = seen_by_one - j * KEYS;
+                if (seen_by_all - j * KEYS < KEYS) {
+                    const int limit = seen - j * KEYS;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32_issue(s_tm + c * 32, s[c]);
-            ptx::tmem_ld_wait_32(s[0]);
-            ptx::reg_fence_32(s[1]);
-            ptx::reg_fence_32(s[2]);
-            ptx::reg_fence_32(s[3]);
-            int limit = len - j * 128;  // columns below it are seen
-            if (p.causal) limit = min(limit, row + 1 - j * 128);
-            if (__any_sync(0xffffffffu, limit < 128)) {
+                    for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c * 32 + i >= limit) s[c][i] = 0xff800000u;
-            }
-            float m[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                m[c] = __uint_as_float(s[c][0]);
-#pragma unroll
-                for (int i = 1; i < 32; ++i) m[c] = fmaxf(m[c], __uint_as_float(s[c][i]));
-            }
-            const float now = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-            if (j == 0) {
-                top = now;
-            } else if (__any_sync(0xffffffffu, (now - top) * sl > 8.0f)) {
-                // only rows that grew that much: a row's bits do not depend on its neighbours
-                const bool grown = (now - top) * sl > 8.0f;
-                const float f = grown ? ptx::ex2_approx((top - now) * sl) : 1.0f;
-                total *= f;
-                if (grown) top = now;
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    ptx::tmem_ld_32x32_wait(o_tm + c * 32, o);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                    ptx::tmem_st_32x32(o_tm + c * 32, o);
+                        for (int i = 0; i < 32; ++i)
+                            if (c * 32 + i >= limit) s[c][i] = 0xff800000u;
                 }
-            }
-            const ptx::f2 base = ptx::make_f2(-top * sl, -top * sl);
-            ptx::f2 sum[2] = {ptx::make_f2(0.0f, 0.0f), ptx::make_f2(0.0f, 0.0f)};
+                float x[8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+                for (int e = 0; e < 8; ++e) x[e] = fmaxf(__uint_as_float(s[0][e]), __uint_as_float(s[1][e]));
+#pragma unroll
+                for (int i = 8; i < 32; i += 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = ptx::max3(x[e], __uint_as_float(s[0][i + e]), __uint_as_float(s[1][i + e]));
+                const float now = ptx::max3(ptx::max3(x[0], x[1], x[2]), ptx::max3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+                if (j == 0) {
+                    top = now;
+                } else {
+                    // only rows that grew that much: a row's bits do not depend on its neighbours
+                    const bool grown = (now - top) * sl > 8.0f;
+                    if (__any_sync(0xffffffffu, grown)) {
+                        const float f = grown ? ptx::ex2_approx((top - now) * sl) : 1.0f;
+                        total *= f;
+                        if (grown) top = now;
+                        ok = warp_wait(wctx2, o_bar(r - 1), half(r - 1), 410);
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            ptx::tmem_ld_32x16_wait(o_tm + c, o);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            ptx::tmem_st_32x16(o_tm + c, o);
+                        }
+                    }
+                }
+                const ptx::f2 base = ptx::make_f2(-top * sl, -top * sl);
+                ptx::f2 sum[2] = {ptx::make_f2(0.0f, 0.0f), ptx::make_f2(0.0f, 0.0f)};
                 uint32_t pk[32];
+                if (one <= 0) {  // no row of the warp sees these keys
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int c = 2 * h + (i >> 4), e = (2 * i) & 31;
-                    const ptx::f2 x = ptx::fma2(ptx::make_f2_bits(s[c][e], s[c][e + 1]), sl2, base);
-                    float a, b;
-                    ptx::split_f2(x, a, b);
-                    a = ptx::ex2_approx(a);
-                    b = ptx::ex2_approx(b);
-                    sum[i & 1] = ptx::add2(sum[i & 1], ptx::make_f2(a, b));
-                    pk[i] = ptx::pack_bf16x2(a, b);
+                    for (int i = 0; i < 32; ++i) pk[i] = 0;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const ptx::f2 y = ptx::fma2(ptx::make_f2_bits(s[i >> 4][2 * (i & 15)], s[i >> 4][2 * (i & 15) + 1]), sl2, base);
+                        float a, b;
+                        ptx::split_f2(y, a, b);
+                        a = ptx::ex2_approx(a);
+                        b = ptx::ex2_approx(b);
+                        sum[i & 1] = ptx::add2(sum[i & 1], ptx::make_f2(a, b));
+                        pk[i] = ptx::pack_bf16x2(a, b);
+                    }
                 }
-                ptx::tmem_st_32x32(s_tm + h * 32, pk);
+                ptx::tmem_st_32x32(s_tm, pk);
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(p_bar(r));
+                float a, b;
+                ptx::split_f2(ptx::add2(sum[0], sum[1]), a, b);
+                total += a + b;
             }
-            ptx::tmem_st_wait();
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(p_bar(t));
-            float a, b;
-            ptx::split_f2(ptx::add2(sum[0], sum[1]), a, b);
-            total += a + b;
-        }
-        if (ok && nt > 0) ok = warp_wait(wctx2, o_bar(t), 0, 420 + t);
-        if (ok && nt > 0) {
+            if (ok) ok = warp_wait(wctx2, o_bar(done + n - 1), half(done + n - 1), 420);
+            if (!ok) break;
+            done += n;
             ptx::tc_fence_after();
-            // through where this warp's queries were: all products that read them are done
-            const int first = row - lane;
-            attn_store_rows<D>(o_tm, 1.0f / total, smem + Cfg::OFF_Q + t * Cfg::TILE + (warp & 3) * 32 * D * 2,
-                               static_cast<__nv_bfloat16 *>(p.out) + (start + first) * p.ld_out + head * p.D, p.ld_out, len - first, p.D);
-            if (p.lse && row < len) p.lse[static_cast<long long>(head) * p.T + start + row] = top * p.scale + logf(total);
+            attn_store_row<D>(o_tm, 1.0f / total, static_cast<__nv_bfloat16 *>(p.out) + (m.start + row) * p.ld_out + m.head * p.D, row < m.len, p.D, wide);
+            if (p.lse && row < m.len) p.lse[static_cast<long long>(m.head) * p.T + m.start + row] = top * p.scale + logf(total);
+            ptx::tc_fence_before();
         }
         ptx::tc_fence_before();
     }
@@ -305,9 +343,9 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     __syncwarp();
     ptx::tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == MMA) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc<1>(tmem, 512);
+        ptx::tmem_dealloc<1>(tmem, Cfg::TMEM);
     }
 }
 

@@ -22,6 +22,11 @@ struct AttnSpan {
     int block;       // block of `rows` rows of it, or -1: nothing to do
 };
 
+__host__ __device__ __forceinline__ bool attn_wide(const void *p, long long ld, int D)
+{
+    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * 2) | static_cast<uintptr_t>(D * 2)) & 31u) == 0;
+}
+
 // The sequence and block that a slot stands for, found by one warp. Sequence i has the slots from cu[i] / rows + i on, at least as many as it
 // has blocks of `rows` rows, so that no sums over the sequences before it are needed; it uses the last ones first (with a
 // causal mask they have the most work). Bounds outside [0, T] or falling ones
@@ -74,41 +79,70 @@ __device__ __forceinline__ bool warp_wait(const WaitCtx &w, uint32_t bar, uint32
     return __all_sync(0xffffffffu, wait_barrier(w, bar, parity, where));
 }
 
-// A tile of 128 rows, in boxes of 64 columns, from row `row` on.
-template <int D>
+// A tile of ROWS rows, in boxes of 64 columns, from row `row` on.
+template <int D, int ROWS = 128>
 __device__ __forceinline__ void attn_load(uint32_t dst, const CUtensorMap *m, uint32_t bar, int head, int row)
 {
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) ptx::tma_load_3d(dst + c * kAttnBox, m, bar, c * 64, head, row);
+    for (int c = 0; c < D / 64; ++c) ptx::tma_load_3d(dst + c * ROWS * 128, m, bar, c * 64, head, row);
 }
 // Rows [from, to) of a tile in shared memory are set to zero by one warp.
-template <int D>
+template <int D, int ROWS = 128>
 __device__ __forceinline__ void attn_zero_rows(uint32_t tile, int from, int to)
 {
     const int lane = static_cast<int>(threadIdx.x & 31);
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
-        for (int i = lane; i < (to - from) * 8; i += 32) ptx::st_shared_v4(tile + c * kAttnBox + from * 128 + i * 16, 0, 0, 0, 0);
+        for (int i = lane; i < (to - from) * 8; i += 32) ptx::st_shared_v4(tile + c * ROWS * 128 + from * 128 + i * 16, 0, 0, 0, 0);
 }
 
-// D[128, 128] = A B^T over `steps` pieces of 16 columns, tiles A and B with the summed index contiguous (boxes of 64 columns).
+// D[128, N] = A B^T over `steps` pieces of 16 columns, tiles A (128 rows) and B (N rows) with the summed index contiguous (boxes of 64 columns).
+template <int N = 128>
 __device__ __forceinline__ void attn_mma_kk(uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t idesc, int steps)
 {
     const uint64_t ad = make_smem_desc(a, 16, 1024), bd = make_smem_desc(b, 16, 1024);
-    for (int k = 0; k < steps; ++k) {
-        const uint64_t off = static_cast<uint64_t>((k >> 2) * (kAttnBox >> 4) + (k & 3) * (32 >> 4));
-        ptx::umma_bf16<1>(d_tmem, ad + off, bd + off, idesc, k > 0 ? 1u : 0u);
-    }
+    for (int k = 0; k < steps; ++k)
+        ptx::umma_bf16<1>(d_tmem, ad + static_cast<uint64_t>((k >> 2) * (kAttnBox >> 4) + (k & 3) * (32 >> 4)),
+                          bd + static_cast<uint64_t>((k >> 2) * (N * 128 >> 4) + (k & 3) * (32 >> 4)), idesc, k > 0 ? 1u : 0u);
 }
 // D[128, N] (+)= A B, A [128, 16 steps] in tensor memory (piece k of 16 columns at a_tmem + 8 k, or, SPLIT, the second 64 columns of A
-// 64 columns of tensor memory after the first), B's rows the summed index (a tile of 128 rows).
-template <bool SPLIT = false>
+// 64 columns of tensor memory after the first), B's rows the summed index (a tile of ROWS rows).
+template <bool SPLIT = false, int ROWS = 128>
 __device__ __forceinline__ void attn_mma_tn(uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, bool accumulate)
 {
-    const uint64_t bd = make_smem_desc(b, kAttnBox, 1024);
+    const uint64_t bd = make_smem_desc(b, ROWS * 128, 1024);
     for (int k = 0; k < steps; ++k)
         ptx::umma_bf16_ts(d_tmem, a_tmem + (SPLIT ? (k >> 2) * 64 + (k & 3) * 8 : k * 8), bd + static_cast<uint64_t>(k * (2048 >> 4)), idesc,
                           accumulate || k > 0 ? 1u : 0u);
+}
+
+// A row of W columns per lane from the fp32 accumulator at `acc` to bf16 in global memory, 32 bytes at a time where rows allow it (`wide`: address, D and
+// ld are multiples of 32 bytes). `in`: the lane has a row; pieces from `cols` on are left out.
+template <int W>
+__device__ __forceinline__ void attn_store_row(uint32_t acc, float factor, __nv_bfloat16 *dst, bool in, int cols, bool wide)
+{
+#pragma unroll
+    for (int c = 0; c < W; c += 32) {
+        if (c >= cols) break;  // the same for all lanes
+        uint32_t o[32];
+        __syncwarp();
+        ptx::tmem_ld_32x32_wait(acc + c, o);
+        if (in) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 16) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = ptx::pack_bf16x2(__uint_as_float(o[k + 2 * i]) * factor, __uint_as_float(o[k + 2 * i + 1]) * factor);
+                if (wide) {
+                    if (c + k < cols) ptx::st_global_v8(dst + c + k, w);
+                } else {
+                    if (c + k < cols) *reinterpret_cast<uint4 *>(dst + c + k) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (c + k + 8 < cols) *reinterpret_cast<uint4 *>(dst + c + k + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                }
+            }
+        }
+    }
+    __syncwarp();
 }
 
 // 32 rows of W columns, a row per lane, from the fp32 accumulator at `acc` to bf16 rows in global memory, by way of shared memory (32 W 2 bytes

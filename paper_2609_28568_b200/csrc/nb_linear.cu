@@ -226,11 +226,12 @@ int get_batch_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t n
     return NB_OK;
 }
 
-// `heads` bf16 matrices [rows, cols] side by side, cols elements from one to the next and ld from row to row, in boxes of 128 rows x 64 columns
+// `heads` bf16 matrices [rows, cols] side by side, cols elements from one to the next and ld from row to row, in boxes of box_rows rows x 64 columns
 // of one of them with the 128-byte swizzle. What lies outside a matrix reads as zero.
-int get_heads_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t rows, uint64_t cols, uint64_t heads, uint64_t ld)
+int get_heads_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t rows, uint64_t cols, uint64_t heads, uint64_t ld,
+                   uint32_t box_rows = 128)
 {
-    TmapKey key{ptr, rows, cols, ld, 64, 128, 3, heads};
+    TmapKey key{ptr, rows, cols, ld, 64, box_rows, 3, heads};
     auto it = s.tmaps.find(key);
     if (it != s.tmaps.end()) {
         *out = it->second;
@@ -238,7 +239,7 @@ int get_heads_tmap(DeviceState &s, CUtensorMap *out, const void *ptr, uint64_t r
     }
     cuuint64_t dims[3] = {cols, heads, rows};
     cuuint64_t strides[2] = {cols * 2, ld * 2};
-    cuuint32_t box[3] = {64, 1, 128};
+    cuuint32_t box[3] = {64, 1, box_rows};
     cuuint32_t estr[3] = {1, 1, 1};
     alignas(64) CUtensorMap m;
     memset(&m, 0, sizeof(m));
@@ -2220,9 +2221,17 @@ AttnParams attn_params(const DeviceState &s, int64_t T, int64_t n, int64_t heads
     return p;
 }
 
-// Launches an attention kernel on `slots` blocks of a sequence for each of `heads` heads.
+// Slots for blocks of `rows` rows (attn_span).
+int64_t attn_slots(const AttnParams &p, int rows)
+{
+    if (p.cu) return p.T / rows + p.n;
+    const int64_t len = p.T / p.n;
+    return p.n * ((len + rows - 1) / rows);
+}
+
+// Launches an attention kernel on the sequences' blocks for each of `heads` heads.
 template <int MAPS, class P>
-int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtensorMap (&maps)[MAPS], P &p, int64_t slots, int64_t heads,
+int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtensorMap (&maps)[MAPS], P &p, const AttnParams &a, int64_t heads,
                      cudaStream_t stream)
 {
     int dev = 0;
@@ -2231,10 +2240,11 @@ int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtenso
         NB_CUDA(cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem)));
         attr_set[dev] = true;
     }
+    const int64_t slots = attn_slots(a, k.rows);
     if (slots * heads >= (1ll << 31)) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(slots * heads));
-    cfg.blockDim = dim3(kAttnThreads);
+    cfg.blockDim = dim3(static_cast<unsigned>(k.threads));
     cfg.dynamicSmemBytes = k.smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr;
@@ -2249,14 +2259,6 @@ int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtenso
     ++g_launches;
     return NB_OK;
 }
-// Slots for blocks of `rows` rows (attn_span).
-int64_t attn_slots(const AttnParams &p, int rows)
-{
-    if (p.cu) return p.T / rows + p.n;
-    const int64_t len = p.T / p.n;
-    return p.n * ((len + rows - 1) / rows);
-}
-
 }  // namespace
 
 // ================================================================================ C ABI
@@ -3064,12 +3066,13 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
     p.ld_out = ld_out;
     p.out = out;
     p.lse = static_cast<float *>(lse);
+    const AttnKernel kernel = attn_forward(p.D);
     CUtensorMap maps[3];
-    if ((rc = get_heads_tmap(*s, &maps[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &maps[1], k, T, D, kv_heads, ld_k)) != NB_OK ||
-        (rc = get_heads_tmap(*s, &maps[2], v, T, D, kv_heads, ld_v)) != NB_OK)
+    if ((rc = get_heads_tmap(*s, &maps[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &maps[1], k, T, D, kv_heads, ld_k, kernel.streamed)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &maps[2], v, T, D, kv_heads, ld_v, kernel.streamed)) != NB_OK)
         return rc;
     static bool attr_set[2][kMaxDevices] = {};
-    return launch_attention(attn_forward(p.D), attr_set[D > 64], maps, p, attn_slots(p, 256), heads, static_cast<cudaStream_t>(stream_));
+    return launch_attention(kernel, attr_set[D > 64], maps, p, p, heads, static_cast<cudaStream_t>(stream_));
 }
 
 int64_t nb_attention_workspace(int64_t T, int64_t heads)
@@ -3128,9 +3131,8 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
         return rc;
     static bool attr_set[4][kMaxDevices] = {};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    const int64_t slots = attn_slots(b.a, 128);
-    if ((rc = launch_attention(attn_backward_q(b.a.D), attr_set[D > 64], maps, b, slots, heads, stream)) != NB_OK) return rc;
-    return launch_attention(attn_backward_kv(b.a.D), attr_set[2 + (D > 64)], maps, b, slots, kv_heads, stream);
+    if ((rc = launch_attention(attn_backward_q(b.a.D), attr_set[D > 64], maps, b, b.a, heads, stream)) != NB_OK) return rc;
+    return launch_attention(attn_backward_kv(b.a.D), attr_set[2 + (D > 64)], maps, b, b.a, kv_heads, stream);
 }
 
 int nb_workspace_reserve(int64_t bytes)
@@ -3381,11 +3383,15 @@ int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us)
         return rc;
     static bool attr_set[3][kMaxDevices] = {};
     if (pass == 0) {
-        CUtensorMap maps[3] = {q, k, v};
-        return launch_attention(attn_forward(D), attr_set[0], maps, b.a, attn_slots(b.a, 256), 1, g_stream);
+        const AttnKernel kernel = attn_forward(D);
+        CUtensorMap maps[3] = {q};
+        if ((rc = get_heads_tmap(*s, &maps[1], tensors[1], T, D, 1, D, kernel.streamed)) != NB_OK ||
+            (rc = get_heads_tmap(*s, &maps[2], tensors[2], T, D, 1, D, kernel.streamed)) != NB_OK)
+            return rc;
+        return launch_attention(kernel, attr_set[0], maps, b.a, b.a, 1, g_stream);
     }
     CUtensorMap maps[4] = {q, dout, k, v};
-    return launch_attention(pass == 1 ? attn_backward_q(D) : attn_backward_kv(D), attr_set[pass], maps, b, attn_slots(b.a, 128), 1, g_stream);
+    return launch_attention(pass == 1 ? attn_backward_q(D) : attn_backward_kv(D), attr_set[pass], maps, b, b.a, 1, g_stream);
 }
 
 int nb_debug_muon_timeout(void *update, const void *grad, void *workspace, int64_t workspace_bytes, int64_t limit_us)
