@@ -12,15 +12,17 @@ static AttnKernel forward_kernel()
     return {reinterpret_cast<const void *>(&attn_forward_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM, 128, Cfg::KEYS};
 }
 AttnKernel attn_forward(int D) { return D <= 64 ? forward_kernel<AttnFwdCfg<64>>() : forward_kernel<AttnFwdCfg<128>>(); }
-AttnKernel attn_backward_q(int D)
+template <class Cfg>
+static AttnKernel backward_q_kernel()
 {
-    if (D <= 64) return {reinterpret_cast<const void *>(&attn_backward_q_kernel<64>), kAttnThreads, AttnBwdCfg<64>::SMEM_Q, 128, 128};
-    return {reinterpret_cast<const void *>(&attn_backward_q_kernel<128>), kAttnThreads, AttnBwdCfg<128>::SMEM_Q, 128, 128};
+    return {reinterpret_cast<const void *>(&attn_backward_q_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM_Q, 128, Cfg::ROWS};
 }
-AttnKernel attn_backward_kv(int D)
+template <class Cfg>
+static AttnKernel backward_kv_kernel()
 {
-    if (D <= 64) return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<64>), kAttnThreads, AttnBwdCfg<64>::SMEM_KV, 128, 128};
-    return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<128>), kAttnThreads, AttnBwdCfg<128>::SMEM_KV, 128, 128};
+    return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM_KV, 128, Cfg::ROWS};
 }
+AttnKernel attn_backward_q(int D) { return D <= 64 ? backward_q_kernel<AttnBwdCfg<64, 1>>() : backward_q_kernel<AttnBwdCfg<128, 2>>(); }
+AttnKernel attn_backward_kv(int D) { return D <= 64 ? backward_kv_kernel<AttnBwdCfg<64, 1>>() : backward_kv_kernel<AttnBwdCfg<128, 2>>(); }
 
 }  // namespace nb

@@ -4,8 +4,6 @@
 
 namespace nb {
 
-constexpr int kAttnTile = 128;
-constexpr int kAttnThreads = 384;  // backward: two warpgroups on scores, warp 8: loads, warp 9: products
 constexpr int kStatusBadSequences = 6;
 
 struct AttnParams {

@@ -145,35 +145,4 @@ __device__ __forceinline__ void attn_store_row(uint32_t acc, float factor, __nv_
     __syncwarp();
 }
 
-// 32 rows of W columns, a row per lane, from the fp32 accumulator at `acc` to bf16 rows in global memory, by way of shared memory (32 W 2 bytes
-// at `stg`, this warp's own), so that neighbouring threads store neighbouring pieces of 16 bytes. Rows and pieces beyond the bounds are left out.
-template <int W>
-__device__ __forceinline__ void attn_store_rows(uint32_t acc, float factor, uint32_t stg, void *dst, long long ld, int rows, int cols)
-{
-    constexpr int CH = W / 8;  // pieces of a row
-    const int lane = static_cast<int>(threadIdx.x & 31);
-#pragma unroll
-    for (int c = 0; c < W / 32; ++c) {
-        uint32_t o[32];
-        ptx::tmem_ld_32x32_wait(acc + c * 32, o);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = ptx::pack_bf16x2(__uint_as_float(o[k * 8 + 2 * i]) * factor, __uint_as_float(o[k * 8 + 2 * i + 1]) * factor);
-            ptx::st_shared_v4(stg + lane * W * 2 + (((c * 4 + k) ^ (lane & (CH < 8 ? CH - 1 : 7))) << 4), w[0], w[1], w[2], w[3]);
-        }
-    }
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        const int r = i * (32 / CH) + lane / CH, k = lane % CH;
-        uint32_t w[4];
-        ptx::ld_shared_v4(stg + r * W * 2 + ((k ^ (r & (CH < 8 ? CH - 1 : 7))) << 4), w[0], w[1], w[2], w[3]);
-        if (r < rows && k * 8 < cols)
-            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(dst) + r * ld + k * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
-
 }  // namespace nb

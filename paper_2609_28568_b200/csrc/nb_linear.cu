@@ -3125,14 +3125,19 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
     b.ld_dq = ld_dq;
     b.ld_dk = ld_dk;
     b.ld_dv = ld_dv;
-    CUtensorMap maps[4];
-    if ((rc = get_heads_tmap(*s, &maps[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &maps[1], dout, T, D, heads, ld_dout)) != NB_OK ||
-        (rc = get_heads_tmap(*s, &maps[2], k, T, D, kv_heads, ld_k)) != NB_OK || (rc = get_heads_tmap(*s, &maps[3], v, T, D, kv_heads, ld_v)) != NB_OK)
+    const AttnKernel of_q = attn_backward_q(b.a.D), of_kv = attn_backward_kv(b.a.D);
+    CUtensorMap mq[4], mkv[4];  // of q, dout, k, v: whole blocks of one pass are streamed by the other
+    if ((rc = get_heads_tmap(*s, &mq[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &mq[1], dout, T, D, heads, ld_dout)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &mq[2], k, T, D, kv_heads, ld_k, of_q.streamed)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &mq[3], v, T, D, kv_heads, ld_v, of_q.streamed)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &mkv[0], q, T, D, heads, ld_q, of_kv.streamed)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &mkv[1], dout, T, D, heads, ld_dout, of_kv.streamed)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &mkv[2], k, T, D, kv_heads, ld_k)) != NB_OK || (rc = get_heads_tmap(*s, &mkv[3], v, T, D, kv_heads, ld_v)) != NB_OK)
         return rc;
     static bool attr_set[4][kMaxDevices] = {};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if ((rc = launch_attention(attn_backward_q(b.a.D), attr_set[D > 64], maps, b, b.a, heads, stream)) != NB_OK) return rc;
-    return launch_attention(attn_backward_kv(b.a.D), attr_set[2 + (D > 64)], maps, b, b.a, kv_heads, stream);
+    if ((rc = launch_attention(of_q, attr_set[D > 64], mq, b, b.a, heads, stream)) != NB_OK) return rc;
+    return launch_attention(of_kv, attr_set[2 + (D > 64)], mkv, b, b.a, kv_heads, stream);
 }
 
 int nb_workspace_reserve(int64_t bytes)
@@ -3377,21 +3382,21 @@ int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us)
     b.dk = tensors[7];
     b.dv = tensors[8];
     b.delta = static_cast<float *>(tensors[9]);
+    const AttnKernel kernel = pass == 0 ? attn_forward(D) : pass == 1 ? attn_backward_q(D) : attn_backward_kv(D);
+    const uint32_t own = 128, streamed = static_cast<uint32_t>(kernel.streamed);
     CUtensorMap q, k, v, dout;
-    if ((rc = get_heads_tmap(*s, &q, tensors[0], T, D, 1, D)) != NB_OK || (rc = get_heads_tmap(*s, &k, tensors[1], T, D, 1, D)) != NB_OK ||
-        (rc = get_heads_tmap(*s, &v, tensors[2], T, D, 1, D)) != NB_OK || (rc = get_heads_tmap(*s, &dout, tensors[5], T, D, 1, D)) != NB_OK)
+    if ((rc = get_heads_tmap(*s, &q, tensors[0], T, D, 1, D, pass == 2 ? streamed : own)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &k, tensors[1], T, D, 1, D, pass == 2 ? own : streamed)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &v, tensors[2], T, D, 1, D, pass == 2 ? own : streamed)) != NB_OK ||
+        (rc = get_heads_tmap(*s, &dout, tensors[5], T, D, 1, D, pass == 2 ? streamed : own)) != NB_OK)
         return rc;
     static bool attr_set[3][kMaxDevices] = {};
     if (pass == 0) {
-        const AttnKernel kernel = attn_forward(D);
-        CUtensorMap maps[3] = {q};
-        if ((rc = get_heads_tmap(*s, &maps[1], tensors[1], T, D, 1, D, kernel.streamed)) != NB_OK ||
-            (rc = get_heads_tmap(*s, &maps[2], tensors[2], T, D, 1, D, kernel.streamed)) != NB_OK)
-            return rc;
+        CUtensorMap maps[3] = {q, k, v};
         return launch_attention(kernel, attr_set[0], maps, b.a, b.a, 1, g_stream);
     }
     CUtensorMap maps[4] = {q, dout, k, v};
-    return launch_attention(pass == 1 ? attn_backward_q(D) : attn_backward_kv(D), attr_set[pass], maps, b, b.a, 1, g_stream);
+    return launch_attention(kernel, attr_set[pass], maps, b, b.a, 1, g_stream);
 }
 
 int nb_debug_muon_timeout(void *update, const void *grad, void *workspace, int64_t workspace_bytes, int64_t limit_us)
