@@ -62,33 +62,17 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     auto p_bar = [&](uint32_t r) { return named(4 + (r & 1)); };  // probabilities are there
     auto o_bar = [&](uint32_t r) { return named(6 + (r & 1)); };  // their product with V is done
     auto half = [](uint32_t r) { return (r >> 1) & 1u; };         // parity of the r-th tile in them
-    auto item_bar = [&](int i) { return named(8 + i); };          // an item has been put down
-    auto ifree_bar = [&](int i) { return named(10 + i); };        // and been read by all
-    const uint32_t part_bar = named(12), next_bar = named(13);    // values of a sequence's last tile, the next item have come
-    const uint32_t answer = bar0 + 400, item0 = bar0 + 416;   // 16 bytes; two of 16
+    const uint32_t part_bar = named(8);  // values of a sequence's last tile have landed
+    const AttnItems items{named(9), bar0 + 400};
+    static_assert(8 * (2 * STAGES + 9 + AttnItems::kBars) <= 400, "barriers");
     const uint32_t tmem_slot = bar0 + 480, abort_addr = bar0 + 484;
-    static_assert(8 * (2 * STAGES + 14) <= 400, "barriers");
 
     const WaitCtx wctx{abort_addr, p.status, p.timeout_ns};
     // The waits for a whole round of work have twice the limit, so that the wait closest to the cause of a stall is reported.
     const WaitCtx wctx2{abort_addr, p.status, 2 * p.timeout_ns};
-    struct Item {
-        int start, len, block, head;
-    };
-    auto tiles_of = [&](const Item &m) {  // tiles of keys that an item's queries see
+    auto tiles_of = [&](const AttnItem &m) {  // tiles of keys that an item's queries see
         const int tiles = (m.len + KEYS - 1) / KEYS;
         return p.causal ? min(tiles, (m.block + 1) * (128 / KEYS)) : tiles;
-    };
-    // the k-th item, by one thread of a warp for all; no more: block < 0
-    auto take = [&](int k, Item &m, bool all) {
-        const uint32_t par = static_cast<uint32_t>(k >> 1) & 1u, at = item0 + (k & 1) * 16;
-        if (!(all ? warp_wait(wctx2, item_bar(k & 1), par, 500) : wait_barrier(wctx2, item_bar(k & 1), par, 500))) return false;
-        uint32_t v[4];
-        ptx::ld_shared_v4(at, v[0], v[1], v[2], v[3]);
-        m = {static_cast<int>(v[0]), static_cast<int>(v[1]), static_cast<int>(v[2]), static_cast<int>(v[3])};
-        if (all) __syncwarp();
-        if (!all || lane == 0) ptx::mbar_arrive(ifree_bar(k & 1));
-        return m.block >= 0;
     };
 
     if (warp == LOAD) {
@@ -96,7 +80,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             ptx::mbar_init(full_bar(lane), 1);
             ptx::mbar_init(empty_bar(lane), 1);
         }
-        if (lane < 14) ptx::mbar_init(named(lane), lane == 4 || lane == 5 ? 4 : lane == 10 || lane == 11 ? 5 : 1);
+        if (lane < 9) ptx::mbar_init(named(lane), lane == 4 || lane == 5 ? 4 : 1);
+        items.init(lane, 5);
         if (lane == 31) ptx::st_shared_u32_volatile(abort_addr, 0);
         ptx::fence_barrier_init();
         if (lane == 30) {
@@ -127,29 +112,15 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             int stage = 0;
             uint32_t phase = 0, parts = 0, asked = 0, used = 0;
             for (int k = 0, at = static_cast<int>(blockIdx.x); ok;) {
+                AttnItem m{0, 0, -1, 0};
                 if (at >= 0) {
-                    if (ptx::elect_one()) {  // the one after
-                        ptx::mbar_expect_tx(next_bar, 16);
-                        ptx::launch_cancel(answer, next_bar);
-                    }
-                    __syncwarp();
-                }
-                Item m{0, 0, -1, 0};
-                if (at >= 0) {
+                    items.ask();
                     const AttnSpan s = attn_span(p, at / p.heads, 128, true);
                     m = {s.start, s.len, s.block, at % p.heads};
                 }
                 if (at < 0 || m.block >= 0) {  // slots without a block are passed over
-                    ok = warp_wait(wctx2, ifree_bar(k & 1), (static_cast<uint32_t>(k >> 1) & 1u) ^ 1u, 510);
-                    if (!ok) break;
-                    if (lane == 0) {
-                        ptx::st_shared_v4(item0 + (k & 1) * 16, static_cast<uint32_t>(m.start), static_cast<uint32_t>(m.len),
-                                          static_cast<uint32_t>(m.block), static_cast<uint32_t>(m.head));
-                        ptx::mbar_arrive(item_bar(k & 1));
-                    }
-                    __syncwarp();
-                    ++k;
-                    if (at < 0) break;
+                    ok = items.put(wctx2, k++, m);
+                    if (!ok || at < 0) break;
                     const int n = tiles_of(m), kv_head = m.head / p.group;
                     for (int i = 0; i < 2 * n && ok; ++i) {
                         const int j = i >> 1;
@@ -187,11 +158,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     }
                     if (!ok) break;
                 }
-                ok = warp_wait(wctx2, next_bar, asked++ & 1u, 520);
-                if (!ok) break;
-                at = ptx::launch_cancelled(answer);
-                ptx::fence_proxy_async_smem();
-                __syncwarp();
+                ok = items.told(wctx2, asked, at);
             }
         } else if (warp == MMA) {
             // ------------------------------------------------------------ products
@@ -203,8 +170,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 auto stage = [&](uint32_t i) { return static_cast<int>((2 * done + i) % STAGES); };
                 auto tile = [&](uint32_t i) { return smem + Cfg::OFF_KV + stage(i) * Cfg::TILE; };
                 auto ready = [&](uint32_t i) { return wait_barrier(wctx, full_bar(stage(i)), ((2 * done + i) / STAGES) & 1u, 300 + stage(i)); };
-                Item m;
-                for (int k = 0; take(k, m, false); ++k) {
+                AttnItem m;
+                for (int k = 0; items.take<false>(wctx2, k, m); ++k) {
                     const int n = tiles_of(m);
                     auto scores = [&](int j) {
                         if (!ready(2 * j)) return false;
@@ -242,8 +209,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const ptx::f2 sl2 = ptx::make_f2(sl, sl);
         const bool wide = attn_wide(p.out, p.ld_out, p.D);
         uint32_t done = 0;  // tiles before this item
-        Item m;
-        for (int k = 0; take(k, m, true); ++k) {
+        AttnItem m;
+        for (int k = 0; items.take<true>(wctx2, k, m); ++k) {
             const int n = tiles_of(m);
             const int first = m.block * 128 + warp * 32, row = first + lane;  // of the sequence
             // keys that some row of the warp sees, all of them, this one

@@ -79,6 +79,66 @@ __device__ __forceinline__ bool warp_wait(const WaitCtx &w, uint32_t bar, uint32
     return __all_sync(0xffffffffu, wait_barrier(w, bar, parity, where));
 }
 
+// ---------------------------------------------------------------- the items of a block
+// A block begins with the item of its own place in the grid. When its loading warp turns to an item it asks for the next one, which
+// the hardware takes off the blocks that have not started; items pass from the loading warp to the others by two slots in shared memory.
+struct AttnItem {
+    int start, len, block, head;  // block < 0: no more
+};
+struct AttnItems {
+    static constexpr int kBars = 5;  // barriers: an item is there (two), it has been read by all (two), the next one has come
+    uint32_t bars, memory;           // kBars of 8 bytes; 48 bytes, 16-byte aligned
+    __device__ __forceinline__ uint32_t there(int k) const { return bars + 8u * (k & 1); }
+    __device__ __forceinline__ uint32_t read(int k) const { return bars + 16u + 8u * (k & 1); }
+    // by lane `lane` of the warp that initialises barriers
+    __device__ __forceinline__ void init(int lane, int readers) const
+    {
+        if (lane < kBars) ptx::mbar_init(bars + 8u * lane, lane == 2 || lane == 3 ? readers : 1);
+    }
+    // the loading warp asks for the item after the one that it has, and is told: its place in the grid, or -1
+    __device__ __forceinline__ void ask() const
+    {
+        if (ptx::elect_one()) {
+            ptx::mbar_expect_tx(bars + 32u, 16);
+            ptx::launch_cancel(memory, bars + 32u);
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ bool told(const WaitCtx &w, uint32_t &asked, int &at) const
+    {
+        if (!warp_wait(w, bars + 32u, asked++ & 1u, 520)) return false;
+        at = ptx::launch_cancelled(memory);
+        ptx::fence_proxy_async_smem();  // the next answer is written where this one was read
+        __syncwarp();
+        return true;
+    }
+    // the loading warp puts the k-th item down
+    __device__ __forceinline__ bool put(const WaitCtx &w, int k, const AttnItem &m) const
+    {
+        if (!warp_wait(w, read(k), (static_cast<uint32_t>(k >> 1) & 1u) ^ 1u, 510)) return false;
+        if ((threadIdx.x & 31) == 0) {
+            ptx::st_shared_v4(memory + 16u + 16u * (k & 1), static_cast<uint32_t>(m.start), static_cast<uint32_t>(m.len), static_cast<uint32_t>(m.block),
+                              static_cast<uint32_t>(m.head));
+            ptx::mbar_arrive(there(k));
+        }
+        __syncwarp();
+        return true;
+    }
+    // the k-th item, for one thread that stands for its warp, or for all of a warp; false: there is none, or a wait ran out
+    template <bool WARP>
+    __device__ __forceinline__ bool take(const WaitCtx &w, int k, AttnItem &m) const
+    {
+        const uint32_t par = static_cast<uint32_t>(k >> 1) & 1u;
+        if (!(WARP ? warp_wait(w, there(k), par, 500) : wait_barrier(w, there(k), par, 500))) return false;
+        uint32_t v[4];
+        ptx::ld_shared_v4(memory + 16u + 16u * (k & 1), v[0], v[1], v[2], v[3]);
+        m = {static_cast<int>(v[0]), static_cast<int>(v[1]), static_cast<int>(v[2]), static_cast<int>(v[3])};
+        if (WARP) __syncwarp();
+        if (!WARP || (threadIdx.x & 31) == 0) ptx::mbar_arrive(read(k));
+        return m.block >= 0;
+    }
+};
+
 // A tile of ROWS rows, in boxes of 64 columns, from row `row` on.
 template <int D, int ROWS = 128>
 __device__ __forceinline__ void attn_load(uint32_t dst, const CUtensorMap *m, uint32_t bar, int head, int row)
