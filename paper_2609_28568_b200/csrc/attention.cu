@@ -15,12 +15,12 @@ AttnKernel attn_forward(int D) { return D <= 64 ? forward_kernel<AttnFwdCfg<64>>
 template <class Cfg>
 static AttnKernel backward_q_kernel()
 {
-    return {reinterpret_cast<const void *>(&attn_backward_q_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM_Q, 128, Cfg::ROWS};
+    return {reinterpret_cast<const void *>(&attn_backward_q_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM, 128, Cfg::ROWS};
 }
 template <class Cfg>
 static AttnKernel backward_kv_kernel()
 {
-    return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM_KV, 128, Cfg::ROWS};
+    return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM, 128, Cfg::ROWS};
 }
 AttnKernel attn_backward_q(int D) { return D <= 64 ? backward_q_kernel<AttnBwdCfg<64, 1>>() : backward_q_kernel<AttnBwdCfg<128, 2>>(); }
 AttnKernel attn_backward_kv(int D) { return D <= 64 ? backward_kv_kernel<AttnBwdCfg<64, 1>>() : backward_kv_kernel<AttnBwdCfg<128, 2>>(); }

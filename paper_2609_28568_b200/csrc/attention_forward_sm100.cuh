@@ -11,7 +11,7 @@
 //
 // Items differ in work by the length of their sequence and their place in it, and are short beside what a block costs to start (first loads, first
 // products: 2 to 3 us). So a block that is done with its item takes another off the grid (the hardware hands out blocks that have not
-// started), asks for it an item ahead, and its loads and first scores come while the last output is still being stored.
+// started), asks for it when its own loads are on their way, and its loads and first scores come while the last output is still being stored.
 //
 // The output accumulator in tensor memory is rescaled only when a row's maximum has grown by more than 2^8 since the last
 // rescaling: until then probabilities up to 2^8 are summed against the old maximum, which changes no bit of their relative precision.
@@ -114,7 +114,6 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             for (int k = 0, at = static_cast<int>(blockIdx.x); ok;) {
                 AttnItem m{0, 0, -1, 0};
                 if (at >= 0) {
-                    items.ask();
                     const AttnSpan s = attn_span(p, at / p.heads, 128, true);
                     m = {s.start, s.len, s.block, at % p.heads};
                 }
@@ -158,7 +157,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     }
                     if (!ok) break;
                 }
-                ok = items.told(wctx2, asked, at);
+                ok = items.next(wctx2, asked, at);
             }
         } else if (warp == MMA) {
             // ------------------------------------------------------------ products

@@ -80,8 +80,8 @@ __device__ __forceinline__ bool warp_wait(const WaitCtx &w, uint32_t bar, uint32
 }
 
 // ---------------------------------------------------------------- the items of a block
-// A block begins with the item of its own place in the grid. When its loading warp turns to an item it asks for the next one, which
-// the hardware takes off the blocks that have not started; items pass from the loading warp to the others by two slots in shared memory.
+// A block begins with the item of its own place in the grid. When its loading warp has the tiles of an item on their way it asks for the next
+// one, which the hardware takes off the blocks that have not started; items pass from the loading warp to the others by two slots in shared memory.
 struct AttnItem {
     int start, len, block, head;  // block < 0: no more
 };
@@ -95,17 +95,14 @@ struct AttnItems {
     {
         if (lane < kBars) ptx::mbar_init(bars + 8u * lane, lane == 2 || lane == 3 ? readers : 1);
     }
-    // the loading warp asks for the item after the one that it has, and is told: its place in the grid, or -1
-    __device__ __forceinline__ void ask() const
+    // the loading warp asks for the next item: its place in the grid, or -1. (Asked for earlier, an item may wait for a block that has much to do.)
+    __device__ __forceinline__ bool next(const WaitCtx &w, uint32_t &asked, int &at) const
     {
         if (ptx::elect_one()) {
             ptx::mbar_expect_tx(bars + 32u, 16);
             ptx::launch_cancel(memory, bars + 32u);
         }
         __syncwarp();
-    }
-    __device__ __forceinline__ bool told(const WaitCtx &w, uint32_t &asked, int &at) const
-    {
         if (!warp_wait(w, bars + 32u, asked++ & 1u, 520)) return false;
         at = ptx::launch_cancelled(memory);
         ptx::fence_proxy_async_smem();  // the next answer is written where this one was read
