@@ -86,9 +86,13 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         ptx::tmem_alloc<1>(tmem_slot, Cfg::TMEM);
         ptx::tmem_relinquish<1>();
     }
-    ptx::tc_fence_before();
-    __syncthreads();
-    ptx::tc_fence_after();
+    if (warp == LOAD) {  // has no use for tensor memory: its first loads need not wait for it
+        ptx::named_bar_arrive(2, Cfg::THREADS);
+    } else {
+        ptx::tc_fence_before();
+        ptx::named_bar_sync(2, Cfg::THREADS);
+        ptx::tc_fence_after();
+    }
     const uint32_t tmem = ptx::ld_shared_u32_volatile(tmem_slot);
     ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
@@ -107,10 +111,12 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             bool ok = true;
             int stage = 0;
             uint32_t phase = 0, parts = 0, asked = 0;
+            AttnOrder order;
+            order.load(p);
             for (int k = 0, at = static_cast<int>(blockIdx.x); ok;) {
                 AttnItem m{0, 0, -1, 0};
                 if (at >= 0) {
-                    const AttnSpan s = attn_span(p, at / p.heads, 128, true);
+                    const AttnSpan s = order.item(p, at / p.heads, false);
                     m = {s.start, s.len, s.block, at % p.heads};
                 }
                 if (at < 0 || m.block >= 0) {  // slots without a block are passed over
@@ -383,9 +389,13 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         ptx::tmem_alloc<1>(tmem_slot, Cfg::TMEM);
         ptx::tmem_relinquish<1>();
     }
-    ptx::tc_fence_before();
-    __syncthreads();
-    ptx::tc_fence_after();
+    if (warp == LOAD) {  // has no use for tensor memory: its first loads need not wait for it
+        ptx::named_bar_arrive(2, Cfg::THREADS);
+    } else {
+        ptx::tc_fence_before();
+        ptx::named_bar_sync(2, Cfg::THREADS);
+        ptx::tc_fence_after();
+    }
     const uint32_t tmem = ptx::ld_shared_u32_volatile(tmem_slot);
     ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
@@ -404,10 +414,12 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             bool ok = true;
             int stage = 0;
             uint32_t phase = 0, parts = 0, asked = 0;
+            AttnOrder order;
+            order.load(p);
             for (int k = 0, at = static_cast<int>(blockIdx.x); ok;) {
                 AttnItem m{0, 0, -1, 0};
                 if (at >= 0) {
-                    const AttnSpan s = attn_span(p, at / kv_heads, 128, false);
+                    const AttnSpan s = order.item(p, at / kv_heads, true);
                     m = {s.start, s.len, s.block, at % kv_heads};
                 }
                 if (at < 0 || m.block >= 0) {  // slots without a block are passed over

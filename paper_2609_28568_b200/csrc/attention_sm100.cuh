@@ -27,44 +27,102 @@ __host__ __device__ __forceinline__ bool attn_wide(const void *p, long long ld, 
     return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * 2) | static_cast<uintptr_t>(D * 2)) & 31u) == 0;
 }
 
-// The sequence and block that a slot stands for, found by one warp. Sequence i has the slots from cu[i] / rows + i on, at least as many as it
-// has blocks of `rows` rows, so that no sums over the sequences before it are needed; it uses the last ones first (with a
-// causal mask they have the most work). Bounds outside [0, T] or falling ones
-// are cut to an empty or shorter sequence (and reported by attn_report_bounds).
-__device__ __forceinline__ AttnSpan attn_span(const AttnParams &p, int slot, int rows, bool descending)
-{
-    const int lane = static_cast<int>(threadIdx.x & 31);
-    AttnSpan s;
-    int local;
-    if (p.cu == nullptr) {
-        const int len = p.T / p.n, per = (len + rows - 1) / rows;
-        const int i = slot / per;
-        s.start = i * len;
-        s.len = i < p.n ? len : 0;
-        local = slot - i * per;
-    } else {
-        int lo = 0, hi = p.n;  // the last i with cu[i] / rows + i <= slot lies in [lo, hi)
-        int at = 0;
-        while (hi - lo > 1) {
-            const int step = (hi - lo + 31) / 32;
-            const int i = lo + lane * step;
-            const int c = i < hi ? p.cu[i] : 0;
-            const unsigned before = __ballot_sync(0xffffffffu, i < hi && max(c, 0) / rows + i <= slot);
-            const int last = before ? 31 - __clz(before) : 0;
-            lo += last * step;
-            hi = min(hi, lo + step);
-        }
-        const int a = p.cu[lo], b = p.cu[lo + 1];
-        const int start = min(max(a, 0), p.T), end = min(max(b, start), p.T);
-        at = max(a, 0) / rows + lo;
-        s.start = start;
-        s.len = end - start;
-        local = slot - at;
+// The order of the items, of blocks of 128 rows, told by one warp. With a causal mask a block has work in proportion to its place in its sequence (dQ and the
+// forward pass: more towards the end; dK, dV: more towards the start), so items come in falling order of that over all sequences: the l-th
+// level is block l (or l-th from the end) of every sequence that has so many, highest level first. A lane holds up to kOwn sequences, and the level
+// of the k-th item is found by sums over the warp. (In order of the sequences 16 of 1024 rows left a fifth of the SMs' time unused at the end.) For more
+// sequences than that, sequence i has the slots from cu[i] / 128 + i on, at least as many as it has blocks, so that no sums over the sequences before
+// it are needed. Bounds outside [0, T] or falling ones are cut to an empty or shorter sequence (and reported by attn_report_bounds).
+class AttnOrder {
+    static constexpr int kOwn = 4;
+    int start_[kOwn], len_[kOwn];
+    int top_;  // levels
+
+    __device__ __forceinline__ static int blocks(int len) { return (len + 127) / 128; }
+    __device__ __forceinline__ int above(int level) const  // items of this level and higher ones
+    {
+        int n = 0;
+#pragma unroll
+        for (int c = 0; c < kOwn; ++c) n += max(blocks(len_[c]) - level, 0);
+        return __reduce_add_sync(0xffffffffu, n);
     }
-    const int blocks = (s.len + rows - 1) / rows;
-    s.block = local < 0 || local >= blocks ? -1 : descending ? blocks - 1 - local : local;
-    return s;
-}
+
+public:
+    __device__ __forceinline__ void load(const AttnParams &p)
+    {
+        const int lane = static_cast<int>(threadIdx.x & 31);
+        int most = 0;
+#pragma unroll
+        for (int c = 0; c < kOwn; ++c) {
+            const int i = c * 32 + lane;
+            start_[c] = len_[c] = 0;
+            if (i < p.n && p.n <= 32 * kOwn) {
+                if (p.cu) {
+                    start_[c] = min(max(p.cu[i], 0), p.T);
+                    len_[c] = min(max(p.cu[i + 1], start_[c]), p.T) - start_[c];
+                } else {
+                    len_[c] = p.T / p.n;
+                    start_[c] = i * len_[c];
+                }
+            }
+            most = max(most, blocks(len_[c]));
+        }
+        top_ = __reduce_max_sync(0xffffffffu, most);
+    }
+    // the k-th item of a head; from_end: blocks at the start of a sequence have the most work
+    __device__ __forceinline__ AttnSpan item(const AttnParams &p, int k, bool from_end) const
+    {
+        const int lane = static_cast<int>(threadIdx.x & 31);
+        AttnSpan s{0, 0, -1};
+        if (p.n > 32 * kOwn) {
+            int first;
+            if (p.cu == nullptr) {
+                s.len = p.T / p.n;
+                first = blocks(s.len);
+                s.start = k / first * s.len;
+                if (k / first >= p.n) s.len = 0;
+                first = k / first * first;
+            } else {
+                int lo = 0, hi = p.n;  // the last i with cu[i] / 128 + i <= k lies in [lo, hi)
+                while (hi - lo > 1) {
+                    const int step = (hi - lo + 31) / 32;
+                    const int i = lo + lane * step;
+                    const unsigned before = __ballot_sync(0xffffffffu, i < hi && max(p.cu[i], 0) / 128 + i <= k);
+                    const int last = before ? 31 - __clz(before) : 0;
+                    lo += last * step;
+                    hi = min(hi, lo + step);
+                }
+                first = max(p.cu[lo], 0) / 128 + lo;
+                s.start = min(max(p.cu[lo], 0), p.T);
+                s.len = min(max(p.cu[lo + 1], s.start), p.T) - s.start;
+            }
+            const int local = k - first, n = blocks(s.len);
+            if (local >= 0 && local < n) s.block = from_end ? local : n - 1 - local;
+            return s;
+        }
+        if (above(0) <= k) return s;
+        int lo = 0, hi = top_;  // the level is the last with more than k items from it on up
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (above(mid) > k) lo = mid;
+            else hi = mid;
+        }
+        int rank = k - above(lo + 1);  // among the sequences that have the level
+#pragma unroll
+        for (int c = 0; c < kOwn; ++c) {
+            const bool has = blocks(len_[c]) > lo;
+            const unsigned all = __ballot_sync(0xffffffffu, has);
+            const unsigned here = __ballot_sync(0xffffffffu, has && __popc(all & ((1u << lane) - 1u)) == rank);
+            if (here) {
+                s.start = __shfl_sync(0xffffffffu, start_[c], __ffs(here) - 1);
+                s.len = __shfl_sync(0xffffffffu, len_[c], __ffs(here) - 1);
+                s.block = from_end ? blocks(s.len) - 1 - lo : lo;
+            }
+            rank -= __popc(all);  // below zero from there on: no sequence of the lanes to come
+        }
+        return s;
+    }
+};
 
 // Reports bounds that fall or leave [0, T]; by one warp of a launch.
 __device__ __forceinline__ void attn_report_bounds(const int *cu, int n, int T, int *status)

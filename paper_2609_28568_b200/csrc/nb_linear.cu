@@ -2221,7 +2221,7 @@ AttnParams attn_params(const DeviceState &s, int64_t T, int64_t n, int64_t heads
     return p;
 }
 
-// Slots for blocks of `rows` rows (attn_span).
+// Slots for blocks of `rows` rows, no fewer than there are (AttnOrder).
 int64_t attn_slots(const AttnParams &p, int rows)
 {
     if (p.cu) return p.T / rows + p.n;
