@@ -269,7 +269,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         }
                     }
                 }
-                const ptx::f2 base = ptx::make_f2(-top * sl, -top * sl);
+                const float shift = top == -INFINITY ? 0.0f : -top * sl;  // nothing but infinities so far: no probability yet
+                const ptx::f2 base = ptx::make_f2(shift, shift);
                 ptx::f2 sum[2] = {ptx::make_f2(0.0f, 0.0f), ptx::make_f2(0.0f, 0.0f)};
                 uint32_t pk[32];
                 if (one <= 0) {  // no row of the warp sees these keys

@@ -189,6 +189,19 @@ def test_later_rows_are_not_seen():
     assert not torch.equal(out[250:], out2[250:])
 
 
+def test_infinite_scores():
+    """Keys that no query can see for their infinite distance: they have no part in the result, wherever they stand."""
+    c = Case([200], 1, 1, 64, seed=18)
+    c.q[:, 0, 0] = 1.0
+    want, lse = nb.attention_forward(c.q[150:], c.k[150:], c.v[150:], causal=False)
+    c.k[:150, 0] = 0.0
+    c.k[:150, 0, 0] = -math.inf
+    got, lse2 = nb.attention_forward(c.q, c.k, c.v, causal=False)
+    # the sums are made up of the same numbers, in other pieces: probabilities, lse and the result each rounded anew
+    e, tol = (got[150:].double() - want.double()).abs(), 4 * ref.U16 * (want.double().abs() + c.v[150:].double().abs().mean(0))
+    assert (e <= tol).all() and (lse2[:, 150:] - lse).abs().max() < 1e-5
+
+
 def test_offsets_past_32_bits():
     """Rows so far apart that the last lies 5 GB behind the first."""
     ld, T = 1 << 23, 300
