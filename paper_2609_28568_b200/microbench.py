@@ -13,7 +13,10 @@ ce_bwd_inplace (over the logits),
 lora_fwd / lora_bwd (rank-16 adapter beside a frozen weight; TFLOP/s counts base + adapter flops),
 norm / norm_bwd (layer norm of [BT, C] bf16 with the residual add in front of it, and its backward with the stream's gradient;
 GB/s, OC is not used), muon / muon_apply (update of BT matrices [OC, C] by orthogonalised momentum, TFLOP/s of its products with half of
-the symmetric ones; and its application to the master weights, GB/s).
+the symmetric ones; and its application to the master weights, GB/s),
+rotary (rotary positions of BT rows of C columns as C / 128 heads of queries and half as many of keys, GB/s; OC is the length of a sequence), attn / attn_bwd
+(causal attention over BT rows in sequences of OC, C / 64 heads of 64 columns of one fused buffer, and its backward pass; TFLOP/s of the pairs that are
+seen, two products forward and five backward).
 Prints microseconds per call and TFLOP/s from CUDA events around REPS back-to-back calls.
 
 With the word `energy` after REPS (GEMM kinds only) the call is instead replayed from a CUDA graph for
@@ -167,6 +170,40 @@ def beside_linears(kind: str, BT: int, C: int, OC: int, reps: int) -> int:
     return 0
 
 
+def between_linears(kind: str, BT: int, C: int, OC: int, reps: int) -> int:
+    """The operators between the qkv linear and attn_proj: see the module docstring."""
+    dev, bf, n = "cuda", torch.bfloat16, max(BT // OC, 1)
+    D = 128 if kind == "rotary" else 64
+    heads = C // D
+    if BT % n or heads < 2 or C % D:
+        print(__doc__)
+        return 2
+    kv = heads // 2 if kind == "rotary" else heads
+    if heads % kv:
+        print(__doc__)
+        return 2
+    qkv = synth.normal(1, (BT, (heads + 2 * kv) * D), 1.0, dev).view(BT, -1, D)
+    q, k, v = qkv.split([heads, kv, kv], 1)
+    if kind == "rotary":
+        freq = nb.rotary_frequencies(D, device=dev)
+        us = timed(lambda: nb.rotary(q, k, freq, n=n, in_place=True), reps)
+        print(f"rotary BT={BT} {heads} and {kv} heads of {D}: {us:.1f} us/call  {4 * BT * (heads + kv) * D / us / 1e3:.1f} GB/s")
+        return 0
+    out, lse = nb.attention_forward(q, k, v, n=n)
+    flops = 2 * n * (BT // n) * (BT // n + 1) * D * heads  # of the two products of the forward pass
+    if kind == "attn":
+        us = timed(lambda: nb.nb_attention_forward(out, lse, q, k, v, None, BT, n, heads, kv, D, C, *(qkv.stride(0),) * 3, D ** -0.5, 1), reps)
+    else:
+        flops = flops * 5 // 2
+        dout, dqkv = synth.normal(2, tuple(out.shape), 1e-3, dev), torch.empty_like(qkv)
+        grads = dqkv.split([heads, kv, kv], 1)
+        ws = torch.empty(nb.nb_attention_workspace(BT, heads), dtype=torch.uint8, device=dev)
+        us = timed(lambda: nb.nb_attention_backward(*grads, dout, out, lse, q, k, v, None, BT, n, heads, kv, D, *(qkv.stride(0),) * 3, C, C,
+                                                    *(qkv.stride(0),) * 3, D ** -0.5, 1, ws, ws.numel()), reps)
+    print(f"{kind} BT={BT} in {n} sequences, {heads} heads of {D}: {us:.1f} us/call  {flops / us / 1e6:.1f} TFLOP/s")
+    return 0
+
+
 def main(argv) -> int:
     if len(argv) < 5:
         print(__doc__)
@@ -179,6 +216,8 @@ def main(argv) -> int:
         return replayed(kind, BT, C, OC, reps)
     if kind in ("norm", "norm_bwd", "muon", "muon_apply"):
         return beside_linears(kind, BT, C, OC, reps)
+    if kind in ("rotary", "attn", "attn_bwd"):
+        return between_linears(kind, BT, C, OC, reps)
     dev = "cuda"
     bf, f32 = torch.bfloat16, torch.float32
     inp = synth.normal(1, (BT, C), 1.0, dev)
