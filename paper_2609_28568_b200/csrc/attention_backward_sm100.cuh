@@ -29,7 +29,7 @@ struct AttnBwdCfg {
     static constexpr uint32_t OFF_OWN = 0;          // the item's own tiles: Q, dO or K, V
     static constexpr uint32_t OFF_RING = 2 * OWN;   // the others, in turn
     static constexpr uint32_t OFF_BAR = OFF_RING + STAGES * TILE;
-    static constexpr uint32_t OFF_ROWS = OFF_BAR + 384;  // dQ: halves of delta of two items; dK, dV: lse and delta of two tiles of queries
+    static constexpr uint32_t OFF_ROWS = OFF_BAR + 384;  // dK, dV: lse and delta of two tiles of queries
     static constexpr uint32_t SMEM = OFF_ROWS + 2048;
     static constexpr int REGS_ROWS = WGS_ == 1 ? 184 : 208, REGS_OTHER = WGS_ == 1 ? 72 : 88;
     static_assert(WGS_ * REGS_ROWS + REGS_OTHER <= (WGS_ + 1) * (WGS_ == 1 ? 128 : 168), "registers");
@@ -70,7 +70,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             ptx::mbar_init(full_bar(lane), 1);
             ptx::mbar_init(empty_bar(lane), 1);
         }
-        if (lane < 9) ptx::mbar_init(named(lane), lane == 5 ? 4 * WGS : 1);
+        if (lane < 9) ptx::mbar_init(named(lane), lane == 5 ? 4 * WGS : lane == 7 ? 4 * WGS + 1 : 1);
         items.init(lane, 4 * WGS + 1);
         if (lane == 31) ptx::st_shared_u32_volatile(abort_addr, 0);
         ptx::fence_barrier_init();
@@ -234,30 +234,33 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             const int row = m.block * 128 + q * 32 + lane;  // of the sequence
             const long long at = m.start + row;
             float delta = 0.0f, nl = 0.0f;
-            {   // delta: a half of the row each where two threads have one
-                const int cols = p.D / 8, mid = WGS == 2 ? (cols + 1) / 2 : cols, c0 = half ? mid : 0, c1 = half ? cols : mid;
-                if (row < m.len) {
-                    const __nv_bfloat16 *g = static_cast<const __nv_bfloat16 *>(b.dout) + at * b.ld_dout + m.head * p.D,
-                                        *o = static_cast<const __nv_bfloat16 *>(p.out) + at * p.ld_out + m.head * p.D;
-#pragma unroll 4
-                    for (int c = c0; c < c1; ++c) {
-                        const uint4 x = ptx::ld_global_v4(g + c * 8), y = ptx::ld_global_v4(o + c * 8);
-                        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+            {   // delta: out from memory, dout from the item's tile. Where two threads have a row, both form all of it: a meeting of theirs could not be
+                // left when a wait has run out elsewhere
+                constexpr int PIECES = D / 8;  // of 16 bytes
+                uint4 y[PIECES];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            delta = fmaf(ptx::bf16_lo(xs[e]), ptx::bf16_lo(ys[e]), delta);
-                            delta = fmaf(ptx::bf16_hi(xs[e]), ptx::bf16_hi(ys[e]), delta);
-                        }
+                for (int c = 0; c < PIECES; ++c) {
+                    y[c] = make_uint4(0, 0, 0, 0);
+                    if (row < m.len && c * 8 < p.D) y[c] = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(p.out) + at * p.ld_out + m.head * p.D + c * 8);
+                }
+                if (row < m.len) nl = -kLog2e * p.lse[static_cast<long long>(m.head) * p.T + at];
+                if (!warp_wait(wctx2, do_bar, static_cast<uint32_t>(k) & 1u, 430)) break;
+                const uint32_t r = static_cast<uint32_t>(q * 32 + lane), do_s = smem + Cfg::OFF_OWN + Cfg::OWN + r * 128;
+#pragma unroll
+                for (int c = 0; c < PIECES; ++c) {
+                    const uint32_t ys[4] = {y[c].x, y[c].y, y[c].z, y[c].w};
+                    uint32_t xs[4];
+                    ptx::ld_shared_v4(do_s + (c >> 3) * kAttnBox + (((c & 7) ^ (r & 7)) << 4), xs[0], xs[1], xs[2], xs[3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        delta = fmaf(ptx::bf16_lo(xs[e]), ptx::bf16_lo(ys[e]), delta);
+                        delta = fmaf(ptx::bf16_hi(xs[e]), ptx::bf16_hi(ys[e]), delta);
                     }
-                    nl = -kLog2e * p.lse[static_cast<long long>(m.head) * p.T + at];
                 }
-                if (WGS == 2) {
-                    const uint32_t mine = smem + Cfg::OFF_ROWS + (k & 1) * 1024 + (q * 32 + lane) * 4;
-                    ptx::st_shared_f32(mine + half * 512, delta);
-                    ptx::named_bar_sync(1, 256);
-                    delta += ptx::ld_shared_f32(mine + (half ^ 1) * 512);
-                }
-                if (half == 0 && row < m.len) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(own_bar);  // this warp has read the item's tile
+                if (row >= m.len) delta = 0.0f;  // dout may hold anything there
+                else if (half == 0) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
             }
             const ptx::f2 base = ptx::make_f2(nl, nl), nd2 = ptx::make_f2(-delta, -delta);
             // keys that all rows of the warp see, that this one sees
