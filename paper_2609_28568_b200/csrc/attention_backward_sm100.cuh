@@ -227,24 +227,34 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         const float sl = p.scale * kLog2e;
         const ptx::f2 sl2 = ptx::make_f2(sl, sl);
         const bool wide = attn_wide(b.dq, b.ld_dq, p.D);
+        constexpr int PIECES = D / 8;  // of 16 bytes
+        uint4 y[PIECES];
+        float l;
+        // an item's rows of out and lse, on their way while the item before is still being stored
+        auto fetch = [&](const AttnItem &m) {
+            const int row = m.block * 128 + q * 32 + lane;
+            const long long at = m.start + row;
+#pragma unroll
+            for (int c = 0; c < PIECES; ++c) {
+                y[c] = make_uint4(0, 0, 0, 0);
+                if (row < m.len && c * 8 < p.D) y[c] = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(p.out) + at * p.ld_out + m.head * p.D + c * 8);
+            }
+            l = row < m.len ? __ldcg(p.lse + static_cast<long long>(m.head) * p.T + at) : 0.0f;
+        };
         uint32_t done = 0;  // tiles before this item
         AttnItem m;
-        for (int k = 0; items.take<true>(wctx2, k, m); ++k) {
+        bool more = items.take<true>(wctx2, 0, m);
+        if (more) fetch(m);
+        for (int k = 0; more; ++k) {
             const int n = tiles_of(m);
             const int row = m.block * 128 + q * 32 + lane;  // of the sequence
             const long long at = m.start + row;
-            float delta = 0.0f, nl = 0.0f;
-            {   // delta: out from memory, dout from the item's tile. Where two threads have a row, both form all of it: a meeting of theirs could not be
-                // left when a wait has run out elsewhere
-                constexpr int PIECES = D / 8;  // of 16 bytes
-                uint4 y[PIECES];
-#pragma unroll
-                for (int c = 0; c < PIECES; ++c) {
-                    y[c] = make_uint4(0, 0, 0, 0);
-                    if (row < m.len && c * 8 < p.D) y[c] = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(p.out) + at * p.ld_out + m.head * p.D + c * 8);
-                }
-                if (row < m.len) nl = -kLog2e * p.lse[static_cast<long long>(m.head) * p.T + at];
-                if (!warp_wait(wctx2, do_bar, static_cast<uint32_t>(k) & 1u, 430)) break;
+            float delta = 0.0f;
+            const float nl = -kLog2e * l;
+            // delta: out from memory, dout from the item's tile. Where two threads have a row, both form all of it: a meeting of theirs could not be left
+            // when a wait has run out elsewhere
+            if (!warp_wait(wctx2, do_bar, static_cast<uint32_t>(k) & 1u, 430)) break;
+            {
                 const uint32_t r = static_cast<uint32_t>(q * 32 + lane), do_s = smem + Cfg::OFF_OWN + Cfg::OWN + r * 128;
 #pragma unroll
                 for (int c = 0; c < PIECES; ++c) {
@@ -315,14 +325,18 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(ds_bar);
             }
-            if (ok) ok = warp_wait(wctx2, done_bar, static_cast<uint32_t>(k) & 1u, 420);
             if (!ok) break;
+            AttnItem next;
+            more = items.take<true>(wctx2, k + 1, next);
+            if (more) fetch(next);
+            if (!warp_wait(wctx2, done_bar, static_cast<uint32_t>(k) & 1u, 420)) break;
             done += n;
             ptx::tc_fence_after();
             constexpr int W = D / WGS;  // columns of a thread
             attn_store_row<W>(dq_tm + lanes + half * W, p.scale, static_cast<__nv_bfloat16 *>(b.dq) + at * b.ld_dq + m.head * p.D + half * W, row < m.len,
                               p.D - half * W, wide);
             ptx::tc_fence_before();
+            m = next;
         }
         ptx::tc_fence_before();
     }
