@@ -227,19 +227,23 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         const float sl = p.scale * kLog2e;
         const ptx::f2 sl2 = ptx::make_f2(sl, sl);
         const bool wide = attn_wide(b.dq, b.ld_dq, p.D);
-        constexpr int PIECES = D / 8;  // of 16 bytes
-        uint4 y[PIECES];
+        // A warp reads its 32 rows of out four (two, of wide heads) at a time, 16 bytes a lane, so that lanes that follow one another read what follows
+        // one another: a row a lane took the loads eight times as long.
+        constexpr int LANES = D / 8, AT_ONCE = 32 / LANES, READS = 32 / AT_ONCE;
+        const int piece = lane % LANES, sub = lane / LANES;
+        uint4 y[READS];
         float l;
         // an item's rows of out and lse, on their way while the item before is still being stored
         auto fetch = [&](const AttnItem &m) {
-            const int row = m.block * 128 + q * 32 + lane;
-            const long long at = m.start + row;
+            const int row0 = m.block * 128 + q * 32;
 #pragma unroll
-            for (int c = 0; c < PIECES; ++c) {
+            for (int c = 0; c < READS; ++c) {
+                const int row = row0 + c * AT_ONCE + sub;
                 y[c] = make_uint4(0, 0, 0, 0);
-                if (row < m.len && c * 8 < p.D) y[c] = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(p.out) + at * p.ld_out + m.head * p.D + c * 8);
+                if (row < m.len && piece * 8 < p.D)
+                    y[c] = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(p.out) + (m.start + row) * p.ld_out + m.head * p.D + piece * 8);
             }
-            l = row < m.len ? __ldcg(p.lse + static_cast<long long>(m.head) * p.T + at) : 0.0f;
+            l = row0 + lane < m.len ? __ldcg(p.lse + static_cast<long long>(m.head) * p.T + m.start + row0 + lane) : 0.0f;
         };
         uint32_t done = 0;  // tiles before this item
         AttnItem m;
@@ -255,17 +259,22 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             // when a wait has run out elsewhere
             if (!warp_wait(wctx2, do_bar, static_cast<uint32_t>(k) & 1u, 430)) break;
             {
-                const uint32_t r = static_cast<uint32_t>(q * 32 + lane), do_s = smem + Cfg::OFF_OWN + Cfg::OWN + r * 128;
+                const uint32_t do_s = smem + Cfg::OFF_OWN + Cfg::OWN + (piece >> 3) * kAttnBox;
 #pragma unroll
-                for (int c = 0; c < PIECES; ++c) {
-                    const uint32_t ys[4] = {y[c].x, y[c].y, y[c].z, y[c].w};
+                for (int c = 0; c < READS; ++c) {
+                    const uint32_t r = static_cast<uint32_t>(q * 32 + c * AT_ONCE + sub), ys[4] = {y[c].x, y[c].y, y[c].z, y[c].w};
                     uint32_t xs[4];
-                    ptx::ld_shared_v4(do_s + (c >> 3) * kAttnBox + (((c & 7) ^ (r & 7)) << 4), xs[0], xs[1], xs[2], xs[3]);
+                    ptx::ld_shared_v4(do_s + r * 128 + (((piece & 7) ^ (r & 7)) << 4), xs[0], xs[1], xs[2], xs[3]);
+                    float part = 0.0f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        delta = fmaf(ptx::bf16_lo(xs[e]), ptx::bf16_lo(ys[e]), delta);
-                        delta = fmaf(ptx::bf16_hi(xs[e]), ptx::bf16_hi(ys[e]), delta);
+                        part = fmaf(ptx::bf16_lo(xs[e]), ptx::bf16_lo(ys[e]), part);
+                        part = fmaf(ptx::bf16_hi(xs[e]), ptx::bf16_hi(ys[e]), part);
                     }
+#pragma unroll
+                    for (int e = LANES / 2; e > 0; e /= 2) part += __shfl_xor_sync(0xffffffffu, part, e);
+                    part = __shfl_sync(0xffffffffu, part, (lane % AT_ONCE) * LANES);  // row c AT_ONCE + i stands in the i-th group
+                    if (lane / AT_ONCE == c) delta = part;
                 }
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(own_bar);  // this warp has read the item's tile
