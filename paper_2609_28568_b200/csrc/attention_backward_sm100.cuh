@@ -6,9 +6,10 @@
 //
 // Both form P and dS themselves: seven products of tiles in place of five, for which no gradient crosses memory in fp32 and
 // none is added up by atomics. The second pass works on transposed tiles (S^T = K Q^T, dP^T = V dO^T), so that P^T and dS^T stand in tensor
-// memory as the A operands of its sums. P and dS are rounded to bf16 for them (half an ulp, 2^-8 of each at most); all sums are fp32. A row of dS adds up
-// to next to nothing, so what the keys have in common cancels in dQ while the roundings of dS do not: there dS is given in two pieces of bf16, the
-// second what the first left out, at the price of one more product (dQ of keys that share half their length was 2.7e-3 off, 1.7e-3 of it its own rounding).
+// memory as the A operands of its sums. P is rounded to bf16 for them (half an ulp, 2^-8 at most); all sums are fp32. A row of dS adds up to next to
+// nothing, so what the keys have in common cancels in dQ while the roundings of dS do not, and much the same holds for dK: dS is given in two pieces of
+// bf16, the second what the first left out, at the price of a product more in each pass. (With one piece dQ of keys that share half their length
+// was 2.7e-3 off and dK up to 2.6e-3, of which their own rounding to bf16 is 1.7e-3.)
 //
 // A thread has 64 values of a row of a tile: heads of up to 64 columns take tiles of 64 columns with one warpgroup, two blocks to an SM, which fill
 // each other's gaps; wider heads have no tensor memory for that and take tiles of 128 with two warpgroups. While these turn dP into dS, the
@@ -36,6 +37,16 @@ struct AttnBwdCfg {
     static_assert(SMEM <= (BLOCKS == 2 ? 113 * 1024 : 232448), "shared memory");
     static_assert(2 * ROWS + 2 * D_ <= TMEM && 3 * ROWS + D_ <= TMEM, "tensor memory");
 };
+
+// Two numbers in two pieces of bf16: rounded, and what that left out, rounded
+__device__ __forceinline__ void split_bf16x2(ptx::f2 v, uint32_t &hi, uint32_t &lo)
+{
+    float a, b;
+    ptx::split_f2(v, a, b);
+    hi = ptx::pack_bf16x2(a, b);
+    ptx::split_f2(ptx::fma2(ptx::make_f2_bits(hi << 16, hi & 0xffff0000u), ptx::make_f2(-1.0f, -1.0f), v), a, b);
+    lo = ptx::pack_bf16x2(a, b);
+}
 
 // ------------------------------------------------------------------------------------------------ dQ
 template <class Cfg>
@@ -311,12 +322,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         const ptx::f2 ds = ptx::mul2(ptx::add2(ptx::make_f2_bits(g[c][i], g[c][i + 1]), nd2), ptx::make_f2_bits(s[c][i], s[c][i + 1]));
-                        float x, y;
-                        ptx::split_f2(ds, x, y);
-                        const uint32_t w = ptx::pack_bf16x2(x, y);
-                        hi[c * 16 + (i >> 1)] = w;
-                        ptx::split_f2(ptx::fma2(ptx::make_f2_bits(w << 16, w & 0xffff0000u), ptx::make_f2(-1.0f, -1.0f), ds), x, y);
-                        lo[c * 16 + (i >> 1)] = ptx::pack_bf16x2(x, y);
+                        split_bf16x2(ds, hi[c * 16 + (i >> 1)], lo[c * 16 + (i >> 1)]);
                     }
                 if (seen_by_all - j * ROWS - half * 64 < 64) {  // columns that are not seen may hold anything
                     const int limit = seen - j * ROWS - half * 64;
@@ -540,6 +546,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                         if (!ok) break;
                         ptx::tc_fence_after();
                         attn_mma_tn<WGS == 2, ROWS>(dk_tm, dp_tm, tile(2 * i), idesc_d, steps, i > 0);
+                        attn_mma_tn<WGS == 2, ROWS>(dk_tm, dp_tm + 32, tile(2 * i), idesc_d, steps, true);  // what the roundings left out
                         ptx::umma_commit<1>(empty_bar(stage(2 * i)));
                         if (i + 1 < n) ok = grads(i + 1);
                         if (++t == per_head) t = 0;
@@ -644,7 +651,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 ok = warp_wait(wctx2, dp_bar, par, 410);
                 if (!ok) break;
                 ptx::tc_fence_after();
-                uint32_t g[2][32];
+                uint32_t g[2][32], lo[32];
                 ptx::tmem_ld_32x32_x2_wait(dp_tm + lanes + half * 64, dp_tm + lanes + half * 64 + 32, g[0], g[1]);
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
@@ -652,19 +659,22 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                     for (int e = 0; e < 32; e += 4) {
                         float4 d;
                         ptx::ld_shared_f32x4(rows + 512 + (c * 32 + e) * 4, d);
-                        float x[4];
-                        ptx::split_f2(ptx::mul2(ptx::add2(ptx::make_f2_bits(g[c][e], g[c][e + 1]), ptx::make_f2(d.x, d.y)),
-                                                ptx::make_f2_bits(s[c][e], s[c][e + 1])), x[0], x[1]);
-                        ptx::split_f2(ptx::mul2(ptx::add2(ptx::make_f2_bits(g[c][e + 2], g[c][e + 3]), ptx::make_f2(d.z, d.w)),
-                                                ptx::make_f2_bits(s[c][e + 2], s[c][e + 3])), x[2], x[3]);
-                        pk[c * 16 + (e >> 1)] = ptx::pack_bf16x2(x[0], x[1]);
-                        pk[c * 16 + (e >> 1) + 1] = ptx::pack_bf16x2(x[2], x[3]);
+#pragma unroll
+                        for (int v = 0; v < 4; v += 2)
+                            split_bf16x2(ptx::mul2(ptx::add2(ptx::make_f2_bits(g[c][e + v], g[c][e + v + 1]), v ? ptx::make_f2(d.z, d.w) : ptx::make_f2(d.x, d.y)),
+                                                   ptx::make_f2_bits(s[c][e + v], s[c][e + v + 1])),
+                                         pk[c * 16 + ((e + v) >> 1)], lo[c * 16 + ((e + v) >> 1)]);
                     }
                 if (cut) {  // what is not seen may hold anything
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) pk[e] = 2 * e >= hidden ? pk[e] : 2 * e + 1 >= hidden ? pk[e] & 0xffff0000u : 0u;
+                    for (int e = 0; e < 32; ++e) {
+                        const uint32_t keep = 2 * e >= hidden ? 0xffffffffu : 2 * e + 1 >= hidden ? 0xffff0000u : 0u;
+                        pk[e] &= keep;
+                        lo[e] &= keep;
+                    }
                 }
                 ptx::tmem_st_32x32(dp_tm + lanes + half * 64, pk);
+                ptx::tmem_st_32x32(dp_tm + lanes + half * 64 + 32, lo);
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before();
                 __syncwarp();
