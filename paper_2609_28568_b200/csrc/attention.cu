@@ -22,7 +22,17 @@ static AttnKernel backward_kv_kernel()
 {
     return {reinterpret_cast<const void *>(&attn_backward_kv_kernel<Cfg>), Cfg::THREADS, Cfg::SMEM, 128, Cfg::ROWS};
 }
-AttnKernel attn_backward_q(int D) { return D <= 64 ? backward_q_kernel<AttnBwdCfg<64, 1>>() : backward_q_kernel<AttnBwdCfg<128, 2>>(); }
-AttnKernel attn_backward_kv(int D) { return D <= 64 ? backward_kv_kernel<AttnBwdCfg<64, 1>>() : backward_kv_kernel<AttnBwdCfg<128, 2>>(); }
+AttnKernel attn_backward_delta(int D)
+{
+    return {reinterpret_cast<const void *>(D <= 64 ? &attn_backward_delta_kernel<64> : &attn_backward_delta_kernel<128>), 256, 0, 256 / (D <= 64 ? 8 : 16), 0};
+}
+AttnKernel attn_backward_q(int D, bool few)
+{
+    return D > 64 ? backward_q_kernel<AttnBwdCfg<128, 2>>() : few ? backward_q_kernel<AttnBwdCfg<64, 2>>() : backward_q_kernel<AttnBwdCfg<64, 1>>();
+}
+AttnKernel attn_backward_kv(int D, bool few)
+{
+    return D > 64 ? backward_kv_kernel<AttnBwdCfg<128, 2>>() : few ? backward_kv_kernel<AttnBwdCfg<64, 2>>() : backward_kv_kernel<AttnBwdCfg<64, 1>>();
+}
 
 }  // namespace nb

@@ -22,7 +22,8 @@ struct AttnParams {
 
 struct AttnBackward {
     AttnParams a;            // a.out: the forward pass's output, a.ld_out its ld; a.lse: read
-    float *delta;            // [heads, T]: sum over a row of dout out, written by the pass of dq, read by that of dk and dv
+    float *delta;            // [heads, T]: sum over a row of dout out, for the pass of dk and dv
+    int side;                // the passes run side by side: delta is there before either of them
     const void *dout;
     void *dq, *dk, *dv;
     long long ld_dout, ld_dq, ld_dk, ld_dv;
@@ -36,7 +37,8 @@ struct AttnKernel {
     int rows, streamed;
 };
 AttnKernel attn_forward(int D);
-AttnKernel attn_backward_q(int D);   // maps: q, dout, k, v
-AttnKernel attn_backward_kv(int D);  // the same
+AttnKernel attn_backward_delta(int D);         // no maps; a block has `rows` of all rows of all heads, fewer than 2^31
+AttnKernel attn_backward_q(int D, bool few);   // maps: q, dout, k, v; few: a block to an SM in place of two (D <= 64)
+AttnKernel attn_backward_kv(int D, bool few);  // the same
 
 }  // namespace nb

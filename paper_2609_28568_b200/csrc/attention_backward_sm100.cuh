@@ -12,9 +12,12 @@
 // was 2.7e-3 off and dK up to 2.6e-3, of which their own rounding to bf16 is 1.7e-3.)
 //
 // A thread has 64 values of a row of a tile: heads of up to 64 columns take tiles of 64 columns with one warpgroup, two blocks to an SM, which fill
-// each other's gaps; wider heads have no tensor memory for that and take tiles of 128 with two warpgroups. While these turn dP into dS, the
+// each other's gaps; wider heads have no tensor memory for that and take tiles of 128 with two warpgroups, as narrow ones do in passes of few items. While these turn dP into dS, the
 // tensor core works on what P was ready for, and the other way round. A block that is done with its item takes another (attention_sm100.cuh), whose tiles
 // and first products come while the last gradients are being stored.
+//
+// Passes that fill the GPU follow one another, and that of dQ leaves delta behind. Where both together do not, delta has a kernel of its own, and dQ and dK, dV run side by side:
+// the pass of dQ lets its successor start when delta and all inputs are there, and dK and dV's blocks wait for dQ's at their end only.
 #pragma once
 #include "attention_sm100.cuh"
 
@@ -46,6 +49,42 @@ __device__ __forceinline__ void split_bf16x2(ptx::f2 v, uint32_t &hi, uint32_t &
     hi = ptx::pack_bf16x2(a, b);
     ptx::split_f2(ptx::fma2(ptx::make_f2_bits(hi << 16, hi & 0xffff0000u), ptx::make_f2(-1.0f, -1.0f), v), a, b);
     lo = ptx::pack_bf16x2(a, b);
+}
+
+__device__ __forceinline__ float dot_bf16x8(uint4 x, uint4 y)
+{
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        sum = fmaf(ptx::bf16_lo(xs[e]), ptx::bf16_lo(ys[e]), sum);
+        sum = fmaf(ptx::bf16_hi(xs[e]), ptx::bf16_hi(ys[e]), sum);
+    }
+    return sum;
+}
+
+// ------------------------------------------------------------------------------------------------ delta
+// For both passes, where they run side by side. Lanes that follow one another read what follows one another: D / 8 of them (rounded up) have a row of a head, and the
+// next ones the row of the next head. All rows are read, whether they are of a sequence or not.
+template <int D>
+__global__ void __launch_bounds__(256)
+attn_backward_delta_kernel(const AttnBackward b)
+{
+    ptx::grid_launch_dependents();
+    ptx::grid_dependency_wait();
+    constexpr int LANES = D / 8, ROWS = 256 / LANES;
+    const AttnParams &p = b.a;
+    const int piece = static_cast<int>(threadIdx.x) % LANES;
+    const int i = static_cast<int>(blockIdx.x * ROWS + threadIdx.x / LANES), row = i / p.heads, head = i - row * p.heads;
+    float sum = 0.0f;
+    if (row < p.T && piece * 8 < p.D) {
+        const uint4 x = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(b.dout) + row * b.ld_dout + head * p.D + piece * 8);
+        const uint4 y = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(p.out) + row * p.ld_out + head * p.D + piece * 8);
+        sum = dot_bf16x8(x, y);
+    }
+#pragma unroll
+    for (int e = LANES / 2; e > 0; e /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, e);
+    if (row < p.T && piece == 0) b.delta[static_cast<long long>(head) * p.T + row] = sum;
 }
 
 // ------------------------------------------------------------------------------------------------ dQ
@@ -105,8 +144,9 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         ptx::tc_fence_after();
     }
     const uint32_t tmem = ptx::ld_shared_u32_volatile(tmem_slot);
-    ptx::grid_launch_dependents();
+    if (!b.side) ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
+    if (b.side) ptx::grid_launch_dependents();  // dK and dV may start: all that they read is there
     const uint32_t dp_tm = tmem + 2 * ROWS, dq_tm = tmem + 3 * ROWS;  // scores: two tiles from 0 on
     auto tiles_of = [&](const AttnItem &m) {  // tiles of keys that an item's queries see
         const int tiles = (m.len + ROWS - 1) / ROWS;
@@ -273,15 +313,10 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                 const uint32_t do_s = smem + Cfg::OFF_OWN + Cfg::OWN + (piece >> 3) * kAttnBox;
 #pragma unroll
                 for (int c = 0; c < READS; ++c) {
-                    const uint32_t r = static_cast<uint32_t>(q * 32 + c * AT_ONCE + sub), ys[4] = {y[c].x, y[c].y, y[c].z, y[c].w};
-                    uint32_t xs[4];
-                    ptx::ld_shared_v4(do_s + r * 128 + (((piece & 7) ^ (r & 7)) << 4), xs[0], xs[1], xs[2], xs[3]);
-                    float part = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        part = fmaf(ptx::bf16_lo(xs[e]), ptx::bf16_lo(ys[e]), part);
-                        part = fmaf(ptx::bf16_hi(xs[e]), ptx::bf16_hi(ys[e]), part);
-                    }
+                    const uint32_t r = static_cast<uint32_t>(q * 32 + c * AT_ONCE + sub);
+                    uint4 x;
+                    ptx::ld_shared_v4(do_s + r * 128 + (((piece & 7) ^ (r & 7)) << 4), x.x, x.y, x.z, x.w);
+                    float part = dot_bf16x8(x, y[c]);
 #pragma unroll
                     for (int e = LANES / 2; e > 0; e /= 2) part += __shfl_xor_sync(0xffffffffu, part, e);
                     part = __shfl_sync(0xffffffffu, part, (lane % AT_ONCE) * LANES);  // row c AT_ONCE + i stands in the i-th group
@@ -290,7 +325,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(own_bar);  // this warp has read the item's tile
                 if (row >= m.len) delta = 0.0f;  // dout may hold anything there
-                else if (half == 0) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
+                else if (half == 0 && !b.side) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
             }
             const ptx::f2 base = ptx::make_f2(nl, nl), nd2 = ptx::make_f2(-delta, -delta);
             // keys that all rows of the warp see, that this one sees
@@ -430,7 +465,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     }
     const uint32_t tmem = ptx::ld_shared_u32_volatile(tmem_slot);
     ptx::grid_launch_dependents();
-    ptx::grid_dependency_wait();
+    if (!b.side) ptx::grid_dependency_wait();
     const int kv_heads = p.heads / p.group;
     const uint32_t s_tm = tmem, dp_tm = tmem + ROWS, dv_tm = tmem + 2 * ROWS, dk_tm = dv_tm + D;
     // tiles of queries that see an item's keys: from first_of on, per head
@@ -712,6 +747,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         ptx::tc_fence_after();
         ptx::tmem_dealloc<1>(tmem, Cfg::TMEM);
     }
+    if (b.side) ptx::grid_dependency_wait();  // what waits for this pass waits for that of dQ too
 }
 
 }  // namespace nb

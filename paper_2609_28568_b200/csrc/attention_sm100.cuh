@@ -58,8 +58,8 @@ public:
             start_[c] = len_[c] = 0;
             if (i < p.n && p.n <= 32 * kOwn) {
                 if (p.cu) {
-                    start_[c] = min(max(p.cu[i], 0), p.T);
-                    len_[c] = min(max(p.cu[i + 1], start_[c]), p.T) - start_[c];
+                    start_[c] = min(max(__ldcg(p.cu + i), 0), p.T);
+                    len_[c] = min(max(__ldcg(p.cu + i + 1), start_[c]), p.T) - start_[c];
                 } else {
                     len_[c] = p.T / p.n;
                     start_[c] = i * len_[c];
@@ -87,14 +87,14 @@ public:
                 while (hi - lo > 1) {
                     const int step = (hi - lo + 31) / 32;
                     const int i = lo + lane * step;
-                    const unsigned before = __ballot_sync(0xffffffffu, i < hi && max(p.cu[i], 0) / 128 + i <= k);
+                    const unsigned before = __ballot_sync(0xffffffffu, i < hi && max(__ldcg(p.cu + i), 0) / 128 + i <= k);
                     const int last = before ? 31 - __clz(before) : 0;
                     lo += last * step;
                     hi = min(hi, lo + step);
                 }
-                first = max(p.cu[lo], 0) / 128 + lo;
-                s.start = min(max(p.cu[lo], 0), p.T);
-                s.len = min(max(p.cu[lo + 1], s.start), p.T) - s.start;
+                first = max(__ldcg(p.cu + lo), 0) / 128 + lo;
+                s.start = min(max(__ldcg(p.cu + lo), 0), p.T);
+                s.len = min(max(__ldcg(p.cu + lo + 1), s.start), p.T) - s.start;
             }
             const int local = k - first, n = blocks(s.len);
             if (local >= 0 && local < n) s.block = from_end ? local : n - 1 - local;
@@ -128,7 +128,7 @@ public:
 __device__ __forceinline__ void attn_report_bounds(const int *cu, int n, int T, int *status)
 {
     for (int i = static_cast<int>(threadIdx.x & 31); i <= n; i += 32)
-        if (cu[i] < (i ? cu[i - 1] : 0) || cu[i] > T)
+        if (__ldcg(cu + i) < (i ? __ldcg(cu + i - 1) : 0) || __ldcg(cu + i) > T)
             if (atomicCAS(status, 0, kStatusBadSequences) == 0) status[1] = i;
 }
 

@@ -2230,6 +2230,24 @@ int64_t attn_slots(const AttnParams &p, int rows)
 }
 
 // Launches an attention kernel on the sequences' blocks for each of `heads` heads.
+// Launches the kernel that forms delta ahead of both passes.
+int launch_delta(const AttnKernel &k, AttnBackward &b, cudaStream_t stream)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>(b.a.T) * b.a.heads + k.rows - 1) / k.rows));
+    cfg.blockDim = dim3(static_cast<unsigned>(k.threads));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = dependent_launch_allowed(stream) ? 1 : 0;
+    void *args[] = {&b};
+    NB_CUDA(cudaLaunchKernelExC(&cfg, k.fn, args));
+    ++g_launches;
+    return NB_OK;
+}
+
 template <int MAPS, class P>
 int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtensorMap (&maps)[MAPS], P &p, const AttnParams &a, int64_t heads,
                      cudaStream_t stream)
@@ -3125,7 +3143,12 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
     b.ld_dq = ld_dq;
     b.ld_dk = ld_dk;
     b.ld_dv = ld_dv;
-    const AttnKernel of_q = attn_backward_q(b.a.D), of_kv = attn_backward_kv(b.a.D);
+    const int64_t slots = attn_slots(b.a, 128);
+    // Heads of up to 64 columns, passes of few items: a block to itself on an SM, with tiles twice as long, in place of two blocks. An item is done in little
+    // more than half the time, which counts where the longest one does (both passes, in us, two blocks / one: 500 x 12 heads 32 / 23, 1000 x 12 54 / 35,
+    // 2000 x 12 98 / 57, 3000 x 16 134 / 117; 4 x 1024 x 12, 384 items: 58 / 57, 8 x 1024: 99 / 104, 16 x 1024: 176 / 187).
+    auto few = [&](int64_t h) { return slots * h <= 3ll * s->num_sms; };
+    const AttnKernel of_q = attn_backward_q(b.a.D, few(heads)), of_kv = attn_backward_kv(b.a.D, few(kv_heads));
     CUtensorMap mq[4], mkv[4];  // of q, dout, k, v: whole blocks of one pass are streamed by the other
     if ((rc = get_heads_tmap(*s, &mq[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &mq[1], dout, T, D, heads, ld_dout)) != NB_OK ||
         (rc = get_heads_tmap(*s, &mq[2], k, T, D, kv_heads, ld_k, of_q.streamed)) != NB_OK ||
@@ -3134,10 +3157,15 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
         (rc = get_heads_tmap(*s, &mkv[1], dout, T, D, heads, ld_dout, of_kv.streamed)) != NB_OK ||
         (rc = get_heads_tmap(*s, &mkv[2], k, T, D, kv_heads, ld_k)) != NB_OK || (rc = get_heads_tmap(*s, &mkv[3], v, T, D, kv_heads, ld_v)) != NB_OK)
         return rc;
-    static bool attr_set[4][kMaxDevices] = {};
+    static bool attr_set[6][kMaxDevices] = {};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if ((rc = launch_attention(of_q, attr_set[D > 64], mq, b, b.a, heads, stream)) != NB_OK) return rc;
-    return launch_attention(of_kv, attr_set[2 + (D > 64)], mkv, b, b.a, kv_heads, stream);
+    // Side by side (a launch more) where the items of both passes together are at most two to an SM, in us, in turn / side by side:
+    // 1 x 12 heads of 64: 13 / 11, 500 x 12: 23 / 16, 1000 x 12: 35 / 29, 1000 x 12 of 128: 44 / 33; 8 sequences of 128 x 12, in 384 slots: 16 / 18,
+    // 2000 x 12: 57 / 53, 4 x 1024 x 12: 57 / 59, 16 x 1024 x 12: 176 / 186 (the passes get into each other's way in L2 and on an SM).
+    b.side = slots * (heads + kv_heads) <= 2ll * s->num_sms;
+    if (b.side && (rc = launch_delta(attn_backward_delta(b.a.D), b, stream)) != NB_OK) return rc;
+    if ((rc = launch_attention(of_q, attr_set[D > 64 ? 0 : few(heads) ? 1 : 2], mq, b, b.a, heads, stream)) != NB_OK) return rc;
+    return launch_attention(of_kv, attr_set[D > 64 ? 3 : few(kv_heads) ? 4 : 5], mkv, b, b.a, kv_heads, stream);
 }
 
 int nb_workspace_reserve(int64_t bytes)
@@ -3382,7 +3410,7 @@ int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us)
     b.dk = tensors[7];
     b.dv = tensors[8];
     b.delta = static_cast<float *>(tensors[9]);
-    const AttnKernel kernel = pass == 0 ? attn_forward(D) : pass == 1 ? attn_backward_q(D) : attn_backward_kv(D);
+    const AttnKernel kernel = pass == 0 ? attn_forward(D) : pass == 1 ? attn_backward_q(D, false) : attn_backward_kv(D, false);
     const uint32_t own = 128, streamed = static_cast<uint32_t>(kernel.streamed);
     CUtensorMap q, k, v, dout;
     if ((rc = get_heads_tmap(*s, &q, tensors[0], T, D, 1, D, pass == 2 ? streamed : own)) != NB_OK ||
