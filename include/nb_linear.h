@@ -435,7 +435,8 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
  *   dout, out  [in]  [T, heads, D] bf16;  lse [in] [heads, T] fp32;  the rest as in the forward pass
  *   workspace  device memory of nb_attention_workspace(T, heads) bytes, 16-byte aligned, the caller's: calls that may run at the same time (on two streams,
  *              or captured into two graphs) need one each
- * Sums are fp32 and in a fixed order: the same inputs give the same bits. p and ds are rounded to bf16 for the tensor cores, gradients once at the end.
+ * Sums are fp32 and in a fixed order: the same inputs give the same bits. For the tensor cores p is rounded to bf16 and ds given
+ * in two pieces of bf16, rounded and what that left out; gradients are rounded once at the end.
  * Rows in no sequence are not written. What is not finite in one sequence reaches no other.
  * nb_attention_workspace returns -1 for sizes that the call would refuse.
  */
@@ -607,7 +608,8 @@ int nb_debug_muon_timeout(void *update, const void *grad, void *workspace, int64
 /*
  * The same for the attention kernels (pass 0: forward, 1: dq, 2: dk and dv) over one sequence of 256 rows and one head of 64, whose streamed tiles wait for
  * 16 bytes more than their copies bring. The products' bounded wait for the first of them runs out; nothing of the pass's results is written but, in pass 1, the workspace.
- * nb_check_status() reports NB_ERR_TIMEOUT naming wait 300. tensors: q, k, v, out, lse, dout, dq, dk, dv, workspace.
+ * nb_check_status() reports NB_ERR_TIMEOUT naming wait 300. tensors: q, k, v, out, lse, dout, dq, dk, dv, workspace. Passes 8, 9 and 10: the same over 512 rows,
+ * whose blocks are shared by two thread blocks each (with more than one tile to walk over).
  */
 int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us);
 

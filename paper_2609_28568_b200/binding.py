@@ -409,7 +409,7 @@ def nb_debug_muon_timeout(update, grad, workspace, workspace_bytes: int, limit_u
 
 
 def nb_debug_attention_timeout(tensors, which: int, limit_us: int) -> None:
-    """A pass of attention over 256 rows whose streamed tiles never come whole: exercises the kernels' time-out exit."""
+    """A pass of attention over 256 rows (512 of passes 8 to 10) whose streamed tiles never come whole: exercises the kernels' time-out exit."""
     lib().nb_set_stream(_stream())
     _check(lib().nb_debug_attention_timeout((_vp * len(tensors))(*(_ptr(t) for t in tensors)), which, limit_us))
 

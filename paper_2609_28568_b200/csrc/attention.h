@@ -17,6 +17,7 @@ struct AttnParams {
     float *lse;              // [heads, T]; forward: or null
     int *status;
     unsigned long long timeout_ns;
+    int parts;               // blocks of an item's cluster, which share its tiles (1: a block to an item)
     int withhold;            // nb_debug_attention_timeout only: bytes that a tile of the ring waits for beyond what its copies bring
 };
 
@@ -36,9 +37,9 @@ struct AttnKernel {
     uint32_t smem;
     int rows, streamed;
 };
-AttnKernel attn_forward(int D);
+AttnKernel attn_forward(int D, bool split);
 AttnKernel attn_backward_delta(int D);         // no maps; a block has `rows` of all rows of all heads, fewer than 2^31
-AttnKernel attn_backward_q(int D, bool few);   // maps: q, dout, k, v; few: a block to an SM in place of two (D <= 64)
-AttnKernel attn_backward_kv(int D, bool few);  // the same
+AttnKernel attn_backward_q(int D, bool few, bool split);   // maps: q, dout, k, v; few: a block to an SM in place of two (D <= 64); split: few too
+AttnKernel attn_backward_kv(int D, bool few, bool split);  // the same
 
 }  // namespace nb

@@ -15,6 +15,8 @@
 // each other's gaps; wider heads have no tensor memory for that and take tiles of 128 with two warpgroups, as narrow ones do in passes of few items. While these turn dP into dS, the
 // tensor core works on what P was ready for, and the other way round. A block that is done with its item takes another (attention_sm100.cuh), whose tiles
 // and first products come while the last gradients are being stored.
+// Few items with much to walk over (one head of keys for many of queries: a block has all their tiles) are shared by the blocks of a cluster as in the forward
+// pass (SPLIT), which add up their sums in a fixed order.
 //
 // Passes that fill the GPU follow one another, and that of dQ leaves delta behind. Where both together do not, delta has a kernel of its own, and dQ and dK, dV run side by side:
 // the pass of dQ lets its successor start when delta and all inputs are there, and dK and dV's blocks wait for dQ's at their end only.
@@ -88,12 +90,12 @@ attn_backward_delta_kernel(const AttnBackward b)
 }
 
 // ------------------------------------------------------------------------------------------------ dQ
-template <class Cfg>
+template <class Cfg, bool SPLIT>
 __global__ void __launch_bounds__(Cfg::THREADS, Cfg::BLOCKS)
 attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDO, const __grid_constant__ CUtensorMap tmK,
    const __grid_constant__ CUtensorMap tmV, const AttnBackward b)
 {
-    constexpr int D = Cfg::D, WGS = Cfg::WGS, ROWS = Cfg::ROWS, STAGES = Cfg::STAGES, LOAD = 4 * WGS, MMA = LOAD + 1;
+    constexpr int D = Cfg::D, WGS = Cfg::WGS, ROWS = Cfg::ROWS, STAGES = Cfg::STAGES, LOAD = 4 * WGS, MMA = LOAD + 1, LEAST = 2;
     const AttnParams &p = b.a;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem = ptx::smem_u32(smem_raw);
@@ -152,6 +154,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         const int tiles = (m.len + ROWS - 1) / ROWS;
         return p.causal ? min(tiles, (m.block + 1) * (128 / ROWS)) : tiles;
     };
+    auto part_of = [&](const AttnItem &m) { return attn_part<SPLIT, LEAST>(p.parts, tiles_of(m)); };  // this block's
 
     if (!smem_ok) {
         // nothing to do
@@ -164,18 +167,19 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             uint32_t phase = 0, parts = 0, asked = 0;
             AttnOrder order;
             order.load(p);
-            for (int k = 0, at = static_cast<int>(blockIdx.x); ok;) {
+            for (int k = 0, at = static_cast<int>(SPLIT ? blockIdx.x / p.parts : blockIdx.x); ok;) {
                 AttnItem m{0, 0, -1, 0};
                 if (at >= 0) {
                     const AttnSpan s = order.item(p, at / p.heads, false);
                     m = {s.start, s.len, s.block, at % p.heads};
                 }
-                if (at < 0 || m.block >= 0) {  // slots without a block are passed over
+                if (SPLIT || at < 0 || m.block >= 0) {  // slots without a block are passed over
                     ok = items.put(wctx2, k, m);
-                    if (!ok || at < 0) break;
-                    const int n = tiles_of(m), kv_head = m.head / p.group;
-                    for (int i = 0; i < 2 * n && ok; ++i) {
-                        const int j = i >> 1;
+                    if (!ok || m.block < 0) break;
+                    const AttnPart own = part_of(m);
+                    const int kv_head = m.head / p.group;
+                    for (int i = 0; i < 2 * own.n && ok; ++i) {
+                        const int j = own.first + (i >> 1);
                         if (i == 0) {
                             ok = warp_wait(wctx2, own_bar, (static_cast<uint32_t>(k) & 1u) ^ 1u, 130);
                             if (!ok) break;
@@ -214,7 +218,8 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                     if (!ok) break;
                     ++k;
                 }
-                ok = items.next(wctx2, asked, at);
+                if (SPLIT) at = -1;
+                else ok = items.next(wctx2, asked, at);
             }
         } else if (warp == MMA) {
             // ------------------------------------------------------------ products
@@ -229,7 +234,9 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                 auto ready = [&](uint32_t i) { return wait_barrier(wctx, full_bar(stage(i)), ((2 * done + i) / STAGES) & 1u, 300 + stage(i)); };
                 AttnItem m;
                 for (int k = 0; items.take<false>(wctx2, k, m); ++k) {
-                    const int n = tiles_of(m);
+                    const AttnPart own = part_of(m);
+                    const int n = own.n;
+                    if (SPLIT && n == 0) continue;
                     const uint32_t kpar = static_cast<uint32_t>(k) & 1u;
                     auto scores = [&](int j) {
                         if (!ready(2 * j)) return false;
@@ -256,7 +263,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                         if (j + 1 < n) ok = grads(j + 1);
                         if (!ok) break;
                         const uint32_t ds = tmem + ((done + j) & 1) * ROWS;
-                        const int steps = (min(ROWS, m.len - j * ROWS) + 15) / 16;
+                        const int steps = (min(ROWS, m.len - (own.first + j) * ROWS) + 15) / 16;
                         attn_mma_tn<WGS == 2, ROWS>(dq_tm, ds, tile(2 * j), idesc_q, steps, j > 0);
                         attn_mma_tn<WGS == 2, ROWS>(dq_tm, ds + 32, tile(2 * j), idesc_q, steps, true);  // what the roundings left out
                         ptx::umma_commit<1>(empty_bar(stage(2 * j)));
@@ -297,11 +304,15 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             l = row0 + lane < m.len ? __ldcg(p.lse + static_cast<long long>(m.head) * p.T + m.start + row0 + lane) : 0.0f;
         };
         uint32_t done = 0;  // tiles before this item
-        AttnItem m;
+        AttnItem m, shared{0, 0, -1, 0};
+        bool sums = false;  // of a shared item are there
         bool more = items.take<true>(wctx2, 0, m);
         if (more) fetch(m);
         for (int k = 0; more; ++k) {
-            const int n = tiles_of(m);
+            const AttnPart own = part_of(m);
+            const int n = own.n;
+            if (SPLIT) shared = m;
+            if (SPLIT && n == 0) break;
             const int row = m.block * 128 + q * 32 + lane;  // of the sequence
             const long long at = m.start + row;
             float delta = 0.0f;
@@ -325,7 +336,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(own_bar);  // this warp has read the item's tile
                 if (row >= m.len) delta = 0.0f;  // dout may hold anything there
-                else if (half == 0 && !b.side) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
+                else if (half == 0 && !b.side && (!SPLIT || own.first == 0)) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
             }
             const ptx::f2 base = ptx::make_f2(nl, nl), nd2 = ptx::make_f2(-delta, -delta);
             // keys that all rows of the warp see, that this one sees
@@ -359,8 +370,8 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                         const ptx::f2 ds = ptx::mul2(ptx::add2(ptx::make_f2_bits(g[c][i], g[c][i + 1]), nd2), ptx::make_f2_bits(s[c][i], s[c][i + 1]));
                         split_bf16x2(ds, hi[c * 16 + (i >> 1)], lo[c * 16 + (i >> 1)]);
                     }
-                if (seen_by_all - j * ROWS - half * 64 < 64) {  // columns that are not seen may hold anything
-                    const int limit = seen - j * ROWS - half * 64;
+                if (seen_by_all - (own.first + j) * ROWS - half * 64 < 64) {  // columns that are not seen may hold anything
+                    const int limit = seen - (own.first + j) * ROWS - half * 64;
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         const uint32_t keep = 2 * i + 1 < limit ? 0xffffffffu : 2 * i < limit ? 0xffffu : 0u;
@@ -383,12 +394,34 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             done += n;
             ptx::tc_fence_after();
             constexpr int W = D / WGS;  // columns of a thread
+            if (SPLIT) {
+                sums = true;
+                break;
+            }
             attn_store_row<W>(dq_tm + lanes + half * W, p.scale, static_cast<__nv_bfloat16 *>(b.dq) + at * b.ld_dq + m.head * p.D + half * W, row < m.len,
                               p.D - half * W, wide);
             ptx::tc_fence_before();
             m = next;
         }
         ptx::tc_fence_before();
+        if (SPLIT) {
+            const AttnShare c(p.parts);
+            ptx::cluster_sync();  // all blocks' products are done: their tiles' memory is free
+            if (sums) attn_give_row<D / WGS, D>(c, dq_tm + lanes + half * (D / WGS), smem, q * 32 + lane, half * (D / WGS));
+            const bool failed = c.failed(abort_addr);
+            ptx::cluster_sync();
+            if (shared.block >= 0 && !failed) {
+                const int row0 = shared.block * 128;
+                attn_join_rows<D, 128 * WGS>(c, smem, attn_sharers<LEAST>(p.parts, tiles_of(shared)),
+                                             static_cast<__nv_bfloat16 *>(b.dq) + (shared.start + row0) * b.ld_dq + shared.head * p.D, b.ld_dq,
+                                             min(128, shared.len - row0), p.D, [&](int, int) { return p.scale; });
+            }
+        }
+    }
+    if (SPLIT && (!smem_ok || warp >= LOAD)) {
+        __syncwarp();
+        ptx::cluster_sync();
+        ptx::cluster_sync();
     }
 
     // ---------------------------------------------------------------- common exit
@@ -406,12 +439,12 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
 }
 
 // ------------------------------------------------------------------------------------------------ dK, dV
-template <class Cfg>
+template <class Cfg, bool SPLIT>
 __global__ void __launch_bounds__(Cfg::THREADS, Cfg::BLOCKS)
 attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDO, const __grid_constant__ CUtensorMap tmK,
    const __grid_constant__ CUtensorMap tmV, const AttnBackward b)
 {
-    constexpr int D = Cfg::D, WGS = Cfg::WGS, ROWS = Cfg::ROWS, STAGES = Cfg::STAGES, LOAD = 4 * WGS, MMA = LOAD + 1;
+    constexpr int D = Cfg::D, WGS = Cfg::WGS, ROWS = Cfg::ROWS, STAGES = Cfg::STAGES, LOAD = 4 * WGS, MMA = LOAD + 1, LEAST = 2;
     const AttnParams &p = b.a;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem = ptx::smem_u32(smem_raw);
@@ -471,6 +504,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     // tiles of queries that see an item's keys: from first_of on, per head
     auto first_of = [&](const AttnItem &m) { return p.causal ? m.block * (128 / ROWS) : 0; };
     auto tiles_of = [&](const AttnItem &m) { return (m.len + ROWS - 1) / ROWS - first_of(m); };
+    auto part_of = [&](const AttnItem &m) { return attn_part<SPLIT, LEAST>(p.parts, tiles_of(m) * p.group); };  // this block's, of all heads' tiles
 
     if (!smem_ok) {
         // nothing to do
@@ -483,27 +517,28 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             uint32_t phase = 0, parts = 0, asked = 0;
             AttnOrder order;
             order.load(p);
-            for (int k = 0, at = static_cast<int>(blockIdx.x); ok;) {
+            for (int k = 0, at = static_cast<int>(SPLIT ? blockIdx.x / p.parts : blockIdx.x); ok;) {
                 AttnItem m{0, 0, -1, 0};
                 if (at >= 0) {
                     const AttnSpan s = order.item(p, at / kv_heads, true);
                     m = {s.start, s.len, s.block, at % kv_heads};
                 }
-                if (at < 0 || m.block >= 0) {  // slots without a block are passed over
+                if (SPLIT || at < 0 || m.block >= 0) {  // slots without a block are passed over
                     ok = items.put(wctx2, k, m);
-                    if (!ok || at < 0) break;
+                    if (!ok || m.block < 0) break;
                     ok = warp_wait(wctx2, own_bar, (static_cast<uint32_t>(k) & 1u) ^ 1u, 130);
                     if (!ok) break;
-                    if (ptx::elect_one()) {
+                    const int first = first_of(m), per_head = tiles_of(m);
+                    const AttnPart own = part_of(m);
+                    if (own.n > 0 && ptx::elect_one()) {
                         ptx::mbar_expect_tx(k_bar, Cfg::OWN);
                         attn_load<D>(smem + Cfg::OFF_OWN, &tmK, k_bar, m.head, m.start + m.block * 128);
                         ptx::mbar_expect_tx(v_bar, Cfg::OWN);
                         attn_load<D>(smem + Cfg::OFF_OWN + Cfg::OWN, &tmV, v_bar, m.head, m.start + m.block * 128);
                     }
                     __syncwarp();
-                    const int first = first_of(m), per_head = tiles_of(m);
-                    int t = 0, head = m.head * p.group;
-                    for (int i = 0; i < 2 * per_head * p.group && ok; ++i) {
+                    int t = own.first % per_head, head = m.head * p.group + own.first / per_head;
+                    for (int i = 0; i < 2 * own.n && ok; ++i) {
                         ok = warp_wait(wctx2, empty_bar(stage), phase ^ 1u, 100 + stage);
                         if (!ok) break;
                         const uint32_t dst = smem + Cfg::OFF_RING + stage * Cfg::TILE;
@@ -535,7 +570,8 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                     if (!ok) break;
                     ++k;
                 }
-                ok = items.next(wctx2, asked, at);
+                if (SPLIT) at = -1;
+                else ok = items.next(wctx2, asked, at);
             }
         } else if (warp == MMA) {
             // ------------------------------------------------------------ products
@@ -550,7 +586,10 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 auto ready = [&](uint32_t i) { return wait_barrier(wctx, full_bar(stage(i)), ((2 * done + i) / STAGES) & 1u, 300 + stage(i)); };
                 AttnItem m;
                 for (int k = 0; items.take<false>(wctx2, k, m); ++k) {
-                    const int first = first_of(m), per_head = tiles_of(m), n = per_head * p.group;
+                    const int first = first_of(m), per_head = tiles_of(m);
+                    const AttnPart own = part_of(m);
+                    const int n = own.n;
+                    if (SPLIT && n == 0) continue;
                     const uint32_t kpar = static_cast<uint32_t>(k) & 1u;
                     auto scores = [&](int i) {
                         if (!ready(2 * i)) return false;
@@ -568,7 +607,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                         return true;
                     };
                     bool ok = wait_barrier(wctx, k_bar, kpar, 330) && scores(0) && wait_barrier(wctx, v_bar, kpar, 331) && grads(0);
-                    int t = 0;
+                    int t = own.first % per_head;
                     for (int i = 0; i < n && ok; ++i) {
                         const int steps = (min(ROWS, m.len - (first + t) * ROWS) + 15) / 16;
                         ok = wait_barrier(wctx2, p_bar, (done + i) & 1u, 350);
@@ -599,8 +638,9 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             for (int k = 0; items.take<true>(wctx2, k, m); ++k) {
                 const int first = first_of(m), per_head = tiles_of(m);
                 bool ok = true;
-                int t = 0, head = m.head * p.group;
-                for (int i = 0; i < per_head * p.group && ok; ++i, ++r) {
+                const AttnPart own = part_of(m);
+                int t = own.first % per_head, head = m.head * p.group + own.first / per_head;
+                for (int i = 0; i < own.n && ok; ++i, ++r) {
                     const long long at = static_cast<long long>(head) * p.T + m.start + (first + t) * ROWS;
                     float l[ROWS / 32], d[ROWS / 32];
 #pragma unroll
@@ -638,11 +678,16 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         const float sl = p.scale * kLog2e;
         const ptx::f2 sl2 = ptx::make_f2(sl, sl);
         uint32_t it = 0;  // tiles so far
-        AttnItem m;
+        AttnItem m, shared{0, 0, -1, 0};
+        bool sums = false;  // of a shared item are there
         for (int k = 0; items.take<true>(wctx2, k, m); ++k) {
-            const int first = first_of(m), per_head = tiles_of(m), n = per_head * p.group;
+            const int first = first_of(m), per_head = tiles_of(m);
+            const AttnPart own = part_of(m);
+            const int n = own.n;
+            if (SPLIT) shared = m;
+            if (SPLIT && n == 0) continue;
             bool ok = true;
-            int t = 0;
+            int t = own.first % per_head;
             for (int i = 0; i < n; ++i, ++it) {
                 const uint32_t par = it & 1u;
                 const uint32_t rows = smem + Cfg::OFF_ROWS + par * 1024 + half * 256;
@@ -722,6 +767,10 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             if (ok) ok = warp_wait(wctx2, done_bar, static_cast<uint32_t>(k) & 1u, 420);
             if (!ok) break;
             ptx::tc_fence_after();
+            if (SPLIT) {
+                sums = true;
+                break;
+            }
             const int row = m.block * 128 + r;
             const long long at = m.start + row;
             if (WGS == 1 || half == 0)
@@ -733,6 +782,28 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             ptx::tc_fence_before();
         }
         ptx::tc_fence_before();
+        if (SPLIT) {
+            const AttnShare c(p.parts);
+            const uint32_t of_dk = smem + 128 * D * 4;
+            ptx::cluster_sync();  // all blocks' products are done: their tiles' memory is free
+            if (sums && (WGS == 1 || half == 0)) attn_give_row<D, D>(c, dv_tm + lanes, smem, r, 0);
+            if (sums && (WGS == 1 || half == 1)) attn_give_row<D, D>(c, dk_tm + lanes, of_dk, r, 0);
+            const bool failed = c.failed(abort_addr);
+            ptx::cluster_sync();
+            if (shared.block >= 0 && !failed) {
+                const int row0 = shared.block * 128, sharers = attn_sharers<LEAST>(p.parts, tiles_of(shared) * p.group), rows = min(128, shared.len - row0);
+                const long long at = shared.start + row0;
+                attn_join_rows<D, 128 * WGS>(c, smem, sharers, static_cast<__nv_bfloat16 *>(b.dv) + at * b.ld_dv + shared.head * p.D, b.ld_dv, rows, p.D,
+                                             [](int, int) { return 1.0f; });
+                attn_join_rows<D, 128 * WGS>(c, of_dk, sharers, static_cast<__nv_bfloat16 *>(b.dk) + at * b.ld_dk + shared.head * p.D, b.ld_dk, rows, p.D,
+                                             [&](int, int) { return p.scale; });
+            }
+        }
+    }
+    if (SPLIT && (!smem_ok || warp >= LOAD)) {
+        __syncwarp();
+        ptx::cluster_sync();
+        ptx::cluster_sync();
     }
 
     // ---------------------------------------------------------------- common exit

@@ -13,6 +13,9 @@
 // products: 2 to 3 us). So a block that is done with its item takes another off the grid (the hardware hands out blocks that have not
 // started), asks for it when its own loads are on their way, and its loads and first scores come while the last output is still being stored.
 //
+// Few items with many keys are shared (SPLIT): the blocks of a cluster have a part of the keys each, with a maximum and a sum of its own, and every block joins an equal share of the
+// rows from what the others write into its shared memory, the parts in their order. That costs 4 us, and halves a long item (nb_linear.cu has what it measured).
+//
 // The output accumulator in tensor memory is rescaled only when a row's maximum has grown by more than 2^8 since the last
 // rescaling: until then probabilities up to 2^8 are summed against the old maximum, which changes no bit of their relative precision.
 // Probabilities are rounded to bf16 for the tensor core (half an ulp, 2^-8 of each at most); their sum takes them unrounded.
@@ -37,14 +40,15 @@ struct AttnFwdCfg {
     static constexpr int REGS_ROWS = 192, REGS_OTHER = 64;
     static_assert(REGS_ROWS + REGS_OTHER <= 2 * 128, "registers");
     static_assert(TMEM >= TM_O + D_ && STAGES >= 4 && SMEM <= MOST, "memory");
+    static_assert(128 * D_ * 4 + 1024 <= OFF_BAR, "a part's sums, maxima");
 };
 
-template <class Cfg>
+template <class Cfg, bool SPLIT>
 __global__ void __launch_bounds__(Cfg::THREADS, Cfg::BLOCKS)
 attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                     const AttnParams p)
 {
-    constexpr int D = Cfg::D, KEYS = Cfg::KEYS, STAGES = Cfg::STAGES, LOAD = 4, MMA = 5;
+    constexpr int D = Cfg::D, KEYS = Cfg::KEYS, STAGES = Cfg::STAGES, LOAD = 4, MMA = 5, LEAST = 4;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem = ptx::smem_u32(smem_raw);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
@@ -74,6 +78,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const int tiles = (m.len + KEYS - 1) / KEYS;
         return p.causal ? min(tiles, (m.block + 1) * (128 / KEYS)) : tiles;
     };
+    auto part_of = [&](const AttnItem &m) { return attn_part<SPLIT, LEAST>(p.parts, tiles_of(m)); };  // this block's
 
     if (warp == LOAD) {
         if (lane < STAGES) {
@@ -117,18 +122,19 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             uint32_t phase = 0, parts = 0, asked = 0, used = 0;
             AttnOrder order;
             order.load(p);
-            for (int k = 0, at = static_cast<int>(blockIdx.x); ok;) {
+            for (int k = 0, at = static_cast<int>(SPLIT ? blockIdx.x / p.parts : blockIdx.x); ok;) {
                 AttnItem m{0, 0, -1, 0};
                 if (at >= 0) {
                     const AttnSpan s = order.item(p, at / p.heads, false);
                     m = {s.start, s.len, s.block, at % p.heads};
                 }
-                if (at < 0 || m.block >= 0) {  // slots without a block are passed over
+                if (SPLIT || at < 0 || m.block >= 0) {  // slots without a block are passed over
                     ok = items.put(wctx2, k++, m);
-                    if (!ok || at < 0) break;
-                    const int n = tiles_of(m), kv_head = m.head / p.group;
-                    for (int i = 0; i < 2 * n && ok; ++i) {
-                        const int j = i >> 1;
+                    if (!ok || m.block < 0) break;
+                    const AttnPart own = part_of(m);
+                    const int kv_head = m.head / p.group;
+                    for (int i = 0; i < 2 * own.n && ok; ++i) {
+                        const int j = own.first + (i >> 1);
                         ok = warp_wait(wctx2, empty_bar(stage), phase ^ 1u, 100 + stage);
                         if (!ok) break;
                         const uint32_t dst = smem + Cfg::OFF_KV + stage * Cfg::TILE;
@@ -163,7 +169,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     }
                     if (!ok) break;
                 }
-                ok = items.next(wctx2, asked, at);
+                if (SPLIT) at = -1;
+                else ok = items.next(wctx2, asked, at);
             }
         } else if (warp == MMA) {
             // ------------------------------------------------------------ products
@@ -177,7 +184,9 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 auto ready = [&](uint32_t i) { return wait_barrier(wctx, full_bar(stage(i)), ((2 * done + i) / STAGES) & 1u, 300 + stage(i)); };
                 AttnItem m;
                 for (int k = 0; items.take<false>(wctx2, k, m); ++k) {
-                    const int n = tiles_of(m);
+                    const AttnPart own = part_of(m);
+                    const int n = own.n;
+                    if (SPLIT && n == 0) continue;
                     auto scores = [&](int j) {
                         if (!ready(2 * j)) return false;
                         ptx::tc_fence_after();
@@ -194,7 +203,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         if (!ok) break;
                         ptx::tc_fence_after();
                         attn_mma_tn<false, KEYS>(tmem + Cfg::TM_O, tmem + ((done + j) & 1) * KEYS, tile(2 * j + 1), idesc_o,
-                                                 (min(KEYS, m.len - j * KEYS) + 15) / 16, j > 0);
+                                                 (min(KEYS, m.len - (own.first + j) * KEYS) + 15) / 16, j > 0);
                         ptx::umma_commit<1>(o_bar(done + j));
                         ptx::umma_commit<1>(empty_bar(stage(2 * j + 1)));
                     }
@@ -214,14 +223,19 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const ptx::f2 sl2 = ptx::make_f2(sl, sl);
         const bool wide = attn_wide(p.out, p.ld_out, p.D);
         uint32_t done = 0;  // tiles before this item
-        AttnItem m;
+        AttnItem m, shared{0, 0, -1, 0};
+        bool sums = false;  // of a shared item are there
+        float top = 0.0f, total = 0.0f;  // the maximum that the sums refer to (of unscaled scores), the sum
         for (int k = 0; items.take<true>(wctx2, k, m); ++k) {
-            const int n = tiles_of(m);
+            const AttnPart own = part_of(m);
+            const int n = own.n;
+            if (SPLIT) shared = m;
+            if (SPLIT && n == 0) continue;
             const int first = m.block * 128 + warp * 32, row = first + lane;  // of the sequence
             // keys that some row of the warp sees, all of them, this one
             const int seen_by_one = min(m.len, p.causal ? first + 32 : m.len), seen_by_all = min(m.len, p.causal ? first + 1 : m.len),
                       seen = min(m.len, p.causal ? row + 1 : m.len);
-            float top = 0.0f, total = 0.0f;  // the maximum that the sums refer to (of unscaled scores), the sum
+            total = 0.0f;
             bool ok = true;
             for (int j = 0; j < n; ++j) {
                 const uint32_t r = done + j, s_tm = tm + (r & 1) * KEYS;
@@ -230,9 +244,9 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 ptx::tc_fence_after();
                 uint32_t s[2][32];
                 ptx::tmem_ld_32x32_x2_wait(s_tm, s_tm + 32, s[0], s[1]);
-                const int one = seen_by_one - j * KEYS;
-                if (seen_by_all - j * KEYS < KEYS) {
-                    const int limit = seen - j * KEYS;
+                const int key = (own.first + j) * KEYS, one = seen_by_one - key;
+                if (seen_by_all - key < KEYS) {
+                    const int limit = seen - key;
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -301,11 +315,63 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             if (!ok) break;
             done += n;
             ptx::tc_fence_after();
+            if (SPLIT) {
+                sums = true;
+                break;
+            }
             attn_store_row<D>(o_tm, 1.0f / total, static_cast<__nv_bfloat16 *>(p.out) + (m.start + row) * p.ld_out + m.head * p.D, row < m.len, p.D, wide);
             if (p.lse && row < m.len) p.lse[static_cast<long long>(m.head) * p.T + m.start + row] = top * p.scale + logf(total);
             ptx::tc_fence_before();
         }
         ptx::tc_fence_before();
+        if (SPLIT) {
+            const AttnShare c(p.parts);
+            const uint32_t stats = smem + Cfg::OFF_BAR - 1024;  // maximum and sum, in the rows' order
+            ptx::cluster_sync();  // all blocks' products are done: their tiles' memory is free
+            if (sums) {
+                const int row = warp * 32 + lane;
+                attn_give_row<D, D>(c, o_tm, smem, row, 0);
+                ptx::st_cluster_v2(ptx::mapa(stats + c.slot(c.rank, row) * 8, c.owner(row)), __float_as_uint(top), __float_as_uint(total));
+            }
+            const bool failed = c.failed(abort_addr);
+            ptx::cluster_sync();
+            if (shared.block >= 0 && !failed) {
+                const int sharers = attn_sharers<LEAST>(p.parts, tiles_of(shared)), row0 = shared.block * 128;
+                const int rows = min(128, shared.len - row0), tid = static_cast<int>(threadIdx.x);
+                const long long at = shared.start + row0;
+                // weights: a part's sums refer to its own maximum. Of a row with nothing but infinities they are 0 / 0, as its result is without parts
+                if (tid < c.rows) {
+                    const int row = c.rank * c.rows + tid;
+                    float2 v[kAttnParts];
+                    float all = -INFINITY, sum = 0.0f;
+#pragma unroll
+                    for (int q = 0; q < kAttnParts; ++q)
+                        if (q < sharers) {
+                            v[q] = make_float2(ptx::ld_shared_f32(stats + c.slot(q, row) * 8), ptx::ld_shared_f32(stats + c.slot(q, row) * 8 + 4));
+                            all = fmaxf(all, v[q].x);
+                        }
+#pragma unroll
+                    for (int q = 0; q < kAttnParts; ++q)
+                        if (q < sharers) {
+                            const float w = v[q].x == -INFINITY ? 0.0f : ptx::ex2_approx((v[q].x - all) * sl);
+                            sum += w * v[q].y;
+                            v[q].x = w;
+                        }
+#pragma unroll
+                    for (int q = 0; q < kAttnParts; ++q)
+                        if (q < sharers) ptx::st_shared_f32(stats + c.slot(q, row) * 8, v[q].x / sum);
+                    if (p.lse && row < rows) p.lse[static_cast<long long>(shared.head) * p.T + at + row] = all * p.scale + logf(sum);
+                }
+                ptx::named_bar_sync(3, 128);
+                attn_join_rows<D, 128>(c, smem, sharers, static_cast<__nv_bfloat16 *>(p.out) + at * p.ld_out + shared.head * p.D, p.ld_out, rows, p.D,
+                                       [&](int q, int row) { return ptx::ld_shared_f32(stats + c.slot(q, row) * 8); });
+            }
+        }
+    }
+    if (SPLIT && (!smem_ok || warp >= LOAD)) {
+        __syncwarp();
+        ptx::cluster_sync();
+        ptx::cluster_sync();
     }
 
     // ---------------------------------------------------------------- common exit

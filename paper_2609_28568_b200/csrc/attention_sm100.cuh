@@ -194,6 +194,83 @@ struct AttnItems {
     }
 };
 
+// ---------------------------------------------------------------- items that a cluster of blocks shares
+// The tiles that a block walks over for an item: n from the first-th on. Of a cluster's blocks as many take part as have LEAST of them each.
+struct AttnPart {
+    int first, n;
+};
+template <int LEAST>
+__device__ __forceinline__ int attn_sharers(int parts, int tiles)
+{
+    return max(1, min(parts, tiles / LEAST));
+}
+template <bool SPLIT, int LEAST>
+__device__ __forceinline__ AttnPart attn_part(int parts, int tiles)
+{
+    if (!SPLIT) return {0, tiles};
+    const int sharers = attn_sharers<LEAST>(parts, tiles), i = static_cast<int>(ptx::cluster_ctarank());
+    if (i >= sharers) return {0, 0};
+    const int first = static_cast<int>(static_cast<long long>(tiles) * i / sharers);
+    return {first, static_cast<int>(static_cast<long long>(tiles) * (i + 1) / sharers) - first};
+}
+// The sums of an item's blocks are joined by all blocks of the cluster (a power of two of them): a block owns 128 / parts of the item's rows and takes its cluster's sums of these,
+// written by the others into its shared memory as `parts` groups of that many rows, [128][D] fp32. Pieces of 16 bytes change places so that eight rows meet no bank twice.
+constexpr int kAttnParts = 8;  // blocks of a cluster, at most
+struct AttnShare {
+    int parts, rank, rows;  // of the cluster; this block; that a block owns
+    __device__ __forceinline__ explicit AttnShare(int n) : parts(n), rank(static_cast<int>(ptx::cluster_ctarank())), rows(128 / n) {}
+    __device__ __forceinline__ uint32_t owner(int row) const { return static_cast<uint32_t>(row / rows); }
+    __device__ __forceinline__ int slot(int part, int row) const { return part * rows + row % rows; }
+    // whether a wait has run out in a block of the cluster, by a whole warp, when all their waits are over
+    __device__ __forceinline__ bool failed(uint32_t abort_addr) const
+    {
+        const int lane = static_cast<int>(threadIdx.x & 31);
+        return __any_sync(0xffffffffu, lane < parts && ptx::ld_cluster_u32_volatile(ptx::mapa(abort_addr, static_cast<uint32_t>(min(lane, parts - 1)))) != 0);
+    }
+};
+// W columns of a row per lane, from column col on, from the fp32 accumulator at `acc` to the row's owner
+template <int W, int D>
+__device__ __forceinline__ void attn_give_row(const AttnShare &c, uint32_t acc, uint32_t sums, int row, int col)
+{
+    const int slot = c.slot(c.rank, row);
+    const uint32_t to = ptx::mapa(sums + slot * (D * 4), c.owner(row));
+#pragma unroll
+    for (int k = 0; k < W; k += 32) {
+        uint32_t o[32];
+        __syncwarp();
+        ptx::tmem_ld_32x32_wait(acc + k, o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            ptx::st_cluster_v4(to + ((((col + k) / 4 + i) ^ (slot & 7)) << 4), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+    }
+    __syncwarp();
+}
+// The block's own rows (of `rows` of the item): the sums of the cluster's first `sharers` blocks, weighed, added in their order and written as bf16 by THREADS threads.
+// weight(part, row): of a part's sums
+template <int D, int THREADS, class Weight>
+__device__ __forceinline__ void attn_join_rows(const AttnShare &c, uint32_t sums, int sharers, __nv_bfloat16 *dst, long long ld, int rows, int cols, const Weight &weight)
+{
+    constexpr int PIECES = D / 8;  // of a row: eight columns each
+    const int row0 = c.rank * c.rows;
+    for (int i = static_cast<int>(threadIdx.x); i < c.rows * PIECES; i += THREADS) {
+        const int row = row0 + i / PIECES, piece = i % PIECES;
+        if (row >= rows || piece * 8 >= cols) continue;
+        float o[8] = {};
+        for (int q = 0; q < sharers; ++q) {
+            const int slot = c.slot(q, row);
+            const float w = weight(q, row);
+            float4 a, b;
+            ptx::ld_shared_f32x4(sums + slot * (D * 4) + (((2 * piece) ^ (slot & 7)) << 4), a);
+            ptx::ld_shared_f32x4(sums + slot * (D * 4) + (((2 * piece + 1) ^ (slot & 7)) << 4), b);
+            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(w, v[e], o[e]);
+        }
+        *reinterpret_cast<uint4 *>(dst + row * ld + piece * 8) =
+            make_uint4(ptx::pack_bf16x2(o[0], o[1]), ptx::pack_bf16x2(o[2], o[3]), ptx::pack_bf16x2(o[4], o[5]), ptx::pack_bf16x2(o[6], o[7]));
+    }
+}
+
 // A tile of ROWS rows, in boxes of 64 columns, from row `row` on.
 template <int D, int ROWS = 128>
 __device__ __forceinline__ void attn_load(uint32_t dst, const CUtensorMap *m, uint32_t bar, int head, int row)

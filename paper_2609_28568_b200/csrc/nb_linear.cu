@@ -2218,6 +2218,7 @@ AttnParams attn_params(const DeviceState &s, int64_t T, int64_t n, int64_t heads
     p.scale = scale;
     p.status = s.status;
     p.timeout_ns = kDefaultTimeoutNs;
+    p.parts = 1;
     return p;
 }
 
@@ -2227,6 +2228,15 @@ int64_t attn_slots(const AttnParams &p, int rows)
     if (p.cu) return p.T / rows + p.n;
     const int64_t len = p.T / p.n;
     return p.n * ((len + rows - 1) / rows);
+}
+
+// Blocks that share an item: a power of two with which all items have no more than `most` and an item of so many tiles leaves `least` to each. A cluster of blocks costs a
+// start and a join of some us, and does without the items that blocks take off the grid: it is for passes with fewer items than SMs, whose time is the longest item's.
+int attn_parts(int64_t items, int64_t tiles, int64_t most, int64_t least)
+{
+    int parts = 8;
+    while (parts > 1 && (items * parts > most || parts * least > tiles)) parts /= 2;
+    return parts;
 }
 
 // Launches an attention kernel on the sequences' blocks for each of `heads` heads.
@@ -2258,18 +2268,25 @@ int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtenso
         NB_CUDA(cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem)));
         attr_set[dev] = true;
     }
-    const int64_t slots = attn_slots(a, k.rows);
-    if (slots * heads >= (1ll << 31)) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
+    const int64_t blocks = attn_slots(a, k.rows) * heads * a.parts;
+    if (blocks >= (1ll << 31)) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(slots * heads));
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(static_cast<unsigned>(k.threads));
     cfg.dynamicSmemBytes = k.smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = dependent_launch_allowed(stream) ? 1 : 0;
+    cudaLaunchAttribute attr[2];
+    if (a.parts > 1) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = static_cast<unsigned>(a.parts);
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.numAttrs = 1;
+    }
+    if (dependent_launch_allowed(stream)) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    cfg.attrs = attr;
     void *args[MAPS + 1];
     for (int i = 0; i < MAPS; ++i) args[i] = &maps[i];
     args[MAPS] = &p;
@@ -3084,13 +3101,20 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
     p.ld_out = ld_out;
     p.out = out;
     p.lse = static_cast<float *>(lse);
-    const AttnKernel kernel = attn_forward(p.D);
+    // Blocks to an item, in us with 1, 2, 4 and 8 of them, causal: 1000 x 4 heads of 64 14, 14, 14, 14; 1000 x 12 16, 15, 23, 37; 2000 x 4 24, 20, 17, 28; 2000 x 8 26, 23, 29, 53;
+    // 2000 x 16 of 128 34, 39, 70, 130; 3000 x 4 34, 27, 29, 43; 3000 x 8 41, 31, 47, 84; 4096 x 4 49, 35, 35, 61; 4096 x 8 56, 43, 67, 115; 4096 x 12 57, 64, 97, 171;
+    // 8192 x 2 90, 59, 47, 76; 8192 x 4 of 128 110, 74, 110, 180; 16384 x 1 of 128 191, 120, 83, 122; whole: 2000 x 1 of 128 25, 21, 18, 19; 2000 x 4 30, 23, 18, 36;
+    // 2000 x 12 34, 40, 49, 88; 4096 x 2 of 128 56, 40, 31, 55. (Of a causal mask's items half are short.)
+    const int64_t items = attn_slots(p, 128) * heads, tiles = T / n / 64 + 1;
+    p.parts = attn_parts(items, tiles, 2ll * s->num_sms, 6);
+    if (causal) p.parts = std::max(p.parts, attn_parts(items, tiles, 4ll * s->num_sms, 20));
+    const AttnKernel kernel = attn_forward(p.D, p.parts > 1);
     CUtensorMap maps[3];
     if ((rc = get_heads_tmap(*s, &maps[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &maps[1], k, T, D, kv_heads, ld_k, kernel.streamed)) != NB_OK ||
         (rc = get_heads_tmap(*s, &maps[2], v, T, D, kv_heads, ld_v, kernel.streamed)) != NB_OK)
         return rc;
-    static bool attr_set[2][kMaxDevices] = {};
-    return launch_attention(kernel, attr_set[D > 64], maps, p, p, heads, static_cast<cudaStream_t>(stream_));
+    static bool attr_set[4][kMaxDevices] = {};
+    return launch_attention(kernel, attr_set[2 * (p.parts > 1) + (D > 64)], maps, p, p, heads, static_cast<cudaStream_t>(stream_));
 }
 
 int64_t nb_attention_workspace(int64_t T, int64_t heads)
@@ -3148,7 +3172,13 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
     // more than half the time, which counts where the longest one does (both passes, in us, two blocks / one: 500 x 12 heads 32 / 23, 1000 x 12 54 / 35,
     // 2000 x 12 98 / 57, 3000 x 16 134 / 117; 4 x 1024 x 12, 384 items: 58 / 57, 8 x 1024: 99 / 104, 16 x 1024: 176 / 187).
     auto few = [&](int64_t h) { return slots * h <= 3ll * s->num_sms; };
-    const AttnKernel of_q = attn_backward_q(b.a.D, few(heads)), of_kv = attn_backward_kv(b.a.D, few(kv_heads));
+    // Blocks to an item, measured on both passes, in us (dq's, dk and dv's): 4096 x 2 heads on 1 of 128: 118 (1, 1), 73 (1, 4), 59 (2, 4); 1000 x 8 on 1 of 64: 109 (1, 1),
+    // 39 (1, 4), 27 (1, 8), 35 (2, 8); 4096 x 8 on 1: 445 (1, 1), 156 (1, 4), 136 (1, 8); 4096 x 16 on 2 of 128: 560 (1, 1), 254 (1, 4), 312 (1, 8); 8 x 1024 x 16 on 2: 210
+    // (1, 1), 174 (1, 2), 208 (1, 4); 8 x 1024 x 16 on 4: 157 (1, 1), 199 (1, 2); 310 x 4 on 1: 28 (1, 1), 18 (1, 4); 1000 x 12 on 12 of 64: 28 (1, 1), 33 (1, 2).
+    const int64_t tiles = T / n / 128 + 1;
+    const int pq = attn_parts(slots * heads, tiles, s->num_sms, 8);
+    const int pk = std::max(attn_parts(slots * kv_heads, tiles * b.a.group, s->num_sms, 3), attn_parts(slots * kv_heads, tiles * b.a.group, 2ll * s->num_sms, 16));
+    const AttnKernel of_q = attn_backward_q(b.a.D, few(heads), pq > 1), of_kv = attn_backward_kv(b.a.D, few(kv_heads), pk > 1);
     CUtensorMap mq[4], mkv[4];  // of q, dout, k, v: whole blocks of one pass are streamed by the other
     if ((rc = get_heads_tmap(*s, &mq[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &mq[1], dout, T, D, heads, ld_dout)) != NB_OK ||
         (rc = get_heads_tmap(*s, &mq[2], k, T, D, kv_heads, ld_k, of_q.streamed)) != NB_OK ||
@@ -3157,15 +3187,17 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
         (rc = get_heads_tmap(*s, &mkv[1], dout, T, D, heads, ld_dout, of_kv.streamed)) != NB_OK ||
         (rc = get_heads_tmap(*s, &mkv[2], k, T, D, kv_heads, ld_k)) != NB_OK || (rc = get_heads_tmap(*s, &mkv[3], v, T, D, kv_heads, ld_v)) != NB_OK)
         return rc;
-    static bool attr_set[6][kMaxDevices] = {};
+    static bool attr_set[10][kMaxDevices] = {};
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     // Side by side (a launch more) where the items of both passes together are at most two to an SM, in us, in turn / side by side:
     // 1 x 12 heads of 64: 13 / 11, 500 x 12: 23 / 16, 1000 x 12: 35 / 29, 1000 x 12 of 128: 44 / 33; 8 sequences of 128 x 12, in 384 slots: 16 / 18,
     // 2000 x 12: 57 / 53, 4 x 1024 x 12: 57 / 59, 16 x 1024 x 12: 176 / 186 (the passes get into each other's way in L2 and on an SM).
     b.side = slots * (heads + kv_heads) <= 2ll * s->num_sms;
     if (b.side && (rc = launch_delta(attn_backward_delta(b.a.D), b, stream)) != NB_OK) return rc;
-    if ((rc = launch_attention(of_q, attr_set[D > 64 ? 0 : few(heads) ? 1 : 2], mq, b, b.a, heads, stream)) != NB_OK) return rc;
-    return launch_attention(of_kv, attr_set[D > 64 ? 3 : few(kv_heads) ? 4 : 5], mkv, b, b.a, kv_heads, stream);
+    b.a.parts = pq;
+    if ((rc = launch_attention(of_q, attr_set[pq > 1 ? 6 + (D > 64) : D > 64 ? 0 : few(heads) ? 1 : 2], mq, b, b.a, heads, stream)) != NB_OK) return rc;
+    b.a.parts = pk;
+    return launch_attention(of_kv, attr_set[pk > 1 ? 8 + (D > 64) : D > 64 ? 3 : few(kv_heads) ? 4 : 5], mkv, b, b.a, kv_heads, stream);
 }
 
 int nb_workspace_reserve(int64_t bytes)
@@ -3391,17 +3423,20 @@ int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us)
         if (!tensors[i]) return fail(NB_ERR_INVALID_ARG, "tensor %d has a NULL pointer", i);
         if (!aligned16(tensors[i])) return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
     }
-    if (pass < 0 || pass > 2) return fail(NB_ERR_INVALID_ARG, "unknown pass %d", pass);
+    const bool split = pass >= 8;  // clusters of two blocks
+    if (split) pass -= 8;
+    if (pass < 0 || pass > 2) return fail(NB_ERR_INVALID_ARG, "unknown pass");
     if (limit_us < 100 || limit_us > 1000000) return fail(NB_ERR_INVALID_ARG, "limit_us must be within [100, 1000000]");
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *s;
     int rc = get_state(&s);
     if (rc != NB_OK) return rc;
-    const int64_t T = 256, D = 64;  // one head, two tiles
+    const int64_t T = split ? 512 : 256, D = 64;  // one head
     AttnBackward b{};
     b.a = attn_params(*s, T, 1, 1, 1, D, nullptr, 0.125f, 1);
     b.a.timeout_ns = static_cast<unsigned long long>(limit_us) * 1000ull;
     b.a.withhold = 16;
+    b.a.parts = split ? 2 : 1;
     b.a.out = tensors[3];
     b.a.lse = static_cast<float *>(tensors[4]);
     b.a.ld_out = b.ld_dout = b.ld_dq = b.ld_dk = b.ld_dv = D;
@@ -3410,7 +3445,7 @@ int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us)
     b.dk = tensors[7];
     b.dv = tensors[8];
     b.delta = static_cast<float *>(tensors[9]);
-    const AttnKernel kernel = pass == 0 ? attn_forward(D) : pass == 1 ? attn_backward_q(D, false) : attn_backward_kv(D, false);
+    const AttnKernel kernel = pass == 0 ? attn_forward(D, split) : pass == 1 ? attn_backward_q(D, false, split) : attn_backward_kv(D, false, split);
     const uint32_t own = 128, streamed = static_cast<uint32_t>(kernel.streamed);
     CUtensorMap q, k, v, dout;
     if ((rc = get_heads_tmap(*s, &q, tensors[0], T, D, 1, D, pass == 2 ? streamed : own)) != NB_OK ||
@@ -3418,13 +3453,13 @@ int nb_debug_attention_timeout(void *const *tensors, int pass, int64_t limit_us)
         (rc = get_heads_tmap(*s, &v, tensors[2], T, D, 1, D, pass == 2 ? own : streamed)) != NB_OK ||
         (rc = get_heads_tmap(*s, &dout, tensors[5], T, D, 1, D, pass == 2 ? streamed : own)) != NB_OK)
         return rc;
-    static bool attr_set[3][kMaxDevices] = {};
+    static bool attr_set[6][kMaxDevices] = {};
     if (pass == 0) {
         CUtensorMap maps[3] = {q, k, v};
-        return launch_attention(kernel, attr_set[0], maps, b.a, b.a, 1, g_stream);
+        return launch_attention(kernel, attr_set[3 * split], maps, b.a, b.a, 1, g_stream);
     }
     CUtensorMap maps[4] = {q, dout, k, v};
-    return launch_attention(kernel, attr_set[pass], maps, b, b.a, 1, g_stream);
+    return launch_attention(kernel, attr_set[3 * split + pass], maps, b, b.a, 1, g_stream);
 }
 
 int nb_debug_muon_timeout(void *update, const void *grad, void *workspace, int64_t workspace_bytes, int64_t limit_us)
