@@ -2234,7 +2234,7 @@ int64_t attn_slots(const AttnParams &p, int rows)
 // start and a join of some us, and does without the items that blocks take off the grid: it is for passes with fewer items than SMs, whose time is the longest item's.
 int attn_parts(int64_t items, int64_t tiles, int64_t most, int64_t least)
 {
-    int parts = 8;
+    int parts = tiles < 8 ? 1 : 8;
     while (parts > 1 && (items * parts > most || parts * least > tiles)) parts /= 2;
     return parts;
 }
@@ -3174,10 +3174,13 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
     auto few = [&](int64_t h) { return slots * h <= 3ll * s->num_sms; };
     // Blocks to an item, measured on both passes, in us (dq's, dk and dv's): 4096 x 2 heads on 1 of 128: 118 (1, 1), 73 (1, 4), 59 (2, 4); 1000 x 8 on 1 of 64: 109 (1, 1),
     // 39 (1, 4), 27 (1, 8), 35 (2, 8); 4096 x 8 on 1: 445 (1, 1), 156 (1, 4), 136 (1, 8); 4096 x 16 on 2 of 128: 560 (1, 1), 254 (1, 4), 312 (1, 8); 8 x 1024 x 16 on 2: 210
-    // (1, 1), 174 (1, 2), 208 (1, 4); 8 x 1024 x 16 on 4: 157 (1, 1), 199 (1, 2); 310 x 4 on 1: 28 (1, 1), 18 (1, 4); 1000 x 12 on 12 of 64: 28 (1, 1), 33 (1, 2).
-    const int64_t tiles = T / n / 128 + 1;
+    // (1, 1), 174 (1, 2), 208 (1, 4); 8 x 1024 x 16 on 4: 157 (1, 1), 199 (1, 2); 310 x 4 on 1: 28 (1, 1), 18 (1, 4); 1000 x 12 on 12 of 64: 28 (1, 1), 33 (1, 2);
+    // 11 x 8 on 1: 19 (1, 2), 16 (1, 4); 66 x 12 on 3: 14 (1, 1), 16 (1, 2).
+    // 2000 x 1 on 1 of 128, whole: 37 (1, 1), 27 (2, 4), 46 (2, 8): clusters of eight wait for SMs that dq has left.
+    const int64_t tiles = T / n / 128 + 1, tiles_kv = tiles * b.a.group, items_kv = slots * kv_heads;
     const int pq = attn_parts(slots * heads, tiles, s->num_sms, 8);
-    const int pk = std::max(attn_parts(slots * kv_heads, tiles * b.a.group, s->num_sms, 3), attn_parts(slots * kv_heads, tiles * b.a.group, 2ll * s->num_sms, 16));
+    const int pk = std::max({attn_parts(items_kv, tiles_kv, s->num_sms - slots * heads * pq, 2), attn_parts(items_kv, tiles_kv, s->num_sms, 3),
+                             attn_parts(items_kv, tiles_kv, 2ll * s->num_sms, 16)});
     const AttnKernel of_q = attn_backward_q(b.a.D, few(heads), pq > 1), of_kv = attn_backward_kv(b.a.D, few(kv_heads), pk > 1);
     CUtensorMap mq[4], mkv[4];  // of q, dout, k, v: whole blocks of one pass are streamed by the other
     if ((rc = get_heads_tmap(*s, &mq[0], q, T, D, heads, ld_q)) != NB_OK || (rc = get_heads_tmap(*s, &mq[1], dout, T, D, heads, ld_dout)) != NB_OK ||
