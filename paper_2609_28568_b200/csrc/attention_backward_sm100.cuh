@@ -11,6 +11,11 @@
 // bf16, the second what the first left out, at the price of a product more in each pass. (With one piece dQ of keys that share half their length
 // was 2.7e-3 off and dK up to 2.6e-3, of which their own rounding to bf16 is 1.7e-3.)
 //
+// What bounds it: of wide heads the products (nine with the second pieces, tensor core busy 49 % in dQ's pass, 64 % in dK and dV's, the latencies from one to the next
+// filling the rest), of narrow ones the latencies of a tile's chain, and that products of 64 columns take as long as ones of 96. Measured, causal, both passes: 16 x 1024
+// rows, 12 heads of 64: 89 + 107 us (328 TFLOP/s of the five products); 23 sequences in 8000 rows, 16 heads of 128 on 8: 124 + 124 us (468); 8192 rows: 0.87 to 1.02 ms
+// (790 TFLOP/s in a burst, 675 under the power cap).
+//
 // A thread has 64 values of a row of a tile: heads of up to 64 columns take tiles of 64 columns with one warpgroup, two blocks to an SM, which fill
 // each other's gaps; wider heads have no tensor memory for that and take tiles of 128 with two warpgroups, as narrow ones do in passes of few items. While these turn dP into dS, the
 // tensor core works on what P was ready for, and the other way round. A block that is done with its item takes another (attention_sm100.cuh), whose tiles

@@ -7,7 +7,8 @@
 // What bounds it are the exponentials (16 a clock and SM) and the latencies of a step (scores, maximum, exponentials, the way back); the two
 // blocks of an SM fill each other's gaps. Two tiles of queries in one block that share keys and values took as long on one long sequence and a fifth longer
 // on packed ones; 128 keys at a time took the same, and more registers. A quarter of the exponentials formed by a polynomial, on the multipliers, saved
-// nothing: those instructions wait in the same line.
+// nothing: those instructions wait in the same line. Measured, causal: 16 x 1024 rows, 12 heads of 64: 55 us (469 TFLOP/s of what is seen, tensor core busy 27 %);
+// 23 sequences in 8000 rows, 16 heads of 128: 70 us (708 TFLOP/s, 49 %); 16384 rows: 0.85 to 1.02 ms (1.29 PFLOP/s in a burst, 1.08 under the power cap).
 //
 // Items differ in work by the length of their sequence and their place in it, and are short beside what a block costs to start (first loads, first
 // products: 2 to 3 us). So a block that is done with its item takes another off the grid (the hardware hands out blocks that have not
