@@ -2239,7 +2239,6 @@ int attn_parts(int64_t items, int64_t tiles, int64_t most, int64_t least)
     return parts;
 }
 
-// Launches an attention kernel on the sequences' blocks for each of `heads` heads.
 // Launches the kernel that forms delta ahead of both passes.
 int launch_delta(const AttnKernel &k, AttnBackward &b, cudaStream_t stream)
 {
@@ -2258,6 +2257,7 @@ int launch_delta(const AttnKernel &k, AttnBackward &b, cudaStream_t stream)
     return NB_OK;
 }
 
+// Launches an attention kernel on the sequences' blocks for each of `heads` heads.
 template <int MAPS, class P>
 int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtensorMap (&maps)[MAPS], P &p, const AttnParams &a, int64_t heads,
                      cudaStream_t stream)
