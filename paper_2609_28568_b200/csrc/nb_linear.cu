@@ -3068,8 +3068,9 @@ int nb_rotary(void *out_q, void *out_k, const void *q, const void *k, const void
     const int tokens = static_cast<int>(want < kRotaryTokens ? want : kRotaryTokens);
     const dim3 grid(static_cast<unsigned>((T + tokens - 1) / tokens));
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    rc = layout == NB_ROTARY_HALF ? launch_chained(rotary_kernel<true>, grid, kRotaryThreads, stream, p, tokens)
-                                  : launch_chained(rotary_kernel<false>, grid, kRotaryThreads, stream, p, tokens);
+    const bool half = layout == NB_ROTARY_HALF, two = (D - R) % 16 == 0 && (half ? R < D : R % 16 == 0);
+    rc = half ? launch_chained(two ? rotary_kernel<true, true> : rotary_kernel<true, false>, grid, kRotaryThreads, stream, p, tokens)
+              : launch_chained(two ? rotary_kernel<false, true> : rotary_kernel<false, false>, grid, kRotaryThreads, stream, p, tokens);
     if (rc != NB_OK) return rc;
     ++g_launches;
     return NB_OK;

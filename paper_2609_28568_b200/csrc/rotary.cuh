@@ -45,15 +45,16 @@ __device__ __forceinline__ int rotary_position(const RotaryParams &p, int row, b
     return row - max(p.cu[lo], 0);
 }
 
-// One thread's piece of a head: two vectors of eight that hold eight pairs, or one that holds four or is only copied.
+// One thread's piece of a head: two vectors of eight that hold eight pairs, or, where the columns are no multiples of 16, one that holds four or is only copied. (Pieces of two
+// where they are: 16384 rows of 12 heads of 80, 32 columns turned: 16.2 us, of one 18.4; 8192 of 24 of 128, 64 turned: 20.6, 25.0.)
 struct RotaryItem {
     uint4 a, b;
-    const __nv_bfloat16 *in;
-    __nv_bfloat16 *out;
+    __nv_bfloat16 *out;  // null: it stays as it is
 };
 
-template <bool HALF>
-__global__ void __launch_bounds__(kRotaryThreads)
+// TWO: pieces that are copied or hold neighbours are of two vectors (where the numbers of columns allow it)
+template <bool HALF, bool TWO>
+__global__ void __launch_bounds__(kRotaryThreads, 5)
 rotary_kernel(const RotaryParams p, int tokens)
 {
     // (cos, sin) of a token's pairs, two to a piece of 16 bytes; piece u stands at u ^ (u >> 3), so that eight threads that read theirs of
@@ -66,10 +67,12 @@ rotary_kernel(const RotaryParams p, int tokens)
     const int row0 = static_cast<int>(blockIdx.x) * tokens, count = min(tokens, p.T - row0);
     const int pairs = p.R / 2, H = p.heads[0] + p.heads[1];
     // pieces of a head: a thread keeps its own, and walks the heads of the block's tokens with the others that have the same
-    const int turned = HALF ? p.R / 16 : p.R / 8, per = turned + (p.D - p.R) / 8;
+    constexpr int vectors = TWO ? 2 : 1;
+    const int turned = p.R / (HALF ? 16 : 8 * vectors), per = turned + (p.D - p.R) / (8 * vectors);
     const int it = tid % per, stride = kRotaryThreads / per;
     const bool turns = it < turned;
-    const int col = turns ? it * 8 : p.R + (it - turned) * 8;
+    const int col = HALF && turns ? it * 8 : turns ? it * 8 * vectors : p.R + (it - turned) * 8 * vectors;
+    const int second = HALF && turns ? pairs : TWO ? 8 : 0;  // columns from the first vector to the second; 0: there is none
     int tok = 0, h = tid / per;
     bool more = h < stride;
     auto settle = [&] {
@@ -82,10 +85,12 @@ rotary_kernel(const RotaryParams p, int tokens)
     auto load = [&](RotaryItem &x) {
         const int t = h < p.heads[0] ? 0 : 1, hh = t ? h - p.heads[0] : h;
         const long long row = row0 + tok;
-        x.in = static_cast<const __nv_bfloat16 *>(t ? p.in[1] : p.in[0]) + row * (t ? p.ld_in[1] : p.ld_in[0]) + hh * p.D + col;
+        const auto *in = static_cast<const __nv_bfloat16 *>(t ? p.in[1] : p.in[0]) + row * (t ? p.ld_in[1] : p.ld_in[0]) + hh * p.D + col;
         x.out = static_cast<__nv_bfloat16 *>(t ? p.out[1] : p.out[0]) + row * (t ? p.ld_out[1] : p.ld_out[0]) + hh * p.D + col;
-        x.a = ptx::ld_global_v4(x.in);
-        if (HALF && turns) x.b = ptx::ld_global_v4(x.in + pairs);
+        if (!turns && in == x.out) x.out = nullptr;
+        if (TWO && !x.out) return;
+        x.a = ptx::ld_global_v4(in);
+        if (second) x.b = ptx::ld_global_v4(in + second);
     };
     RotaryItem x;
     settle();
@@ -118,9 +123,10 @@ rotary_kernel(const RotaryParams p, int tokens)
         h += stride;
         settle();
         if (more) load(x);
-        if (!in_sequence[now]) continue;
+        if (!in_sequence[now] || !y.out) continue;
         if (!turns) {
-            if (y.in != y.out) *reinterpret_cast<uint4 *>(y.out) = y.a;
+            *reinterpret_cast<uint4 *>(y.out) = y.a;
+            if (TWO) *reinterpret_cast<uint4 *>(y.out + 8) = y.b;
             continue;
         }
         const uint32_t a[4] = {y.a.x, y.a.y, y.a.z, y.a.w}, b[4] = {y.b.x, y.b.y, y.b.z, y.b.w};
@@ -138,15 +144,22 @@ rotary_kernel(const RotaryParams p, int tokens)
             *reinterpret_cast<uint4 *>(y.out) = make_uint4(oa[0], oa[1], oa[2], oa[3]);
             *reinterpret_cast<uint4 *>(y.out + pairs) = make_uint4(ob[0], ob[1], ob[2], ob[3]);
         } else {
+            auto turn4 = [&](const uint32_t *v, uint32_t *o, int first) {
 #pragma unroll
-            for (int k = 0; k < 4; k += 2) {
-                const int u = 2 * it + (k >> 1);
-                const float4 c = cs[u ^ (u >> 3)];
-                const float a0 = ptx::bf16_lo(a[k]), b0 = ptx::bf16_hi(a[k]), a1 = ptx::bf16_lo(a[k + 1]), b1 = ptx::bf16_hi(a[k + 1]);
-                oa[k] = ptx::pack_bf16x2(a0 * c.x - b0 * c.y, b0 * c.x + a0 * c.y);
-                oa[k + 1] = ptx::pack_bf16x2(a1 * c.z - b1 * c.w, b1 * c.z + a1 * c.w);
-            }
+                for (int k = 0; k < 4; k += 2) {
+                    const int u = first + (k >> 1);
+                    const float4 c = cs[u ^ (u >> 3)];
+                    const float a0 = ptx::bf16_lo(v[k]), b0 = ptx::bf16_hi(v[k]), a1 = ptx::bf16_lo(v[k + 1]), b1 = ptx::bf16_hi(v[k + 1]);
+                    o[k] = ptx::pack_bf16x2(a0 * c.x - b0 * c.y, b0 * c.x + a0 * c.y);
+                    o[k + 1] = ptx::pack_bf16x2(a1 * c.z - b1 * c.w, b1 * c.z + a1 * c.w);
+                }
+            };
+            turn4(a, oa, 2 * it * vectors);
             *reinterpret_cast<uint4 *>(y.out) = make_uint4(oa[0], oa[1], oa[2], oa[3]);
+            if (TWO) {
+                turn4(b, ob, 2 * it * vectors + 2);
+                *reinterpret_cast<uint4 *>(y.out + 8) = make_uint4(ob[0], ob[1], ob[2], ob[3]);
+            }
         }
     }
 }

@@ -153,3 +153,23 @@ def test_captured():
     torch.cuda.synchronize()
     for a, b in zip(held, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("D,R,layout", [(80, 32, NEIGHBOURS), (96, 64, HALF), (128, 64, HALF), (128, 32, NEIGHBOURS), (72, 16, NEIGHBOURS), (24, 8, NEIGHBOURS), (40, 16, HALF),
+                                        (48, 48, NEIGHBOURS), (104, 80, HALF)])
+def test_part_of_a_head(D, R, layout):
+    """Columns that are copied, in pieces of one or two vectors; in place they are left alone, NaN among them."""
+    c = Case([70, 1, 30], 6, 2, D, first=3, pad=9, fused=True)
+    check(c, R, layout)
+    check(c, R, layout, inverse=True, scale=0.75)
+    f = nb.rotary_frequencies(R)
+    want = nb.rotary(c.q, c.k, f, cu_seqlens=c.cu, layout=layout)
+    v = c.v.clone()
+    if R < D:
+        c.q[20, 1, R], c.k[20, 1, D - 1] = math.nan, math.inf
+        want[0][20, 1, R], want[1][20, 1, D - 1] = math.nan, math.inf
+    nb.rotary(c.q, c.k, f, cu_seqlens=c.cu, layout=layout, in_place=True)
+    rows = slice(3, 104)
+    for got, w in zip((c.q, c.k, c.v), (*want, v)):
+        assert torch.equal(got[rows].nan_to_num(nan=9.0, posinf=8.0), w[rows].nan_to_num(nan=9.0, posinf=8.0))
+        assert torch.isnan(got[:3]).all() and torch.isnan(got[104:]).all()
