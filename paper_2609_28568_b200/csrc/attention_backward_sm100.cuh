@@ -344,8 +344,8 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                 else if (half == 0 && !b.side && (!SPLIT || own.first == 0)) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
             }
             const ptx::f2 base = ptx::make_f2(nl, nl), nd2 = ptx::make_f2(-delta, -delta);
-            // keys that all rows of the warp see, that this one sees
-            const int seen_by_all = min(m.len, p.causal ? row - lane + 1 : m.len), seen = min(m.len, p.causal ? row + 1 : m.len);
+            // keys that all rows of the warp see, that this one sees. Of one key alone the gradient is zero (formed, it would be the rounding of dP - delta)
+            const int seen_by_all = min(m.len, p.causal ? row - lane + 1 : m.len), sees = min(m.len, p.causal ? row + 1 : m.len), seen = sees == 1 ? 0 : sees;
             bool ok = true;
             for (int j = 0; j < n; ++j) {
                 const uint32_t r = done + j, s_tm = tmem + lanes + (r & 1) * ROWS + half * 64;
@@ -691,6 +691,8 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             const int n = own.n;
             if (SPLIT) shared = m;
             if (SPLIT && n == 0) continue;
+            // the first key is all that the first query sees, and has no gradient from it
+            const bool lonely = (p.causal || m.len == 1) && m.block == 0 && r == 0 && half == 0;
             bool ok = true;
             int t = own.first % per_head;
             for (int i = 0; i < n; ++i, ++it) {
@@ -757,6 +759,10 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                         pk[e] &= keep;
                         lo[e] &= keep;
                     }
+                }
+                if (lonely && first + t == 0) {
+                    pk[0] &= 0xffff0000u;
+                    lo[0] &= 0xffff0000u;
                 }
                 ptx::tmem_st_32x32(dp_tm + lanes + half * 64, pk);
                 ptx::tmem_st_32x32(dp_tm + lanes + half * 64 + 32, lo);

@@ -168,3 +168,23 @@ def test_timeout(which):
     for x in (out, lse, dq, dk, dv):
         assert (x == 5.0).all()
     check(Case([2000], 1, 1, 64))  # and the device is as it was
+
+
+@pytest.mark.parametrize("heads,kv,D", [(3, 3, 64), (8, 1, 64), (4, 2, 128), (12, 1, 128), (300, 300, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_one_key_alone_has_no_gradient(heads, kv, D, causal):
+    """Its probability is one whatever its score. (dP and delta, summed in different orders, differ in their last bits.)"""
+    lengths = [1, 1, 40, 1, 300]
+    c = Case(lengths, heads, kv, D, seed=7, pad=3)
+    out, lse, grads, ws = tensors(c)
+    ld, wide = [t.stride(0) for t in (c.q, c.k, c.v)], c.heads * c.D
+    nb.nb_attention_forward(out, lse, c.q, c.k, c.v, c.cu, c.T, 5, heads, kv, D, wide, *ld, D ** -0.5, causal)
+    nb.nb_attention_backward(*grads, c.dout, out, lse, c.q, c.k, c.v, c.cu, c.T, 5, heads, kv, D, *(g.stride(0) for g in grads), wide, wide, *ld, D ** -0.5, causal,
+                             ws, ws.numel())
+    dq, dk, dv = grads
+    for row in (0, 1, 42):
+        assert (dq[row] == 0).all() and (dk[row] == 0).all()
+        want = c.dout[row].double().unflatten(0, (kv, heads // kv)).sum(1)
+        assert ((dv[row].double() - want).abs() <= want.abs() * 2.0 ** -8 + c.dout[row].abs().max().double() * heads * 2.0 ** -20).all()
+    for row in (2, 43):
+        assert (dq[row] == 0).all() == causal
