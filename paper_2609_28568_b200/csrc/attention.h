@@ -5,6 +5,7 @@
 namespace nb {
 
 constexpr int kStatusBadSequences = 6;
+constexpr int kAttnFirst = 1, kAttnSecond = 2;  // AttnBackward::side
 
 struct AttnParams {
     int T, n, heads, group;  // group: queries' heads per head of keys
@@ -24,7 +25,7 @@ struct AttnParams {
 struct AttnBackward {
     AttnParams a;            // a.out: the forward pass's output, a.ld_out its ld; a.lse: read
     float *delta;            // [heads, T]: sum over a row of dout out, for the pass of dk and dv
-    int side;                // the passes run side by side: delta is there before either of them
+    int side;                // 0, or the pass's place among two that run side by side: delta is there before either of them
     const void *dout;
     void *dq, *dk, *dv;
     long long ld_dout, ld_dq, ld_dk, ld_dv;

@@ -23,8 +23,7 @@
 // Few items with much to walk over (one head of keys for many of queries: a block has all their tiles) are shared by the blocks of a cluster as in the forward
 // pass (SPLIT), which add up their sums in a fixed order.
 //
-// Passes that fill the GPU follow one another, and that of dQ leaves delta behind. Where both together do not, delta has a kernel of its own, and dQ and dK, dV run side by side:
-// the pass of dQ lets its successor start when delta and all inputs are there, and dK and dV's blocks wait for dQ's at their end only.
+// Passes that fill the GPU follow one another, and that of dQ leaves delta behind. Where both together do not, delta has a kernel of its own, and dQ and dK, dV run side by side.
 #pragma once
 #include "attention_sm100.cuh"
 
@@ -94,6 +93,18 @@ attn_backward_delta_kernel(const AttnBackward b)
     if (row < p.T && piece == 0) b.delta[static_cast<long long>(head) * p.T + row] = sum;
 }
 
+// Side by side: the first pass lets the second start when delta and all inputs are there, the second waits for the first at its end, so that what follows waits for both.
+__device__ __forceinline__ void attn_backward_begin(int side)
+{
+    if (side != kAttnFirst) ptx::grid_launch_dependents();
+    if (side != kAttnSecond) ptx::grid_dependency_wait();
+    if (side == kAttnFirst) ptx::grid_launch_dependents();
+}
+__device__ __forceinline__ void attn_backward_end(int side)
+{
+    if (side == kAttnSecond) ptx::grid_dependency_wait();
+}
+
 // ------------------------------------------------------------------------------------------------ dQ
 template <class Cfg, bool SPLIT>
 __global__ void __launch_bounds__(Cfg::THREADS, Cfg::BLOCKS)
@@ -151,9 +162,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         ptx::tc_fence_after();
     }
     const uint32_t tmem = ptx::ld_shared_u32_volatile(tmem_slot);
-    if (!b.side) ptx::grid_launch_dependents();
-    ptx::grid_dependency_wait();
-    if (b.side) ptx::grid_launch_dependents();  // dK and dV may start: all that they read is there
+    attn_backward_begin(b.side);
     const uint32_t dp_tm = tmem + 2 * ROWS, dq_tm = tmem + 3 * ROWS;  // scores: two tiles from 0 on
     auto tiles_of = [&](const AttnItem &m) {  // tiles of keys that an item's queries see
         const int tiles = (m.len + ROWS - 1) / ROWS;
@@ -441,6 +450,7 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         ptx::tc_fence_after();
         ptx::tmem_dealloc<1>(tmem, Cfg::TMEM);
     }
+    attn_backward_end(b.side);
 }
 
 // ------------------------------------------------------------------------------------------------ dK, dV
@@ -502,8 +512,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         ptx::tc_fence_after();
     }
     const uint32_t tmem = ptx::ld_shared_u32_volatile(tmem_slot);
-    ptx::grid_launch_dependents();
-    if (!b.side) ptx::grid_dependency_wait();
+    attn_backward_begin(b.side);
     const int kv_heads = p.heads / p.group;
     const uint32_t s_tm = tmem, dp_tm = tmem + ROWS, dv_tm = tmem + 2 * ROWS, dk_tm = dv_tm + D;
     // tiles of queries that see an item's keys: from first_of on, per head
@@ -829,7 +838,7 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         ptx::tc_fence_after();
         ptx::tmem_dealloc<1>(tmem, Cfg::TMEM);
     }
-    if (b.side) ptx::grid_dependency_wait();  // what waits for this pass waits for that of dQ too
+    attn_backward_end(b.side);
 }
 
 }  // namespace nb
