@@ -438,6 +438,7 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
  * Sums are fp32 and in a fixed order: the same inputs give the same bits. For the tensor cores p is rounded to bf16 and ds given
  * in two pieces of bf16, rounded and what that left out; gradients are rounded once at the end.
  * A query that sees one key alone (the first of a causal sequence) has a gradient of exactly zero, and so has that key from it, if its scores and dout are finite.
+ * A key whose score is -infinity for all queries that see it gets gradients dk and dv of exactly zero (dq is the sum that it is: zero times that key's infinity is not a number).
  * Rows in no sequence are not written. What is not finite in one sequence reaches no other.
  * nb_attention_workspace returns -1 for sizes that the call would refuse.
  */

@@ -567,7 +567,10 @@ attn_backward_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                         if (part) {  // the last tile of each head's queries, then of their gradients
                             ok = warp_wait(wctx, part_bar, parts++ & 1u, 150);
                             if (!ok) break;
-                            attn_zero_rows<D, ROWS>(dst, valid, up);
+                            // Queries are filled up with the last one: a key with a score of -infinity for all of them has P = 0 there too (with
+                            // queries of zeros its infinity would make NaN)
+                            if (i & 1) attn_zero_rows<D, ROWS>(dst, valid, up);
+                            else attn_repeat_row<D, ROWS>(dst, valid, up);
                             ptx::fence_proxy_async_smem();
                             __syncwarp();
                             if (lane == 0) ptx::mbar_arrive(full_bar(stage));

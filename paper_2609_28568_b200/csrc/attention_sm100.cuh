@@ -7,7 +7,7 @@
 // Tiles are 128 rows of a sequence by 64 or 128 columns (D rounded up: what lies beyond D reads as zero), fetched by TMA in
 // boxes of 128 rows x 64 columns of one head with the 128-byte swizzle. A sequence's last tile ends inside a box: the
 // rows after it are another sequence's or nobody's, and where they would enter a sum as 0 x value they are overwritten with zeros
-// in shared memory (they may hold infinities or NaN).
+// in shared memory (they may hold infinities or NaN), or, of queries that keys walk over, with the sequence's last query.
 #pragma once
 #include "attention.h"
 #include "gemm_sm100.cuh"
@@ -286,6 +286,20 @@ __device__ __forceinline__ void attn_zero_rows(uint32_t tile, int from, int to)
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
         for (int i = lane; i < (to - from) * 8; i += 32) ptx::st_shared_v4(tile + c * ROWS * 128 + from * 128 + i * 16, 0, 0, 0, 0);
+}
+// Rows [from, to) of a tile become its row from - 1, by one warp. (A row's pieces of 16 bytes stand where the swizzle puts them.)
+template <int D, int ROWS>
+__device__ __forceinline__ void attn_repeat_row(uint32_t tile, int from, int to)
+{
+    const int lane = static_cast<int>(threadIdx.x & 31);
+    auto at = [&](int row, int piece) { return tile + static_cast<uint32_t>(row * 128 + ((piece ^ (row & 7)) << 4)); };
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+        for (int i = lane; i < (to - from) * 8; i += 32) {
+            uint32_t v[4];
+            ptx::ld_shared_v4(at(from - 1, i & 7) + c * ROWS * 128, v[0], v[1], v[2], v[3]);
+            ptx::st_shared_v4(at(from + (i >> 3), i & 7) + c * ROWS * 128, v[0], v[1], v[2], v[3]);
+        }
 }
 
 // D[128, N] = A B^T over `steps` pieces of 16 columns, tiles A (128 rows) and B (N rows) with the summed index contiguous (boxes of 64 columns).
