@@ -531,9 +531,9 @@ def _sequences(cu_seqlens, n: int, T: int, **others) -> int:
     return len(cu_seqlens) - 1
 
 
-def _like(t, cu_seqlens, shape=None, dtype=torch.bfloat16):
+def _like(t, cu_seqlens, n, shape=None, dtype=torch.bfloat16):
     """A dense tensor of t's shape; of zeros where there may be rows in no sequence, which a call does not write."""
-    make = torch.empty if cu_seqlens is None else torch.zeros
+    make = torch.empty if cu_seqlens is None and n > 0 else torch.zeros
     return make(t.shape if shape is None else shape, dtype=dtype, device=t.device)
 
 
@@ -547,8 +547,8 @@ def rotary(q, k, freq, positions=None, cu_seqlens=None, n=1, scale=1.0, layout=R
     _want(freq, torch.float64, (freq.numel(),), "freq")
     _want(positions, torch.int32, (T,), "positions")
     n = _sequences(cu_seqlens, n, T, k=k)
-    out_q = q if in_place else _like(q, cu_seqlens)
-    out_k = k if in_place or k is None else _like(k, cu_seqlens)
+    out_q = q if in_place else _like(q, cu_seqlens, n)
+    out_k = k if in_place or k is None else _like(k, cu_seqlens, n)
     nb_rotary(out_q, out_k, q, k, freq, positions, cu_seqlens, T, n, heads, kv_heads, D, 2 * freq.numel(), ld_q if in_place else heads * D,
               ld_k if in_place else kv_heads * D, ld_q, ld_k, scale, layout, int(inverse))
     return out_q, out_k
@@ -567,8 +567,8 @@ def attention_forward(q, k, v, cu_seqlens=None, n=1, scale=None, causal=True, tr
     T = q.shape[0]
     heads, kv_heads, D, ld_q, ld_k, ld_v = _attention_sizes(q, k, v)
     n = _sequences(cu_seqlens, n, T, k=k, v=v)
-    out = _like(q, cu_seqlens)
-    lse = _like(q, cu_seqlens, (heads, T), torch.float32) if train else None
+    out = _like(q, cu_seqlens, n)
+    lse = _like(q, cu_seqlens, n, (heads, T), torch.float32) if train else None
     nb_attention_forward(out, lse, q, k, v, cu_seqlens, T, n, heads, kv_heads, D, heads * D, ld_q, ld_k, ld_v, D ** -0.5 if scale is None else scale,
                          int(causal))
     return out, lse
@@ -583,7 +583,7 @@ def attention_backward(dout, out, lse, q, k, v, cu_seqlens=None, n=1, scale=None
     for t, name in ((dout, "dout"), (out, "out")):
         _want(t, torch.bfloat16, q.shape, name)
     _want(lse, torch.float32, (heads, T), "lse")
-    dq, dk, dv = grads if grads is not None else (_like(t, cu_seqlens) for t in (q, k, v))
+    dq, dk, dv = grads if grads is not None else (_like(t, cu_seqlens, n) for t in (q, k, v))
     for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
         _want(t, torch.bfloat16, like.shape, name)
     ws = torch.empty(nb_attention_workspace(T, heads), dtype=torch.uint8, device=q.device)
