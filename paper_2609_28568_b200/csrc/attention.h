@@ -24,7 +24,7 @@ struct AttnParams {
 
 struct AttnBackward {
     AttnParams a;            // a.out: the forward pass's output, a.ld_out its ld; a.lse: read
-    float *delta;            // [heads, T]: sum over a row of dout out, for the pass of dk and dv
+    float *delta;            // [heads, T]: sum over a row of dout out, for the pass of dk and dv (side by side: for both)
     int side;                // 0, or the pass's place among two that run side by side: delta is there before either of them
     const void *dout;
     void *dq, *dk, *dv;

@@ -94,6 +94,9 @@ attn_backward_delta_kernel(const AttnBackward b)
 }
 
 // Side by side: the first pass lets the second start when delta and all inputs are there, the second waits for the first at its end, so that what follows waits for both.
+// The second starts when every block of the first has either said so, which each does after its own wait for all that came before the passes (delta's kernel, and through its
+// wait what it waited for: their writes are in L2 then), or has been taken off the grid. Nothing else orders the second's reads behind those writes, so all of them go to L2:
+// tiles by TMA, lse, delta and cu_seqlens by __ldcg. Neither pass reads through L1, whose lines may be of a time before.
 __device__ __forceinline__ void attn_backward_begin(int side)
 {
     if (side != kAttnFirst) ptx::grid_launch_dependents();
@@ -303,17 +306,24 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         // one another: a row a lane took the loads eight times as long.
         constexpr int LANES = D / 8, AT_ONCE = 32 / LANES, READS = 32 / AT_ONCE;
         const int piece = lane % LANES, sub = lane / LANES;
+        // Side by side delta is there already, and the pass may run before its own wait for what came earlier: nothing of out is read then (see attn_backward_begin).
+        // Passes of one warpgroup are of many items, which never run so.
+        const bool side = WGS == 2 && b.side != 0;
         uint4 y[READS];
-        float l;
-        // an item's rows of out and lse, on their way while the item before is still being stored
+        float l, given = 0.0f;
+        // an item's rows of out (or delta) and lse, on their way while the item before is still being stored
         auto fetch = [&](const AttnItem &m) {
             const int row0 = m.block * 128 + q * 32;
+            if (side) {
+                if (row0 + lane < m.len) given = __ldcg(b.delta + static_cast<long long>(m.head) * p.T + m.start + row0 + lane);
+            } else {
 #pragma unroll
-            for (int c = 0; c < READS; ++c) {
-                const int row = row0 + c * AT_ONCE + sub;
-                y[c] = make_uint4(0, 0, 0, 0);
-                if (row < m.len && piece * 8 < p.D)
-                    y[c] = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(p.out) + (m.start + row) * p.ld_out + m.head * p.D + piece * 8);
+                for (int c = 0; c < READS; ++c) {
+                    const int row = row0 + c * AT_ONCE + sub;
+                    y[c] = make_uint4(0, 0, 0, 0);
+                    if (row < m.len && piece * 8 < p.D)
+                        y[c] = ptx::ld_global_v4(static_cast<const __nv_bfloat16 *>(p.out) + (m.start + row) * p.ld_out + m.head * p.D + piece * 8);
+                }
             }
             l = row0 + lane < m.len ? __ldcg(p.lse + static_cast<long long>(m.head) * p.T + m.start + row0 + lane) : 0.0f;
         };
@@ -334,7 +344,9 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
             // delta: out from memory, dout from the item's tile. Where two threads have a row, both form all of it: a meeting of theirs could not be left
             // when a wait has run out elsewhere
             if (!warp_wait(wctx2, do_bar, static_cast<uint32_t>(k) & 1u, 430)) break;
-            {
+            if (side) {
+                delta = given;
+            } else {
                 const uint32_t do_s = smem + Cfg::OFF_OWN + Cfg::OWN + (piece >> 3) * kAttnBox;
 #pragma unroll
                 for (int c = 0; c < READS; ++c) {
@@ -347,11 +359,11 @@ attn_backward_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
                     part = __shfl_sync(0xffffffffu, part, (lane % AT_ONCE) * LANES);  // row c AT_ONCE + i stands in the i-th group
                     if (lane / AT_ONCE == c) delta = part;
                 }
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(own_bar);  // this warp has read the item's tile
-                if (row >= m.len) delta = 0.0f;  // dout may hold anything there
-                else if (half == 0 && !b.side && (!SPLIT || own.first == 0)) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
             }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(own_bar);  // this warp has read the item's tile
+            if (row >= m.len) delta = 0.0f;  // dout may hold anything there
+            else if (half == 0 && !side && (!SPLIT || own.first == 0)) b.delta[static_cast<long long>(m.head) * p.T + at] = delta;
             const ptx::f2 base = ptx::make_f2(nl, nl), nd2 = ptx::make_f2(-delta, -delta);
             // keys that all rows of the warp see, that this one sees. Of one key alone the gradient is zero (formed, it would be the rounding of dP - delta)
             const int seen_by_all = min(m.len, p.causal ? row - lane + 1 : m.len), sees = min(m.len, p.causal ? row + 1 : m.len), seen = sees == 1 ? 0 : sees;
