@@ -411,6 +411,7 @@ int nb_rotary(void *out_q, void *out_k, const void *q, const void *k, const void
  *                     the tensors is touched, results are undefined) and nb_check_status reports NB_ERR_INVALID_ARG.
  *   scale       positive and finite
  * D a multiple of 8, at most NB_HEAD_MAX_D; heads a multiple of kv_heads, at most NB_HEAD_MAX_HEADS; ld_* multiples of 8, at least the row's width. Pointers 16-byte aligned (lse and cu_seqlens: 4).
+ * T / 128 + n times heads below 2^31 (without cu_seqlens: the blocks of 128 rows of all sequences, times heads); attention refuses more.
  * An output that overlaps another argument is refused (columns of one buffer with one ld do not overlap).
  * Scores, their maximum and sum, and the output's sums are fp32; probabilities are rounded to bf16 for the product with v. T == 0 and n == 0 do nothing.
  * What is not finite in one sequence, or in rows that belong to none, reaches no other sequence. Within a sequence an infinity or a NaN

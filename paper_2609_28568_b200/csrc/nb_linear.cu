@@ -2223,11 +2223,14 @@ AttnParams attn_params(const DeviceState &s, int64_t T, int64_t n, int64_t heads
 }
 
 // Slots for blocks of `rows` rows, no fewer than there are (AttnOrder).
-int64_t attn_slots(const AttnParams &p, int rows)
+int64_t attn_slots(int64_t T, int64_t n, const void *cu, int rows)
 {
-    if (p.cu) return p.T / rows + p.n;
-    const int64_t len = p.T / p.n;
-    return p.n * ((len + rows - 1) / rows);
+    return cu ? T / rows + n : n * ((T / n + rows - 1) / rows);
+}
+// A launch has fewer than 2^31 blocks, and so many slots times heads are numbers of 32 bits on the device. (Items that clusters share are few.)
+int check_slots(int64_t T, int64_t n, int64_t heads, const void *cu)
+{
+    return attn_slots(T, n, cu, 128) * heads < (1ll << 31) ? NB_OK : fail(NB_ERR_UNSUPPORTED, "too many tiles");
 }
 
 // Blocks that share an item: a power of two with which all items have no more than `most` and an item of so many tiles leaves `least` to each. A cluster of blocks costs a
@@ -2268,8 +2271,7 @@ int launch_attention(const AttnKernel &k, bool (&attr_set)[kMaxDevices], CUtenso
         NB_CUDA(cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem)));
         attr_set[dev] = true;
     }
-    const int64_t blocks = attn_slots(a, k.rows) * heads * a.parts;
-    if (blocks >= (1ll << 31)) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
+    const int64_t blocks = attn_slots(a.T, a.n, a.cu, k.rows) * heads * a.parts;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(static_cast<unsigned>(k.threads));
@@ -3088,6 +3090,7 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
         return rc;
     if (!(scale > 0.0f) || scale > 3.0e38f) return fail(NB_ERR_INVALID_ARG, "scale must be positive and finite");
     if (T == 0 || n == 0) return NB_OK;  // tensors without elements have no address
+    if ((rc = check_slots(T, n, heads, cu_seqlens)) != NB_OK) return rc;
     if (!out || !q || !k || !v) return fail(NB_ERR_INVALID_ARG, "out, q, k and v must not be NULL");
     if (!aligned16(out) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned4(lse) || !aligned4(cu_seqlens))
         return fail(NB_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, lse and cu_seqlens 4-byte aligned");
@@ -3106,7 +3109,7 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
     // 2000 x 16 of 128 34, 39, 70, 130; 3000 x 4 34, 27, 29, 43; 3000 x 8 41, 31, 47, 84; 4096 x 4 49, 35, 35, 61; 4096 x 8 56, 43, 67, 115; 4096 x 12 57, 64, 97, 171;
     // 8192 x 2 90, 59, 47, 76; 8192 x 4 of 128 110, 74, 110, 180; 16384 x 1 of 128 191, 120, 83, 122; whole: 2000 x 1 of 128 25, 21, 18, 19; 2000 x 4 30, 23, 18, 36;
     // 2000 x 12 34, 40, 49, 88; 4096 x 2 of 128 56, 40, 31, 55. (Of a causal mask's items half are short.)
-    const int64_t items = attn_slots(p, 128) * heads, tiles = T / n / 64 + 1;
+    const int64_t items = attn_slots(T, n, cu_seqlens, 128) * heads, tiles = T / n / 64 + 1;
     p.parts = attn_parts(items, tiles, 2ll * s->num_sms, 6);
     if (causal) p.parts = std::max(p.parts, attn_parts(items, tiles, 4ll * s->num_sms, 20));
     const AttnKernel kernel = attn_forward(p.D, p.parts > 1);
@@ -3138,6 +3141,7 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
         return rc;
     if (!(scale > 0.0f) || scale > 3.0e38f) return fail(NB_ERR_INVALID_ARG, "scale must be positive and finite");
     if (T == 0 || n == 0) return NB_OK;  // tensors without elements have no address
+    if ((rc = check_slots(T, n, heads, cu_seqlens)) != NB_OK) return rc;
     if (!dq || !dk || !dv || !dout || !out || !lse || !q || !k || !v)
         return fail(NB_ERR_INVALID_ARG, "dq, dk, dv, dout, out, lse, q, k and v must not be NULL");
     if (!aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dout) || !aligned16(out) || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
@@ -3168,7 +3172,7 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
     b.ld_dq = ld_dq;
     b.ld_dk = ld_dk;
     b.ld_dv = ld_dv;
-    const int64_t slots = attn_slots(b.a, 128);
+    const int64_t slots = attn_slots(T, n, cu_seqlens, 128);
     // Heads of up to 64 columns, passes of few items: a block to itself on an SM, with tiles twice as long, in place of two blocks. An item is done in little
     // more than half the time, which counts where the longest one does (both passes, in us, two blocks / one: 500 x 12 heads 32 / 23, 1000 x 12 54 / 35,
     // 2000 x 12 98 / 57, 3000 x 16 134 / 117; 4 x 1024 x 12, 384 items: 58 / 57, 8 x 1024: 99 / 104, 16 x 1024: 176 / 187).
