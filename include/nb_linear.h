@@ -409,7 +409,7 @@ int nb_rotary(void *out_q, void *out_k, const void *q, const void *k, const void
  *   cu_seqlens  [in]  [n + 1] int32 on the device, rising (equal neighbours: an empty sequence) within [0, T]; or NULL: n sequences of T / n rows.
  *                     Rows in no sequence are neither used nor written. Bounds that fall or lie outside [0, T] are cut (nothing outside
  *                     the tensors is touched, results are undefined) and nb_check_status reports NB_ERR_INVALID_ARG.
- *   scale       positive and finite
+ *   scale       positive, at most 2^127
  * D a multiple of 8, at most NB_HEAD_MAX_D; heads a multiple of kv_heads, at most NB_HEAD_MAX_HEADS; ld_* multiples of 8, at least the row's width. Pointers 16-byte aligned (lse and cu_seqlens: 4).
  * T / 128 + n times heads below 2^31 (without cu_seqlens: the blocks of 128 rows of all sequences, times heads); attention refuses more.
  * An output that overlaps another argument is refused (columns of one buffer with one ld do not overlap).

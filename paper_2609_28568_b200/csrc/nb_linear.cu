@@ -3088,7 +3088,7 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
     if ((rc = check_ld("out", ld_out, heads * D)) != NB_OK || (rc = check_ld("q", ld_q, heads * D)) != NB_OK ||
         (rc = check_ld("k", ld_k, kv_heads * D)) != NB_OK || (rc = check_ld("v", ld_v, kv_heads * D)) != NB_OK)
         return rc;
-    if (!(scale > 0.0f) || scale > 3.0e38f) return fail(NB_ERR_INVALID_ARG, "scale must be positive and finite");
+    if (!(scale > 0.0f) || scale > 0x1p127f) return fail(NB_ERR_INVALID_ARG, "scale must be positive and at most 2^127");  // 1.44 times it is finite
     if (T == 0 || n == 0) return NB_OK;  // tensors without elements have no address
     if ((rc = check_slots(T, n, heads, cu_seqlens)) != NB_OK) return rc;
     if (!out || !q || !k || !v) return fail(NB_ERR_INVALID_ARG, "out, q, k and v must not be NULL");
@@ -3139,7 +3139,7 @@ int nb_attention_backward(void *dq, void *dk, void *dv, const void *dout, const 
         (rc = check_ld("dout", ld_dout, wide)) != NB_OK || (rc = check_ld("out", ld_out, wide)) != NB_OK || (rc = check_ld("q", ld_q, wide)) != NB_OK ||
         (rc = check_ld("k", ld_k, narrow)) != NB_OK || (rc = check_ld("v", ld_v, narrow)) != NB_OK)
         return rc;
-    if (!(scale > 0.0f) || scale > 3.0e38f) return fail(NB_ERR_INVALID_ARG, "scale must be positive and finite");
+    if (!(scale > 0.0f) || scale > 0x1p127f) return fail(NB_ERR_INVALID_ARG, "scale must be positive and at most 2^127");  // 1.44 times it is finite
     if (T == 0 || n == 0) return NB_OK;  // tensors without elements have no address
     if ((rc = check_slots(T, n, heads, cu_seqlens)) != NB_OK) return rc;
     if (!dq || !dk || !dv || !dout || !out || !lse || !q || !k || !v)

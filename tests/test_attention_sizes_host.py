@@ -31,3 +31,10 @@ def backward(L, T, n, heads, D=8, cu=at(9), scale=0.125):
 @pytest.mark.parametrize("call", [forward, backward])
 def test_too_many_blocks(L, call, T, n, heads):
     assert call(L, T, n, heads) == nb.NB_ERR_UNSUPPORTED and b"too many tiles" in L.nb_last_error()
+
+
+@pytest.mark.parametrize("scale", [1.8e38, 2.5e38, 3.2e38])
+@pytest.mark.parametrize("call", [forward, backward])
+def test_scales_that_leave_the_type(L, call, scale):
+    """Scores are formed in units of log 2, for which 1.44 times the scale has to be a number too."""
+    assert call(L, 300, 2, 4, scale=scale) == nb.NB_ERR_INVALID_ARG and b"scale" in L.nb_last_error()
