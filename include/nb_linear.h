@@ -385,7 +385,8 @@ int nb_muon_apply(void *const *master, void *const *weight, const void *const *u
  *
  * nb_rotary_frequencies writes to host memory, freq[j] = base^(-2 j / R), for j < R / 2. Scaled contexts: with original == 0 all
  * of them divided by factor; with original > 0 by parts: those that turn more than `high` times over `original` positions stay, those that turn
- * less than `low` times are divided by factor, with a straight line (of freq over the turns) between.
+ * less than `low` times are divided by factor, with a straight line (of freq over the turns) between. Other ramps (over the pairs' index, as some
+ * programs have it) are tables of the caller's own: nb_rotary takes any.
  */
 #define NB_ROTARY_HALF 0
 #define NB_ROTARY_NEIGHBOURS 1
@@ -416,6 +417,7 @@ int nb_rotary(void *out_q, void *out_k, const void *q, const void *k, const void
  * Scores, their maximum and sum, and the output's sums are fp32; probabilities are rounded to bf16 for the product with v. T == 0 and n == 0 do nothing.
  * What is not finite in one sequence, or in rows that belong to none, reaches no other sequence. Within a sequence an infinity or a NaN
  * in v may reach the rows of the 128 before it too, which do not see it.
+ * The same call gives the same bits. A sequence's bits may change in their last places with what else is in the call: the sizes of all of it choose the kernels' tiles and whether several blocks share a row's keys.
  */
 #define NB_HEAD_MAX_D 128
 #define NB_HEAD_MAX_HEADS 1024
@@ -436,11 +438,12 @@ int nb_attention_forward(void *out, void *lse, const void *q, const void *k, con
  *   dout, out  [in]  [T, heads, D] bf16;  lse [in] [heads, T] fp32;  the rest as in the forward pass
  *   workspace  device memory of nb_attention_workspace(T, heads) bytes, 16-byte aligned, the caller's: calls that may run at the same time (on two streams,
  *              or captured into two graphs) need one each
- * Sums are fp32 and in a fixed order: the same inputs give the same bits. For the tensor cores p is rounded to bf16 and ds given
+ * Sums are fp32 and in a fixed order: the same inputs give the same bits (of a sequence in other company: see the forward pass). For the tensor cores p is rounded to bf16 and ds given
  * in two pieces of bf16, rounded and what that left out; gradients are rounded once at the end.
  * A query that sees one key alone (the first of a causal sequence) has a gradient of exactly zero, and so has that key from it, if its scores and dout are finite.
  * A key whose score is -infinity for all queries that see it gets gradients dk and dv of exactly zero (dq is the sum that it is: zero times that key's infinity is not a number).
- * Rows in no sequence are not written. What is not finite in one sequence reaches no other.
+ * Rows in no sequence are not written. What is not finite in one sequence reaches no other. Within a sequence an infinity or a NaN in k may reach dq of the rows of the 128 before
+ * it, and one in q or dout dk and dv of those of the 128 after it, which it has no part in.
  * nb_attention_workspace returns -1 for sizes that the call would refuse.
  */
 int64_t nb_attention_workspace(int64_t T, int64_t heads);

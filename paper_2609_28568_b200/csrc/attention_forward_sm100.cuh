@@ -265,7 +265,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (j == 0) {
                     top = now;
                 } else {
-                    // only rows that grew that much: a row's bits do not depend on its neighbours
+                    // only rows that grew that much: a row's bits do not depend on the others of its warp
                     const bool grown = (now - top) * sl > 8.0f;
                     if (__any_sync(0xffffffffu, grown)) {
                         const float f = grown ? ptx::ex2_approx((top - now) * sl) : 1.0f;

@@ -4,8 +4,8 @@
 //
 // Rows are tokens, T of them; head h of a tensor is D columns from column h D on, rows are ld elements apart. Sequence i is
 // the rows [cu[i], cu[i+1]) (or T / n rows each), queries' heads h = 0..heads-1 read the keys of head h / (heads / kv_heads).
-// Tiles are 128 rows of a sequence by 64 or 128 columns (D rounded up: what lies beyond D reads as zero), fetched by TMA in
-// boxes of 128 rows x 64 columns of one head with the 128-byte swizzle. A sequence's last tile ends inside a box: the
+// Tiles are rows of a sequence by 64 or 128 columns (D rounded up: what lies beyond D reads as zero): 128 rows of an item's own, 64 or 128 of those that it
+// walks over. TMA fetches them in boxes of so many rows x 64 columns of one head with the 128-byte swizzle. A sequence's last tile ends inside a box: the
 // rows after it are another sequence's or nobody's, and where they would enter a sum as 0 x value they are overwritten with zeros
 // in shared memory (they may hold infinities or NaN), or, of queries that keys walk over, with the sequence's last query.
 #pragma once
